@@ -391,6 +391,146 @@ gp_status gp_recomputed_output(gp_partition* p, void* y, gp_stream stream);
  * GP_ERR_INVALID_ARG: tflops is NULL; GP_ERR_HIP: a launch or event failed. */
 gp_status gp_mfma_peak(void* stream, double* tflops);
 
+/* ------------------------------------------------------------------------
+ * Operators on the caller's own tensors.  They need no partition, allocate
+ * nothing, keep nothing between calls and enqueue on the given stream of the
+ * current device; calls on different streams may overlap as long as their
+ * outputs and workspaces do not.  dtype is a gp_dtype.  All of them may be
+ * recorded into a captured graph (gp_adamw_step: with a device step counter).
+ */
+
+/* The most alternatives gp_token_logprobs gives. */
+#define GP_TOP_MAX 32
+/* In `tokens`: no token here (a padded position). */
+#define GP_NO_TOKEN (-1)
+
+/*
+ * Log probabilities of given tokens under rows of logits, with the entropy of
+ * each row's distribution and its most likely tokens.
+ *   logits  : device [rows, vocab], rows ld elements apart (ld >= vocab).
+ *             x = min(max(z, -clip), clip) with clip > 0, else z; s = scale x
+ *             (scale: 1 / temperature, finite and > 0).
+ *   tokens  : device int32 [rows] in [0, vocab), or GP_NO_TOKEN, whose logp is
+ *             0; any other value gives a NaN.  May be NULL where logp is.
+ *   logp    : s_token - lse.  lse: log sum_v exp(s_v).
+ *   entropy : -sum_v p_v log p_v, p = exp(s - lse).
+ *             Each device fp32 [rows]; any may be NULL.
+ *   top     : 0 .. GP_TOP_MAX (and at most vocab) alternatives.  top_ids (device
+ *             int32) and top_logp (fp32), both [rows, top]: the tokens of the
+ *             largest x, largest first, equal ones by index, and s - lse.
+ *   ws      : device scratch of ws_bytes bytes, 16-byte aligned;
+ *             gp_token_logprobs_workspace says how many make the call fastest.  With
+ *             fewer (0 and NULL included) it gives the same alternatives, and sums
+ *             in another order.
+ * A logit x of -1e30 or less (-inf, or a type's lowest value, as masks leave it) is a
+ * token that cannot occur: p = 0, logp -inf.  A row of nothing else has lse and logp
+ * -inf and entropy 0.
+ * A row with NaN or +inf gives NaN; NaN counts as the largest logit.  Sums are
+ * fp32, in an order that only the sizes and the alignment decide.
+ * GP_ERR_INVALID_ARG: NULL logits, negative sizes, vocab < 1, ld < vocab, scale or
+ *   clip out of range, top out of range or without both outputs, logp without
+ *   tokens, a pointer not aligned to its element, rows > 2^31 - 1.
+ */
+gp_status gp_token_logprobs(int dtype, const void* logits, long rows, int vocab, long ld, const int* tokens,
+                            float scale, float clip, float* logp, float* lse, float* entropy, int top, int* top_ids,
+                            float* top_logp, void* ws, size_t ws_bytes, gp_stream stream);
+gp_status gp_token_logprobs_workspace(int dtype, long rows, int vocab, int top, size_t* bytes);
+
+/*
+ * The gradient of sum_r dlogp_r logp_r + dentropy_r entropy_r with respect to
+ * the logits, from the lse and entropy that gp_token_logprobs gave:
+ *   dz_v = [|z_v| <= clip] scale (dlogp ([v = token] - p_v) - dentropy p_v (s_v - lse + entropy))
+ * (the bracket only with clip > 0).  dlogp and dentropy: device fp32 [rows];
+ * either may be NULL, and then tokens or entropy may be.  A row whose token is
+ * GP_NO_TOKEN takes dlogp as 0, a row with lse = -inf has a zero gradient, a token
+ * outside [0, vocab) gives a row of NaN.
+ *   dlogits : device [rows, vocab] in dtype, rows ldd apart; may be logits itself
+ *             (with ldd = ld), and must not overlap it otherwise.  The ldd - vocab
+ *             elements behind a row are left as they were.
+ * GP_ERR_INVALID_ARG: as gp_token_logprobs; NULL lse or dlogits, neither dlogp
+ *   nor dentropy, an overlap.
+ */
+gp_status gp_token_logprobs_backward(int dtype, const void* logits, long rows, int vocab, long ld, const int* tokens,
+                                     float scale, float clip, const float* lse, const float* entropy,
+                                     const float* dlogp, const float* dentropy, void* dlogits, long ldd,
+                                     gp_stream stream);
+
+/* One gradient of gp_grad_norm: count elements at a device address. */
+typedef struct {
+    const void* grad;
+    long long count;
+} gp_grad_tensor;
+
+/*
+ * The 2-norm over n tensors (host array, dtype all of them) and the factor that
+ * clips it: norm_factor (device fp32 [2]) receives the norm and
+ * min(1, max_norm / norm); 1 for a norm of 0, and NaN where the norm is not finite,
+ * which makes gp_adamw_step leave everything as it was.  Squares are summed in
+ * fp64 in a fixed order.  max_norm > 0; INFINITY gives the norm alone.
+ *   ws : device scratch, 8-byte aligned, of at least the bytes that
+ *        gp_grad_norm_workspace(n, &bytes) names.
+ * n = 0 gives norm 0.  A tensor of count 0 may have a NULL address.
+ * GP_ERR_INVALID_ARG: n < 0, NULL arrays, a negative count, a misaligned address,
+ *   max_norm not > 0, a workspace that is NULL or too small.
+ */
+gp_status gp_grad_norm(int dtype, const gp_grad_tensor* grads, int n, float max_norm, float* norm_factor, void* ws,
+                       size_t ws_bytes, gp_stream stream);
+gp_status gp_grad_norm_workspace(int n, size_t* bytes);
+
+/* Elements that share a scale in 8-bit AdamW states. */
+#define GP_STATE_BLOCK 256
+
+/* One tensor of gp_adamw_step; every address is a device address. */
+typedef struct {
+    void* param;      /* [count] in param_dtype, updated */
+    const void* grad; /* [count] in grad_dtype */
+    void* m;          /* first moment: fp32 [count], or e4m3 bytes [count] */
+    void* v;          /* second moment: fp32 [count], or its square root as e4m3 bytes [count] */
+    float* m_scale;   /* 8-bit states: fp32 [ceil(count / GP_STATE_BLOCK)]; else NULL */
+    float* v_scale;
+    void* copy;       /* fp32 parameters: bf16 [count] that receives the new ones rounded; may be NULL */
+    long long count;
+    double weight_decay;
+} gp_adamw_tensor;
+
+typedef struct {
+    int param_dtype, grad_dtype; /* gp_dtype, of every tensor of the call */
+    int state_bits;              /* 32 or 8 */
+    unsigned seed;               /* 8-bit states: of the random bits they are rounded with */
+    double lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps > 0 */
+} gp_adamw_config;
+
+/*
+ * One AdamW update of n tensors (host array):
+ *   g = factor grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2
+ *   param <- (1 - lr weight_decay) param
+ *            - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, the parameter rounded once (round to nearest even).  t is `step` (>= 1),
+ * or, with step_dev given (device int64; step is then 0), step_dev[0] + 1, and the call
+ * stores it back: what a captured step needs, since a replay repeats `step`.
+ *   factor  : device fp32 [1] that every gradient is multiplied with (gp_grad_norm's
+ *             second value); NULL: 1.  If it is NaN nothing is changed, step_dev included.
+ * States in 8 bits: GP_STATE_BLOCK consecutive elements share the scale
+ * max|x| / 448, and x / scale is rounded to e4m3 up or down at random, so that the
+ * small changes of a moment are kept on average where rounding to nearest would lose
+ * them (with beta2 = 0.999 nearly all).  What is not zero in v does not become zero.  The 16
+ * random bits are a fixed function of seed, t and the element's index i in its
+ * tensor, so a step gives the same bits each time:
+ *   h = floor(i / 4) + 0x3C6EF372 seed + 0x1E3779B1 t;  h ^= h >> 16;  h *= 0x6A3F9B15;
+ *   h ^= h >> 15;  h *= 0x5D47C1E3;  h ^= h >> 16;  h *= K[i mod 4],
+ *   K = 0x4F1BBCDD, 0x7A6D2C8B, 0x35E9A1F7, 0x1D872B41   (mod 2^32);
+ *   m takes the low 16 bits, v the high 16.
+ * A block whose largest value is below 2^-100 is stored as zeros.
+ * Tensors must not overlap.  n = 0 and tensors of count 0 are fine.
+ * GP_ERR_INVALID_ARG: NULL arrays or addresses, a negative count, unknown types or
+ *   state_bits, hyperparameters out of range (weight_decay >= 0 and lr weight_decay <= 1),
+ *   copy with bf16 parameters, scales missing or given with 32-bit states, a misaligned
+ *   address, not exactly one of step and step_dev.
+ * GP_ERR_STATE: `step` given while the stream is being captured.
+ */
+gp_status gp_adamw_step(const gp_adamw_tensor* tensors, int n, const gp_adamw_config* cfg, long long step,
+                        long long* step_dev, const float* factor, gp_stream stream);
+
 /* Message of the calling thread's last failure (library-owned, valid until the
  * thread's next failing call); "" if none. */
 const char* gp_last_error(void);

@@ -39,7 +39,11 @@ EXPORTS = ["gp_partition_create", "gp_partition_configure", "gp_partition_destro
            "gp_get_param", "gp_get_grad", "gp_partition_memory", "gp_param_count", "gp_forward_microbatch",
            "gp_backward_microbatch_remat", "gp_accumulate_and_step", "gp_timer_select", "gp_timer_read",
            "gp_timer_reset", "gp_timer_sample", "gp_mfma_peak", "gp_recomputed_output", "gp_memory_plan",
-           "gp_forward_microbatch_noalloc", "gp_plan_cells", "gp_stream_create", "gp_stream_destroy", "gp_last_error"]
+           "gp_forward_microbatch_noalloc", "gp_plan_cells", "gp_stream_create", "gp_stream_destroy",
+           "gp_token_logprobs", "gp_token_logprobs_workspace", "gp_token_logprobs_backward", "gp_grad_norm",
+           "gp_grad_norm_workspace", "gp_adamw_step", "gp_last_error"]
+
+GP_TOP_MAX, GP_NO_TOKEN, GP_STATE_BLOCK = 32, -1, 256
 
 
 class gp_config(ctypes.Structure):
@@ -49,6 +53,22 @@ class gp_config(ctypes.Structure):
                 ("label_smoothing", ctypes.c_float), ("ln_eps", ctypes.c_float),
                 ("check_finite", ctypes.c_int), ("keep_activations", ctypes.c_int), ("optimizer", ctypes.c_int),
                 ("rms_decay", ctypes.c_float), ("rms_eps", ctypes.c_float), ("logit_clip", ctypes.c_float)]
+
+
+class gp_grad_tensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("count", ctypes.c_longlong)]
+
+
+class gp_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("count", ctypes.c_longlong), ("weight_decay", ctypes.c_double)]
+
+
+class gp_adamw_config(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int), ("grad_dtype", ctypes.c_int), ("state_bits", ctypes.c_int),
+                ("seed", ctypes.c_uint), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double)]
 
 
 class GpError(RuntimeError):
@@ -93,6 +113,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.gp_stream_create.argtypes = [ctypes.POINTER(VP)]
     lib.gp_stream_destroy.argtypes = [VP]
     lib.gp_memory_plan.argtypes = [I, I, I, I, ctypes.POINTER(gp_config)] + [ctypes.POINTER(SZ)] * 4
+    L, F = ctypes.c_long, ctypes.c_float
+    lib.gp_token_logprobs.argtypes = [I, VP, L, I, L, VP, F, F, VP, VP, VP, I, VP, VP, VP, SZ, VP]
+    lib.gp_token_logprobs_workspace.argtypes = [I, L, I, I, ctypes.POINTER(SZ)]
+    lib.gp_token_logprobs_backward.argtypes = [I, VP, L, I, L, VP, F, F, VP, VP, VP, VP, VP, L, VP]
+    lib.gp_grad_norm.argtypes = [I, ctypes.POINTER(gp_grad_tensor), I, F, VP, VP, SZ, VP]
+    lib.gp_grad_norm_workspace.argtypes = [I, ctypes.POINTER(SZ)]
+    lib.gp_adamw_step.argtypes = [ctypes.POINTER(gp_adamw_tensor), I, ctypes.POINTER(gp_adamw_config),
+                                  ctypes.c_longlong, VP, VP, VP]
     lib.gp_last_error.argtypes = []
     lib.gp_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -229,6 +257,41 @@ def gp_stream_destroy(stream):
 def gp_recomputed_output(h, y, stream):
     """y: device address of an [n, S, D] buffer in the partition dtype."""
     _check(load().gp_recomputed_output(h, y, stream))
+
+
+def gp_token_logprobs(dtype, logits, rows, vocab, ld, tokens, scale, clip, logp, lse, entropy, top, top_ids, top_logp,
+                      ws, ws_bytes, stream):
+    _check(load().gp_token_logprobs(dtype, logits, rows, vocab, ld, tokens, scale, clip, logp, lse, entropy, top,
+                                    top_ids, top_logp, ws, ws_bytes, stream))
+
+
+def gp_token_logprobs_workspace(dtype, rows, vocab, top):
+    """Bytes of scratch with which gp_token_logprobs is fastest."""
+    v = ctypes.c_size_t()
+    _check(load().gp_token_logprobs_workspace(dtype, rows, vocab, top, ctypes.byref(v)))
+    return v.value
+
+
+def gp_token_logprobs_backward(dtype, logits, rows, vocab, ld, tokens, scale, clip, lse, entropy, dlogp, dentropy,
+                               dlogits, ldd, stream):
+    _check(load().gp_token_logprobs_backward(dtype, logits, rows, vocab, ld, tokens, scale, clip, lse, entropy, dlogp,
+                                             dentropy, dlogits, ldd, stream))
+
+
+def gp_grad_norm(dtype, grads, n, max_norm, norm_factor, ws, ws_bytes, stream):
+    """grads: an array of gp_grad_tensor."""
+    _check(load().gp_grad_norm(dtype, grads, n, max_norm, norm_factor, ws, ws_bytes, stream))
+
+
+def gp_grad_norm_workspace(n):
+    v = ctypes.c_size_t()
+    _check(load().gp_grad_norm_workspace(n, ctypes.byref(v)))
+    return v.value
+
+
+def gp_adamw_step(tensors, n, cfg: gp_adamw_config, step, step_dev, factor, stream):
+    """tensors: an array of gp_adamw_tensor."""
+    _check(load().gp_adamw_step(tensors, n, ctypes.byref(cfg), step, step_dev, factor, stream))
 
 
 def gp_mfma_peak(stream=None):

@@ -1,0 +1,229 @@
+"""Torch-facing operators on the caller's own tensors (marshalling only).
+
+Beside the partition's own head and update: log probabilities of given tokens
+with entropy and alternatives (``token_logprobs``) and their gradient
+(``token_logprobs_backward``), the norm over many gradients (``grad_norm``) and
+AdamW over many tensors with states in 32 or 8 bits (``AdamW``).  Every step of
+the work runs in libgp.so, on the current stream of the tensors' device;
+results and scratch memory come from torch's allocator.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional, Sequence, Union
+
+import torch
+
+from . import gp
+
+DTYPE = {torch.float32: gp.GP_F32, torch.bfloat16: gp.GP_BF16}
+
+
+class TokenLogprobs(NamedTuple):
+    logp: Optional[torch.Tensor]      # fp32 [rows]; None without tokens
+    lse: torch.Tensor                 # fp32 [rows]
+    entropy: torch.Tensor             # fp32 [rows]
+    top_ids: Optional[torch.Tensor]   # int32 [rows, top]; None for top = 0
+    top_logp: Optional[torch.Tensor]  # fp32 [rows, top]
+
+
+def _device(t):
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a GPU")
+    return torch.cuda.device(t.device)
+
+
+def _stream(t):
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows(name, t):
+    """(rows, vocab, ld) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in DTYPE:
+        raise ValueError(f"{name} must be a matrix in float32 or bfloat16")
+    rows, vocab = t.shape
+    if vocab > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    ld = t.stride(0) if rows > 1 else max(vocab, t.stride(0))
+    if ld < vocab:
+        raise ValueError(f"{name}: rows must not overlap")
+    return rows, vocab, ld
+
+
+def _vector(name, t, rows, dtype, device):
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != (rows,) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} vector of one value per row on {device}")
+
+
+def token_logprobs(logits, tokens=None, scale=1.0, clip=0.0, top=0) -> TokenLogprobs:
+    """gp_token_logprobs of rows of logits [rows, vocab] (a row stride is fine)
+    and int32 tokens [rows] (gp.GP_NO_TOKEN where there is none; None: no
+    logp).  scale: 1 / temperature; clip: the head's logit clip, 0 = off."""
+    rows, vocab, ld = _rows("logits", logits)
+    _vector("tokens", tokens, rows, torch.int32, logits.device)
+    with _device(logits):
+        def new(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=logits.device)
+        dt = DTYPE[logits.dtype]
+        need = gp.gp_token_logprobs_workspace(dt, rows, vocab, top)
+        ws = new(need, dtype=torch.uint8) if need else None
+        r = TokenLogprobs(new(rows) if tokens is not None else None, new(rows), new(rows),
+                          new(rows, top, dtype=torch.int32) if top else None, new(rows, top) if top else None)
+        gp.gp_token_logprobs(dt, logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip, _ptr(r.logp),
+                             r.lse.data_ptr(), r.entropy.data_ptr(), top, _ptr(r.top_ids), _ptr(r.top_logp), _ptr(ws),
+                             need, _stream(logits))
+    return r
+
+
+def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentropy=None, scale=1.0, clip=0.0,
+                            out=None):
+    """gp_token_logprobs_backward: the gradient of sum dlogp logp + dentropy
+    entropy with respect to the logits.  out: where it goes (may be logits
+    itself); allocated otherwise."""
+    rows, vocab, ld = _rows("logits", logits)
+    _vector("tokens", tokens, rows, torch.int32, logits.device)
+    for name, t in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
+        _vector(name, t, rows, torch.float32, logits.device)
+    with _device(logits):
+        if out is None:
+            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device:
+            raise ValueError("out must have the type, shape and device of the logits")
+        ldd = ld if out.data_ptr() == logits.data_ptr() and rows <= 1 else _rows("out", out)[2]
+        gp.gp_token_logprobs_backward(DTYPE[logits.dtype], logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip,
+                                      _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), out.data_ptr(), ldd,
+                                      _stream(logits))
+    return out
+
+
+def _same(name, tensors, like=None):
+    """Tensors of one type on one device, each contiguous (and of the shapes of `like`)."""
+    tensors = list(tensors)
+    for t in tensors:
+        if t.dtype != tensors[0].dtype or t.device != tensors[0].device or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous tensors of one type on one GPU")
+    if like is not None and (len(like) != len(tensors) or any(a.numel() != b.numel() for a, b in zip(like, tensors))):
+        raise ValueError(f"{name} must match the parameters one by one")
+    return tensors
+
+
+class TensorList:
+    """Gradients whose addresses a program passes again and again: checked and
+    listed once.  Holds the tensors."""
+
+    def __init__(self, tensors: Sequence[torch.Tensor]):
+        self.tensors = _same("gradients", tensors)
+        if not self.tensors or self.tensors[0].dtype not in DTYPE:
+            raise ValueError("a TensorList needs float32 or bfloat16 tensors")
+        self.dtype = DTYPE[self.tensors[0].dtype]
+        self.array = (gp.gp_grad_tensor * len(self.tensors))()
+        for a, t in zip(self.array, self.tensors):
+            a.grad, a.count = t.data_ptr(), t.numel()
+
+
+def grad_norm(grads: Union[TensorList, Sequence[torch.Tensor]], max_norm=float("inf")):
+    """fp32 [2] on the device: the 2-norm over all the tensors, and the factor
+    min(1, max_norm / norm) that clips them (NaN where the norm is not finite)."""
+    g = grads if isinstance(grads, TensorList) else TensorList(grads)
+    t = g.tensors[0]
+    with _device(t):
+        out = torch.empty(2, dtype=torch.float32, device=t.device)
+        need = gp.gp_grad_norm_workspace(len(g.tensors))
+        ws = torch.empty(need, dtype=torch.uint8, device=t.device)
+        gp.gp_grad_norm(g.dtype, g.array, len(g.tensors), max_norm, out.data_ptr(), ws.data_ptr(), need, _stream(t))
+    return out
+
+
+class AdamW:
+    """AdamW over a list of parameters, one gp_adamw_step per ``step``.
+
+    params: contiguous fp32 or bf16 tensors.  grads: one per parameter, read at
+    every step (``bind_grads`` names others).  state_bits: 32, or 8 (e4m3 values
+    with an fp32 scale per 256 elements, v held as its square root); the states
+    start at zero, or m, v (and m_scale, v_scale) are taken as they are, of the
+    types that ``m`` and ``v`` of another AdamW have.  copies: bf16 tensors that
+    receive the updated fp32 parameters.  weight_decay: a number or one per
+    parameter.  steps: updates done before.  capturable: the step counter lives
+    on the device (``step_dev``), as a step recorded into a graph needs."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m=None, v=None, m_scale=None,
+                 v_scale=None, copies=None, state_bits: Optional[int] = None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8,
+                 weight_decay: Union[float, Sequence[float]] = 0.0, seed=0, steps=0, capturable=False):
+        self.params = _same("params", params)
+        if not self.params or self.params[0].dtype not in DTYPE:
+            raise ValueError("params must be float32 or bfloat16 tensors")
+        if state_bits is None:
+            state_bits = 8 if m and m[0].dtype == torch.float8_e4m3fn else 32
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 32 or 8")
+        dev, n = self.params[0].device, len(self.params)
+        kind = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        if (m is None) != (v is None):
+            raise ValueError("m and v come together")
+        if m is None:
+            m = [torch.zeros(p.shape, dtype=kind, device=dev) for p in self.params]
+            v = [torch.zeros(p.shape, dtype=kind, device=dev) for p in self.params]
+        self.m, self.v = _same("m", m, self.params), _same("v", v, self.params)
+        if any(t.dtype != kind or t.device != dev for t in self.m + self.v):
+            raise ValueError(f"m and v must be {kind} on {dev}")
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            blocks = [(p.numel() + gp.GP_STATE_BLOCK - 1) // gp.GP_STATE_BLOCK for p in self.params]
+            if m_scale is None and v_scale is None:
+                m_scale, v_scale = ([torch.zeros(b, device=dev) for b in blocks] for _ in range(2))
+            if m_scale is None or v_scale is None:
+                raise ValueError("m_scale and v_scale come together")
+            self.m_scale, self.v_scale = _same("m_scale", m_scale), _same("v_scale", v_scale)
+            for s in (self.m_scale, self.v_scale):
+                if [t.numel() for t in s] != blocks or any(t.dtype != torch.float32 or t.device != dev for t in s):
+                    raise ValueError("m_scale and v_scale must hold one float32 per 256 elements of their parameter")
+        elif m_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to 8-bit states")
+        self.copies = None if copies is None else _same("copies", copies, self.params)
+        if self.copies and any(t.dtype != torch.bfloat16 or t.device != dev for t in self.copies):
+            raise ValueError(f"copies must be bfloat16 on {dev}")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        if len(decay) != n:
+            raise ValueError("weight_decay must be a number or one per parameter")
+        self.array = (gp.gp_adamw_tensor * n)()
+        for i, (a, p) in enumerate(zip(self.array, self.params)):
+            a.param, a.count, a.weight_decay = p.data_ptr(), p.numel(), decay[i]
+            a.m, a.v = self.m[i].data_ptr(), self.v[i].data_ptr()
+            if state_bits == 8:
+                a.m_scale, a.v_scale = self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()
+            if self.copies:
+                a.copy = self.copies[i].data_ptr()
+        self.cfg = gp.gp_adamw_config(DTYPE[self.params[0].dtype], 0, state_bits, seed, lr, betas[0], betas[1], eps)
+        self.steps = steps
+        self.step_dev = torch.full((1,), steps, dtype=torch.int64, device=dev) if capturable else None
+        self.bind_grads(grads)
+
+    def bind_grads(self, grads: Sequence[torch.Tensor]):
+        """The gradients that the next steps read."""
+        grads = _same("grads", grads, self.params)
+        if grads[0].dtype not in DTYPE or grads[0].device != self.params[0].device:
+            raise ValueError("grads must be float32 or bfloat16 on the parameters' device")
+        self.grads = grads
+        self.cfg.grad_dtype = DTYPE[grads[0].dtype]
+        for a, g in zip(self.array, grads):
+            a.grad = g.data_ptr()
+
+    def step(self, lr: Optional[float] = None, factor: Optional[torch.Tensor] = None):
+        """One update.  factor: fp32 on the device, multiplied into every
+        gradient (``grad_norm(...)[1:]``); a NaN leaves everything as it was.
+        The host's count ``steps`` goes up either way."""
+        if lr is not None:
+            self.cfg.lr = lr
+        p = self.params[0]
+        if factor is not None and (factor.dtype != torch.float32 or factor.numel() != 1 or factor.device != p.device):
+            raise ValueError("factor must be one float32 on the parameters' device")
+        with _device(p):
+            gp.gp_adamw_step(self.array, len(self.params), self.cfg, 0 if self.step_dev is not None else self.steps + 1,
+                             _ptr(self.step_dev), _ptr(factor), _stream(p))
+        self.steps += 1

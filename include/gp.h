@@ -409,7 +409,7 @@ gp_status gp_mfma_peak(void* stream, double* tflops);
  * each row's distribution and its most likely tokens.
  *   logits  : device [rows, vocab], rows ld elements apart (ld >= vocab).
  *             x = min(max(z, -clip), clip) with clip > 0, else z; s = scale x
- *             (scale: 1 / temperature, finite and > 0).
+ *             (scale: 1 / temperature, in [1e-6, 1e6]).
  *   tokens  : device int32 [rows] in [0, vocab), or GP_NO_TOKEN, whose logp is
  *             0; any other value gives a NaN.  May be NULL where logp is.
  *   logp    : s_token - lse.  lse: log sum_v exp(s_v).
@@ -423,8 +423,8 @@ gp_status gp_mfma_peak(void* stream, double* tflops);
  *             fewer (0 and NULL included) it gives the same alternatives, and sums
  *             in another order.
  * A logit x of -1e30 or less (-inf, or a type's lowest value, as masks leave it) is a
- * token that cannot occur: p = 0, logp -inf.  A row of nothing else has lse and logp
- * -inf and entropy 0.
+ * token that cannot occur: p = 0, logp -inf, among the alternatives last and in
+ * order of index.  A row of nothing else has lse and logp -inf and entropy 0.
  * A row with NaN or +inf gives NaN; NaN counts as the largest logit.  Sums are
  * fp32, in an order that only the sizes and the alignment decide.
  * GP_ERR_INVALID_ARG: NULL logits, negative sizes, vocab < 1, ld < vocab, scale or

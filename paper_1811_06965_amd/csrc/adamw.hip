@@ -112,7 +112,7 @@ __device__ __forceinline__ unsigned e4m3_code(float y, unsigned rnd16) {
 __device__ __forceinline__ void block_scale(float top, float& scale, float& inv) {
     const bool tiny = top < 0x1p-100f;
     scale = tiny ? 0.f : top * (1.f / 448.f);
-    inv = tiny ? 0.f : 448.f / top;
+    inv = tiny ? 0.f : 1.f / top * 448.f;
 }
 // fmaxf drops a NaN; here it has to reach the scale.
 __device__ __forceinline__ float max_nan(float a, float b) { return b > a || b != b ? b : a; }

@@ -59,7 +59,7 @@ def quantise(x, rnd, keep):
         top = np.abs(b).max()
         tiny = top < F(2.0 ** -100)
         scales.append(F(0) if tiny else top * (F(1) / F(448)))
-        inv = F(0) if tiny else F(448) / top
+        inv = F(0) if tiny else F(1) / top * F(448)
         y = b * inv
         c = ((np.abs(y) * F(2.0 ** -120)).view(np.uint32) + (rnd[a:a + 256] << np.uint32(4)) + np.uint32(8)) >> np.uint32(20)
         c = np.minimum(c, 126)

@@ -427,8 +427,8 @@ gp_status gp_mfma_peak(void* stream, double* tflops);
  * order of index.  A row of nothing else has lse and logp -inf and entropy 0.
  * A row with NaN or +inf gives NaN; NaN counts as the largest logit.  Sums are
  * fp32, in an order that only the sizes and the alignment decide.
- * GP_ERR_INVALID_ARG: NULL logits, negative sizes, vocab < 1, ld < vocab, scale or
- *   clip out of range, top out of range or without both outputs, logp without
+ * GP_ERR_INVALID_ARG: NULL logits, negative sizes, vocab < 1 or > 2^30, ld < vocab,
+ *   scale or clip out of range, top out of range or without both outputs, logp without
  *   tokens, a pointer not aligned to its element, rows > 2^31 - 1.
  */
 gp_status gp_token_logprobs(int dtype, const void* logits, long rows, int vocab, long ld, const int* tokens,

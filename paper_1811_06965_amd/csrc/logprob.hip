@@ -11,7 +11,6 @@ namespace {
 
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float NEVER = -1e30f;  // a logit down here is a mask's, its token cannot occur
-constexpr int ROW_THREADS = 256;
 constexpr int SPLIT_MAX = 64;    // workgroups of one row: the lanes of the wave that joins them
 
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -26,73 +25,76 @@ struct Part {
     float r, a, b;
 };
 constexpr float NO_REF = -2e30f;  // below every reference
-// c2 = scale log2 e
-__device__ __forceinline__ Part join(Part x, Part y, float c2) {
-    const float r = max_nan(x.r, y.r), dx = x.r - r, dy = y.r - r;
-    const float fx = __builtin_amdgcn_exp2f(dx * c2), fy = __builtin_amdgcn_exp2f(dy * c2);
-    return {r, x.a * fx + y.a * fy, fx * (x.b + x.a * dx) + fy * (y.b + y.a * dy)};
+// A reduction over the 64 lanes in the data-parallel unit: pairs, quads, eights and
+// sixteens in place, then the four rows of sixteen into lane 63, whose value is given
+// to all.  In rows that a step leaves out, `none` (neutral to op) stands in.
+template <int CTRL, int ROWS> __device__ __forceinline__ unsigned lanes_from(unsigned none, unsigned x) {
+    return (unsigned)__builtin_amdgcn_update_dpp((int)none, (int)x, CTRL, ROWS, 0xF, false);
 }
+template <typename Op> __device__ __forceinline__ unsigned wave_reduce(unsigned x, unsigned none, Op op) {
+    x = op(x, lanes_from<0xB1, 0xF>(none, x));   // lane ^ 1
+    x = op(x, lanes_from<0x4E, 0xF>(none, x));   // lane ^ 2
+    x = op(x, lanes_from<0x141, 0xF>(none, x));  // mirrored within eight
+    x = op(x, lanes_from<0x140, 0xF>(none, x));  // mirrored within sixteen
+    x = op(x, lanes_from<0x142, 0xA>(none, x));  // lane 15 of the row before, in rows 1 and 3
+    x = op(x, lanes_from<0x143, 0xC>(none, x));  // lane 31, in rows 2 and 3
+    return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+}
+template <typename Op> __device__ __forceinline__ float wave_reduce_f(float x, float none, Op op) {
+    return __uint_as_float(wave_reduce(__float_as_uint(x), __float_as_uint(none), [&](unsigned a, unsigned b) {
+        return __float_as_uint(op(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+__device__ __forceinline__ unsigned wave_max_u(unsigned x) {
+    return wave_reduce(x, 0u, [](unsigned a, unsigned b) { return a > b ? a : b; });
+}
+// The parts of 64 lanes as one.  c2 = scale log2 e.
 __device__ __forceinline__ Part wave_join(Part p, float c2) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        p = join(p, Part{__shfl_xor(p.r, o, WAVE), __shfl_xor(p.a, o, WAVE), __shfl_xor(p.b, o, WAVE)}, c2);
-    return p;
+    const float r = wave_reduce_f(p.r, NO_REF, [](float a, float b) { return max_nan(a, b); });
+    const float d = p.r - r, f = __builtin_amdgcn_exp2f(d * c2);
+    auto add = [](float a, float b) { return a + b; };
+    return {r, wave_reduce_f(p.a * f, 0.f, add), wave_reduce_f(f * (p.b + p.a * d), 0.f, add)};
 }
 
-// The order of alternatives as one integer: larger logits first (a NaN before all,
-// both zeros equal), then the lower index.  No key is 0 or ~0.
+// The order of alternatives as integers: the code of a logit (larger first, a NaN
+// before all, both zeros equal), and in the low half of a key its index, lower first.
+// No code is 0, no key 0 or ~0.
 typedef unsigned long long u64;
-constexpr unsigned NAN_ORDER = 0xFFFFFFFEu;
-__device__ __forceinline__ u64 rank_key(float x, int v) {
-    unsigned u = __float_as_uint(x + 0.f);
-    u = (u >> 31) ? ~u : u | 0x80000000u;
-    if (x != x) u = NAN_ORDER;
-    return ((u64)u << 32) | (0xFFFFFFFFu - (unsigned)v);
+constexpr unsigned NAN_CODE = 0xFFFFFFFEu;
+__device__ __forceinline__ unsigned code_of(float x) {
+    const unsigned u = __float_as_uint(x + 0.f);
+    return x != x ? NAN_CODE : (u >> 31) ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ u64 key_of(unsigned code, int v) { return ((u64)code << 32) | (0xFFFFFFFFu - (unsigned)v); }
 __device__ __forceinline__ float key_value(u64 k) {
     const unsigned u = (unsigned)(k >> 32);
-    if (u == NAN_ORDER) return NAN;
+    if (u == NAN_CODE) return NAN;
     return __uint_as_float((u >> 31) ? u & 0x7FFFFFFFu : ~u);
 }
 __device__ __forceinline__ int key_index(u64 k) { return (int)(0xFFFFFFFFu - (unsigned)k); }
 __device__ __forceinline__ u64 wave_max_key(u64 k) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const u64 x = __shfl_xor(k, o, WAVE);
-        k = x > k ? x : k;
-    }
-    return k;
+    const unsigned hi = wave_max_u((unsigned)(k >> 32));
+    const unsigned lo = wave_max_u((unsigned)(k >> 32) == hi ? (unsigned)k : 0u);
+    return ((u64)hi << 32) | lo;
 }
 
-// A row in chunks of 16 bytes of memory: chunk j holds the elements N j - mis .. + N - 1
-// that lie in [0, V); only the first and the last can be short.
+// A row in chunks of 16 bytes, the last one short where V asks for it.  Global memory
+// takes 16-byte accesses at any element's address.
 template <typename T> struct Chunks {
     static constexpr int N = Vec16<T>::N;
-    typedef typename Vec16<T>::type vec;
-    const T* base;  // of chunk 0, 16-byte aligned
-    int V, mis, count, f0, f1;  // chunks f0 .. f1 - 1 are whole
-    __device__ __forceinline__ Chunks(const T* row, int V_) : V(V_) {
-        mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-        base = row - mis;
-        count = (V + mis + N - 1) / N;
-        f0 = mis ? 1 : 0;
-        f1 = (V + mis) / N;
+    typedef typename Vec16<T>::type vec __attribute__((aligned(sizeof(T))));
+    static __device__ __forceinline__ vec load(const T* row, int j) {
+        return *reinterpret_cast<const vec*>(row + (long)j * N);
     }
-    __device__ __forceinline__ int first(int j) const { return j * N - mis; }
-    __device__ __forceinline__ bool whole(int j) const { return j >= f0 && j < f1; }
-    __device__ __forceinline__ vec load(int j) const { return reinterpret_cast<const vec*>(base)[j]; }
-    // any chunk; `none` in the places outside the row
-    __device__ __forceinline__ void values(int j, float none, float (&x)[N]) const {
-        if (whole(j)) {
-            const vec v = load(j);
+    // the values of any chunk of a row of V; `none` behind its end
+    static __device__ __forceinline__ void values(const T* row, int V, int j, float none, float (&x)[N]) {
+        if (j < V / N) {
+            const vec v = load(row, j);
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = to_f32((T)v[e]);
         } else {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int v = first(j) + e;
-                x[e] = v >= 0 && v < V ? to_f32(base[(long)j * N + e]) : none;
-            }
+            for (int e = 0; e < N; ++e) x[e] = j * N + e < V ? to_f32(row[(long)j * N + e]) : none;
         }
     }
 };
@@ -133,36 +135,157 @@ __device__ __forceinline__ void write_row(const RowOut& o, long row, Part p, con
     }
 }
 
-// A workgroup per row, or `splits` of them, each over `per` chunks of it; thread t
-// takes the chunks t, t + 256, ..  One pass gives the sums and each thread's largest
-// logit.  Alternatives: the k-th largest of the 256 threads' largest is a bound
-// that at least k logits reach, and only the k threads whose largest does hold any
-// such logit; those threads' chunks are read a second time and what reaches the
-// bound (a few more than k) is ranked.  A row with a NaN, or more than CAND
-// such logits, goes through its logits once per alternative instead.
-constexpr int CAND = 1024;
-template <typename T, bool CLIP, bool TOP>
-__global__ void __launch_bounds__(ROW_THREADS) logprob_kernel(const T* __restrict__ z, int V, long ld,
-                                                              const int* __restrict__ tokens, float scale, float clip,
-                                                              RowOut out, int top, int splits, int per,
-                                                              Part* __restrict__ parts, u64* __restrict__ lists) {
-    constexpr int N = Chunks<T>::N, U = 4;
-    __shared__ Part red[4];
-    __shared__ u64 best[TOP ? ROW_THREADS : 1], cand[TOP ? CAND : 1];
-    __shared__ int owner[TOP ? GP_TOP_MAX : 1], found;
+// Alternatives of one workgroup's part of a row.  Its threads make GROUPS groups of
+// neighbours.  A bound that the largest logits of at least `top` groups reach is
+// reached by at least `top` logits, and only by logits of the groups whose largest
+// does: those groups' chunks are read a second time and what reaches the bound, a few
+// more than `top` logits, is ranked.  One wave finds the bound bit by bit from the
+// groups' largest, as coarse as OWNERS groups above it allow.  Where more than
+// OWNERS groups are equal at the bound, the logits above it come from
+// the groups that have any, and those at it from the row's start on, until there are
+// enough.  A row with a NaN, or with more than CAND logits that reach the bound, goes
+// through its logits once per alternative instead.
+constexpr int OWNERS = 48;
+template <int NT> struct TopShared {
+    static constexpr int GROUPS = NT < 256 ? NT : 256, CAND = 4 * GROUPS, TIE_CHUNKS = GROUPS / 2;
+    unsigned most[GROUPS];
+    u64 best[NT / WAVE];
+    u64 cand[CAND + TIE_CHUNKS * 8];  // ties come in where fewer than `top` are listed
+    int owner[GROUPS];
+    int owners, found;
+    unsigned bound;
+};
+template <typename T, int NT, typename Bounded, typename Give>
+__device__ __forceinline__ void find_top(TopShared<NT>& sh, const T* zr, int V, int c0, int c1, int top, bool has_nan,
+                                         Bounded bounded, Give give) {
+    typedef Chunks<T> C;
+    typedef TopShared<NT> S;
+    constexpr int N = C::N, G = NT / S::GROUPS, PER = S::GROUPS / WAVE, ROOM = S::CAND + S::TIE_CHUNKS * 8;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    auto take = [&](int j, auto wanted) {  // lists a chunk's logits whose code is wanted
+        float x[N];
+        C::values(zr, V, j, 0.f, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const unsigned code = code_of(bounded(x[e]));
+            if (j * N + e < V && wanted(code)) {
+                const int at = atomicAdd(&sh.found, 1);
+                if (at < ROOM) sh.cand[at] = key_of(code, j * N + e);
+            }
+        }
+    };
+    bool slow = has_nan;
+    if (!slow) {
+        if (w == 0) {
+            unsigned m[PER], bound = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) m[i] = sh.most[lane + WAVE * i];
+            auto reach = [&](unsigned t) {
+                int c = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) c += __popcll(__ballot(m[i] >= t));
+                return c;
+            };
+            int n = reach(1);
+            if (n < top) {
+                bound = 1;  // fewer groups hold a logit: all that do
+            } else {
+                for (int bit = 31; bit >= 0 && (bound == 0 || n > top + top / 4 + 2); --bit) {
+                    const int c = reach(bound | (1u << bit));
+                    if (c >= top) {
+                        bound |= 1u << bit;
+                        n = c;
+                    }
+                }
+            }
+            const unsigned least = n > OWNERS && n >= top ? bound + 1 : bound;  // ties: the groups above the bound
+            int base = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const u64 mask = __ballot(m[i] >= least);
+                if (m[i] >= least) sh.owner[base + __popcll(mask & ((1ull << lane) - 1))] = lane + WAVE * i;
+                base += __popcll(mask);
+            }
+            if (lane == 0) {
+                sh.owners = base;
+                sh.bound = least;
+                sh.found = 0;
+            }
+        }
+        __syncthreads();
+        const unsigned least = sh.bound;
+        const int rounds = (c1 - c0 + NT - 1) / NT, each = sh.owners * G;
+        for (int i = tid; i < each * rounds; i += NT) {
+            const int o = i % each, j = c0 + sh.owner[o / G] * G + o % G + i / each * NT;
+            if (j < c1) take(j, [&](unsigned code) { return code >= least; });
+        }
+        __syncthreads();
+        int n = sh.found;
+        slow = n > S::CAND;
+        // too few: the rest equal the bound below
+        for (int j0 = c0, step = S::TIE_CHUNKS / 4; !slow && n < top && least > 1 && j0 < c1;
+             j0 += step, step = S::TIE_CHUNKS) {
+            __syncthreads();
+            if (tid < step)
+                for (int i = tid; i < step; i += NT)
+                    if (j0 + i < c1) take(j0 + i, [&](unsigned code) { return code == least - 1; });
+            __syncthreads();
+            n = sh.found;
+        }
+        if (!slow) {
+            for (int i = tid; i < n; i += NT) {
+                const u64 key = sh.cand[i];
+                int r = 0;
+                for (int k = 0; k < n; ++k) r += sh.cand[k] > key ? 1 : 0;
+                if (r < top) give(r, key);
+            }
+            for (int k = n + tid; k < top; k += NT) give(k, 0);  // a part of fewer logits
+        }
+    }
+    if (slow) {
+        u64 last = ~0ull;
+        for (int k = 0; k < top; ++k) {
+            u64 mine = 0;
+            for (int j = c0 + tid; j < c1; j += NT) {
+                float x[N];
+                C::values(zr, V, j, 0.f, x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const u64 key = j * N + e < V ? key_of(code_of(bounded(x[e])), j * N + e) : 0;
+                    if (key < last && key > mine) mine = key;
+                }
+            }
+            mine = wave_max_key(mine);
+            __syncthreads();
+            if (lane == 0) sh.best[w] = mine;
+            __syncthreads();
+            last = wave_max_key(lane < NT / WAVE ? sh.best[lane] : 0);
+            if (tid == 0) give(k, last);
+        }
+    }
+}
+
+// A workgroup of NT threads per row, or `splits` of them, each over `per` chunks of it;
+// thread t takes the chunks t, t + NT, ..
+template <typename T, bool CLIP, bool TOP, int NT>
+__global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, int V, long ld,
+                                                     const int* __restrict__ tokens, float scale, float clip, RowOut out,
+                                                     int top, int splits, int per, Part* __restrict__ parts,
+                                                     u64* __restrict__ lists) {
+    typedef Chunks<T> C;
+    constexpr int N = C::N, U = 4, NW = NT / WAVE;
+    __shared__ Part red[NW];
     const long row = blockIdx.x / splits;
     const int split = (int)(blockIdx.x - row * splits);
     const T* zr = z + row * ld;
-    const Chunks<T> ch(zr, V);
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int c0 = min(split * per, ch.count), c1 = min(c0 + per, ch.count);
+    const int chunks = V / N + (V % N ? 1 : 0), c0 = min(split * per, chunks), c1 = min(c0 + per, chunks);
     const float c2 = scale * LOG2E, near = 8.f / c2, lo = CLIP ? -clip : NEVER, hi = CLIP ? clip : INFINITY;
     auto bounded = [&](float x) { return CLIP ? min_nan(max_nan(x, lo), hi) : max_nan(x, lo); };
 
     Part p = {NO_REF, 0.f, 0.f};
-    float most = -INFINITY;  // this thread's largest logit, and its first chunk that holds it
-    int most_j = -1;
-    auto add = [&](const float (&x)[N], int j) {
+    float most = -INFINITY;  // this thread's largest logit
+    auto add = [&](const float (&x)[N]) {
         float cm = x[0];
 #pragma unroll
         for (int e = 1; e < N; ++e) cm = max_nan(cm, x[e]);
@@ -170,10 +293,7 @@ __global__ void __launch_bounds__(ROW_THREADS) logprob_kernel(const T* __restric
             const float d = p.r - cm, f = __builtin_amdgcn_exp2f(d * c2);
             p = {cm, p.a * f, f * (p.b + p.a * d)};
         }
-        if (TOP && cm > most) {
-            most = cm;
-            most_j = j;
-        }
+        if (TOP) most = max_nan(most, cm);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float d = x[e] - p.r, q = __builtin_amdgcn_exp2f(d * c2);
@@ -181,132 +301,62 @@ __global__ void __launch_bounds__(ROW_THREADS) logprob_kernel(const T* __restric
             p.b = __builtin_fmaf(q, d, p.b);
         }
     };
-    auto add_any = [&](int j) {  // a chunk that may be short: outside the row, nothing
-        float x[N];
-        ch.values(j, -INFINITY, x);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const int v = ch.first(j) + e;
-            x[e] = v >= 0 && v < V ? bounded(x[e]) : NEVER;
-        }
-        add(x, j);
-    };
-    if (c0 < ch.f0 && tid == 0 && c0 < c1) add_any(c0);
-    int j = c0 + tid;
-    if (j < ch.f0) j += ROW_THREADS;
-    const int f1 = min(c1, ch.f1);
-    for (; j < f1; j += U * ROW_THREADS) {
-        typename Chunks<T>::vec v[U];
+    const int f1 = min(c1, V / N);  // whole chunks
+    for (int j = c0 + tid; j < f1; j += U * NT) {
+        typename C::vec v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (j + u * ROW_THREADS < f1) v[u] = ch.load(j + u * ROW_THREADS);
+            if (j + u * NT < f1) v[u] = C::load(zr, j + u * NT);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (j + u * ROW_THREADS >= f1) break;
+            if (j + u * NT >= f1) break;
             float x[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = bounded(to_f32((T)v[u][e]));
-            add(x, j + u * ROW_THREADS);
+            add(x);
         }
     }
-    // the short last chunk, if it is not the first
-    if (c1 == ch.count && c1 - 1 >= c0 && ch.f1 < ch.count && c1 - 1 >= ch.f0 && tid == (c1 - 1 - c0) % ROW_THREADS)
-        add_any(c1 - 1);
+    if (f1 < c1 && tid == (f1 - c0) % NT) {  // the short last chunk: a mask behind its end adds nothing
+        float x[N];
+        C::values(zr, V, f1, 0.f, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = f1 * N + e < V ? bounded(x[e]) : NEVER;
+        add(x);
+    }
 
     p = wave_join(p, c2);
     if (lane == 0) red[w] = p;
-    if (TOP && tid == 0) found = 0;
-    __syncthreads();
-    p = join(join(red[0], red[1], c2), join(red[2], red[3], c2), c2);
-    const RowLog log_p(p, scale);
-    if (splits > 1) {
-        if (tid == 0) parts[blockIdx.x] = p;
-    } else if (tid == 0) {
-        write_row(out, row, p, log_p, zr, V, tokens, lo, hi);
-    }
+    auto sums = [&] { return wave_join(lane < NW ? red[lane] : Part{NO_REF, 0.f, 0.f}, c2); };
+    auto write = [&](const RowLog& log_p) {
+        if (tid != 0) return;
+        if (splits > 1)
+            parts[blockIdx.x] = p;
+        else
+            write_row(out, row, p, log_p, zr, V, tokens, lo, hi);
+    };
     if constexpr (TOP) {
-        auto give = [&](int k, u64 key) {
+        __shared__ TopShared<NT> sh;
+        unsigned m = most == -INFINITY ? 0u : code_of(most);  // 0: no logit
+        constexpr int G = NT / TopShared<NT>::GROUPS;
+#pragma unroll
+        for (int o = 1; o < G; o *= 2) m = max(m, __shfl_xor(m, o, WAVE));
+        if (tid % G == 0) sh.most[tid / G] = m;
+        __syncthreads();
+        p = sums();
+        const RowLog log_p(p, scale);
+        write(log_p);
+        find_top<T, NT>(sh, zr, V, c0, c1, top, p.a != p.a, bounded, [&](int k, u64 key) {
             if (splits > 1) {
                 lists[(long)blockIdx.x * top + k] = key;
             } else {
                 out.top_ids[row * top + k] = key_index(key);
                 out.top_logp[row * top + k] = log_p(key_value(key));
             }
-        };
-        // the key of element e of chunk j; 0 outside the row
-        auto key_of = [&](float x, int j2, int e) -> u64 {
-            const int v = ch.first(j2) + e;
-            return v >= 0 && v < V ? rank_key(bounded(x), v) : 0;
-        };
-        bool slow = p.a != p.a;
-        if (!slow) {
-            u64 mine = 0;
-            if (most_j >= 0) {
-                float x[N];
-                ch.values(most_j, 0.f, x);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const u64 key = key_of(x[e], most_j, e);
-                    mine = key > mine ? key : mine;
-                }
-            }
-            best[tid] = mine;
-            __syncthreads();
-            int rank = 0;
-            for (int i = 0; i < ROW_THREADS; ++i) rank += best[i] > mine ? 1 : 0;
-            // fewer than `top` threads hold a logit: then all that do
-            if (rank < top && mine) owner[rank] = tid;
-            const int owners = min(top, (int)__syncthreads_count(mine != 0));
-            const u64 bound = owners == top ? best[owner[top - 1]] : 1;
-            const int rounds = (c1 - c0 + ROW_THREADS - 1) / ROW_THREADS;
-            for (int i = tid; i < owners * rounds; i += ROW_THREADS) {
-                const int j2 = c0 + owner[i % owners] + i / owners * ROW_THREADS;
-                if (j2 >= c1) continue;
-                float x[N];
-                ch.values(j2, 0.f, x);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const u64 key = key_of(x[e], j2, e);
-                    if (key >= bound) {
-                        const int at = atomicAdd(&found, 1);
-                        if (at < CAND) cand[at] = key;
-                    }
-                }
-            }
-            __syncthreads();
-            const int n = found;
-            slow = n > CAND;
-            if (!slow) {
-                for (int i = tid; i < n; i += ROW_THREADS) {
-                    const u64 key = cand[i];
-                    int r = 0;
-                    for (int k = 0; k < n; ++k) r += cand[k] > key ? 1 : 0;
-                    if (r < top) give(r, key);
-                }
-                for (int k = n + tid; k < top; k += ROW_THREADS) give(k, 0);  // a split of fewer logits
-            }
-        }
-        if (slow) {
-            u64 last = ~0ull;
-            for (int k = 0; k < top; ++k) {
-                u64 mine = 0;
-                for (int j2 = c0 + tid; j2 < c1; j2 += ROW_THREADS) {
-                    float x[N];
-                    ch.values(j2, 0.f, x);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const u64 key = key_of(x[e], j2, e);
-                        if (key < last && key > mine) mine = key;
-                    }
-                }
-                mine = wave_max_key(mine);
-                __syncthreads();
-                if (lane == 0) best[w] = mine;
-                __syncthreads();
-                last = std::max(std::max(best[0], best[1]), std::max(best[2], best[3]));
-                if (tid == 0) give(k, last);
-            }
-        }
+        });
+    } else {
+        __syncthreads();
+        p = sums();
+        write(RowLog(p, scale));
     }
 }
 
@@ -317,23 +367,25 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(const T* __restrict__ 
                                                           const int* __restrict__ tokens, float scale, float lo, float hi,
                                                           RowOut out, int top, int splits,
                                                           const Part* __restrict__ parts, const u64* __restrict__ lists) {
+    __shared__ u64 list[SPLIT_MAX * GP_TOP_MAX];
     const long row = blockIdx.x;
     const int s = threadIdx.x;
+    for (int i = s; i < splits * top; i += WAVE) list[i] = lists[row * splits * top + i];
     Part p = {NO_REF, 0.f, 0.f};
     if (s < splits) p = parts[row * splits + s];
     p = wave_join(p, scale * LOG2E);
     const RowLog log_p(p, scale);
     if (s == 0) write_row(out, row, p, log_p, z + row * ld, V, tokens, lo, hi);
-    const u64* list = lists + (row * splits + s) * top;
+    __syncthreads();
     int at = 0;
-    u64 head = s < splits && top > 0 ? list[0] : 0;
+    u64 head = s < splits && top > 0 ? list[s * top] : 0;
     for (int k = 0; k < top; ++k) {
         const u64 key = wave_max_key(head);
         if (s == 0) {
             out.top_ids[row * top + k] = key_index(key);
             out.top_logp[row * top + k] = log_p(key_value(key));
         }
-        if (head == key && s < splits) head = ++at < top ? list[at] : 0;
+        if (head == key && s < splits) head = ++at < top ? list[s * top + at] : 0;
     }
 }
 
@@ -347,13 +399,14 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(const T* z, int V, lo
                                                            const float* __restrict__ dlogp,
                                                            const float* __restrict__ dentropy, T* dz, long ldd,
                                                            int splits, int per) {
-    constexpr int N = Chunks<T>::N, U = 4;
-    typedef typename Chunks<T>::vec vec;
+    typedef Chunks<T> C;
+    constexpr int N = C::N, U = 4;
+    typedef typename C::vec vec;
     const long row = blockIdx.x / splits;
     const int split = (int)(blockIdx.x - row * splits);
-    const Chunks<T> ch(z + row * ld, V);
-    const Chunks<T> to(dz + row * ldd, V);
-    const int c0 = min(split * per, ch.count), c1 = min(c0 + per, ch.count);
+    const T* zr = z + row * ld;
+    T* dr = dz + row * ldd;
+    const int chunks = V / N + (V % N ? 1 : 0), c0 = min(split * per, chunks), c1 = min(c0 + per, chunks);
     const float l = lse[row];
     float a = dlogp ? dlogp[row] : 0.f;
     const float b = dentropy ? dentropy[row] : 0.f, h = dentropy ? entropy[row] : 0.f;
@@ -374,7 +427,7 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(const T* z, int V, lo
             const float d = max_nan(__builtin_fmaf(s, scale, -l), -200.f);
             g[e] = -__builtin_amdgcn_exp2f(d * LOG2E) * __builtin_fmaf(B, d, A);
         }
-        const int k = t - ch.first(j);
+        const int k = t - j * N;
         if (t >= 0 && k >= 0 && k < N) {
 #pragma unroll
             for (int e = 0; e < N; ++e) g[e] += e == k ? at : 0.f;
@@ -385,49 +438,61 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(const T* z, int V, lo
             if (flat) g[e] = fill;
         }
     };
-    const bool same = ch.mis == to.mis;  // both rows lie alike on the 16-byte grid
-    auto store = [&](int j, const float (&g)[N]) {
-        if (same && ch.whole(j)) {
-            vec o;
-#pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = to_elt<T>(g[e]);
-            reinterpret_cast<vec*>(dz + row * ldd - to.mis)[j] = o;
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int v = ch.first(j) + e;
-                if (v >= 0 && v < V) dz[row * ldd + v] = to_elt<T>(g[e]);
-            }
-        }
-    };
-    for (int j = c0 + (int)threadIdx.x; j < c1; j += U * 256) {
+    const int f1 = min(c1, V / N);  // whole chunks
+    for (int j = c0 + (int)threadIdx.x; j < f1; j += U * 256) {
         vec v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (j + u * 256 < c1 && ch.whole(j + u * 256)) v[u] = ch.load(j + u * 256);
+            if (j + u * 256 < f1) v[u] = C::load(zr, j + u * 256);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int k = j + u * 256;
-            if (k >= c1) break;
+            if (j + u * 256 >= f1) break;
             float x[N], g[N];
-            if (ch.whole(k)) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) x[e] = to_f32((T)v[u][e]);
-            } else {
-                ch.values(k, 0.f, x);
-            }
-            grads(x, k, g);
-            store(k, g);
+            for (int e = 0; e < N; ++e) x[e] = to_f32((T)v[u][e]);
+            grads(x, j + u * 256, g);
+            vec o;
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = to_elt<T>(g[e]);
+            *reinterpret_cast<vec*>(dr + (long)(j + u * 256) * N) = o;
         }
+    }
+    if (f1 < c1 && (int)threadIdx.x == (f1 - c0) % 256) {  // the short last chunk
+        float x[N], g[N];
+        C::values(zr, V, f1, 0.f, x);
+        grads(x, f1, g);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (f1 * N + e < V) dr[(long)f1 * N + e] = to_elt<T>(g[e]);
     }
 }
 
-// Workgroups of a row: as many as give 1024 in all (four per CU) while each thread
-// still has two chunks or more.
+int chunk_count(int dtype, int vocab) {
+    const int n = dtype == GP_BF16 ? 8 : 4;
+    return vocab / n + (vocab % n ? 1 : 0);
+}
+// Workgroups of a row, joined by a second launch: several for up to 32 rows of 128 KB or
+// more, each over 16 KB or more of it, while one workgroup's loads, at 60 GB/s, take
+// longer than the joining.  us, split / whole: one row of 131072 bf16 with 5
+// alternatives 9.4 / 14.8, 32 such rows 10.9 / 15.3, one of 262144 fp32 9.3 / 25.2; but
+// one of 32000 bf16 8.4 / 7.4 and 64 of 131072 17.3 / 16.4.
 int row_splits(int dtype, long rows, int vocab) {
-    const long chunks = vocab / (dtype == GP_BF16 ? 8 : 4);
-    const long s = std::min(rows > 0 ? 1024 / rows : 1, chunks / (2 * ROW_THREADS));
-    return (int)std::max(1L, std::min<long>(s, SPLIT_MAX));
+    const long chunks = chunk_count(dtype, vocab);
+    if (rows < 1 || rows > 32 || chunks < 8192) return 1;
+    return (int)std::min<long>(SPLIT_MAX, std::min(1024 / rows, chunks / 1024));
+}
+// Threads of a workgroup.  Short rows take one wave, whose joins and rankings wait for
+// nobody; few rows, or rows over 128 KB, the most loads in flight; in between many rows
+// share a CU, and alternatives are ranked faster by more threads.  us at 64 / 256 / 512 / 1024
+// threads: 4096 x 1000 bf16 with 5 alternatives 8.6 / 15.1 / 24.7 / 42.6; 3000 x 4111
+// with 1 12.4 / 15.3 / 23.3 / 36.3; 512 x 9000 fp32 with 20 18.0 / 7.8 / 8.1 / 9.3; 93 x
+// 50021 fp32 with 20 69 / 15.7 / 11.7 / 10.6; 1024 x 32000 bf16 20.2 / 14.4 / 14.5 / 15.7,
+// with 20 46 / 20.0 / 19.1 / 23.0; 4096 x 128000 with 8 319 / 216 / 191 / 193.
+int row_threads(long rows, int chunks, int splits, int top) {
+    if (chunks <= 256 || (chunks <= 1024 && rows >= 1024)) return 64;
+    if (splits > 1 || chunks <= 3072) return 256;
+    if (rows < 768 || chunks > 8192) return 1024;
+    return top ? 512 : 256;
 }
 size_t split_bytes(long rows, int splits, int top) { return (size_t)rows * splits * (sizeof(Part) + 8 * (size_t)top); }
 
@@ -437,7 +502,8 @@ gp_status check_rows(int dtype, const void* logits, long rows, int vocab, long l
     auto bad = [](const char* m) { return set_error(GP_ERR_INVALID_ARG, m); };
     if (dtype != GP_F32 && dtype != GP_BF16) return bad("token_logprobs: unknown dtype");
     if (rows < 0 || rows > 0x7FFFFFFFL) return bad("token_logprobs: rows must be in [0, 2^31 - 1]");
-    if (vocab < 1 || ld < vocab) return bad("token_logprobs: vocab must be >= 1 and ld >= vocab");
+    if (vocab < 1 || vocab > (1 << 30) || ld < vocab)
+        return bad("token_logprobs: vocab must be in [1, 2^30] and ld >= vocab");
     if (!(scale >= 1e-6f && scale <= 1e6f)) return bad("token_logprobs: scale must be in [1e-6, 1e6]");
     if (!(clip >= 0.f) || !std::isfinite(clip)) return bad("token_logprobs: clip must be >= 0 and finite");
     if (!logits && rows > 0) return bad("token_logprobs: logits must not be NULL");
@@ -448,26 +514,42 @@ gp_status check_rows(int dtype, const void* logits, long rows, int vocab, long l
 template <typename T>
 gp_status launch_rows(const T* z, long rows, int V, long ld, const int* tokens, float scale, float clip,
                       const RowOut& out, int top, void* ws, size_t ws_bytes, hipStream_t st) {
-    const int dtype = sizeof(T) == 2 ? GP_BF16 : GP_F32, N = 16 / sizeof(T);
+    const int dtype = sizeof(T) == 2 ? GP_BF16 : GP_F32;
     int splits = row_splits(dtype, rows, V);
     if (splits > 1) {
         const size_t fit = ws ? ws_bytes / split_bytes(rows, 1, top) : 0;
         splits = (int)std::min<size_t>(splits, std::max<size_t>(fit, 1));
     }
-    const int chunks = (V + 2 * (N - 1)) / N;  // of the worst alignment
-    const int per = (chunks + splits - 1) / splits;
+    const int chunks = chunk_count(dtype, V), per = (chunks + splits - 1) / splits;
     u64* lists = static_cast<u64*>(ws);
     Part* parts = reinterpret_cast<Part*>(lists + (splits > 1 ? (size_t)rows * splits * top : 0));
     const unsigned grid = (unsigned)(rows * splits);
     const bool clipped = clip > 0.f;
-#define GP_ROWS(CLIP, TOP) \
-    klaunch(logprob_kernel<T, CLIP, TOP>, grid, ROW_THREADS, 0, st, z, V, ld, tokens, scale, clip, out, top, splits, per, \
-            parts, lists)
-    if (clipped && top) GP_ROWS(true, true);
-    else if (clipped) GP_ROWS(true, false);
-    else if (top) GP_ROWS(false, true);
-    else GP_ROWS(false, false);
+    const int nt = row_threads(rows, chunks, splits, top);
+#define GP_ROWS_NT(CLIP, TOP, NT) \
+    klaunch(logprob_kernel<T, CLIP, TOP, NT>, grid, NT, 0, st, z, V, ld, tokens, scale, clip, out, top, splits, per, parts, \
+            lists)
+#define GP_ROWS(CLIP, TOP)                      \
+    do {                                        \
+        if (nt == 64)                           \
+            GP_ROWS_NT(CLIP, TOP, 64);          \
+        else if (nt == 256)                     \
+            GP_ROWS_NT(CLIP, TOP, 256);         \
+        else if (nt == 512 && TOP)              \
+            GP_ROWS_NT(CLIP, TOP, (TOP ? 512 : 64)); \
+        else                                    \
+            GP_ROWS_NT(CLIP, TOP, 1024);        \
+    } while (0)
+    if (clipped && top)
+        GP_ROWS(true, true);
+    else if (clipped)
+        GP_ROWS(true, false);
+    else if (top)
+        GP_ROWS(false, true);
+    else
+        GP_ROWS(false, false);
 #undef GP_ROWS
+#undef GP_ROWS_NT
     if (splits > 1)
         klaunch(logprob_join_kernel<T>, (unsigned)rows, 64, 0, st, z, V, ld, tokens, scale, clipped ? -clip : NEVER,
                 clipped ? clip : INFINITY, out, top, splits, parts, lists);
@@ -478,7 +560,7 @@ gp_status launch_rows(const T* z, long rows, int V, long ld, const int* tokens, 
 template <typename T>
 gp_status launch_grad(const T* z, long rows, int V, long ld, const int* tokens, float scale, float clip, const float* lse,
                       const float* entropy, const float* dlogp, const float* dentropy, T* dz, long ldd, hipStream_t st) {
-    const int N = 16 / sizeof(T), chunks = (V + 2 * (N - 1)) / N;
+    const int chunks = chunk_count(sizeof(T) == 2 ? GP_BF16 : GP_F32, V);
     // 4096 workgroups in all where the rows have that much to split
     const long want = std::max(1L, std::min<long>((4096 + rows - 1) / rows, chunks / 512));
     const int splits = (int)want, per = (chunks + splits - 1) / splits;
@@ -502,7 +584,7 @@ using namespace gp;
 extern "C" {
 
 gp_status gp_token_logprobs_workspace(int dtype, long rows, int vocab, int top, size_t* bytes) {
-    if (!bytes || (dtype != GP_F32 && dtype != GP_BF16) || rows < 0 || vocab < 1 || top < 0 || top > GP_TOP_MAX)
+    if (!bytes || (dtype != GP_F32 && dtype != GP_BF16) || rows < 0 || vocab < 1 || vocab > (1 << 30) || top < 0 || top > GP_TOP_MAX)
         return set_error(GP_ERR_INVALID_ARG, "token_logprobs_workspace: an argument is out of range");
     const int splits = row_splits(dtype, rows, vocab);
     *bytes = splits > 1 ? split_bytes(rows, splits, top) : 0;

@@ -27,14 +27,20 @@ class TokenLogprobs(NamedTuple):
     top_logp: Optional[torch.Tensor]  # fp32 [rows, top]
 
 
-def _device(t):
+def _on(device, call):
+    """call(stream) with the device current and its current stream's handle."""
+    i = device.index
+    if i == torch.cuda.current_device():
+        call(torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(i):
+            call(torch._C._cuda_getCurrentRawStream(i))
+
+
+def _gpu(t):
     if not t.is_cuda:
         raise ValueError("tensors must be on a GPU")
-    return torch.cuda.device(t.device)
-
-
-def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return t.device
 
 
 def _ptr(t):
@@ -55,9 +61,8 @@ def _rows(name, t):
 
 
 def _vector(name, t, rows, dtype, device):
-    if t is None:
-        return
-    if t.dtype != dtype or tuple(t.shape) != (rows,) or t.device != device or not t.is_contiguous():
+    if t is not None and (t.dtype != dtype or t.dim() != 1 or t.numel() != rows or t.device != device
+                          or not t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous {dtype} vector of one value per row on {device}")
 
 
@@ -66,19 +71,19 @@ def token_logprobs(logits, tokens=None, scale=1.0, clip=0.0, top=0) -> TokenLogp
     and int32 tokens [rows] (gp.GP_NO_TOKEN where there is none; None: no
     logp).  scale: 1 / temperature; clip: the head's logit clip, 0 = off."""
     rows, vocab, ld = _rows("logits", logits)
-    _vector("tokens", tokens, rows, torch.int32, logits.device)
-    with _device(logits):
-        def new(*shape, dtype=torch.float32):
-            return torch.empty(shape, dtype=dtype, device=logits.device)
-        dt = DTYPE[logits.dtype]
-        need = gp.gp_token_logprobs_workspace(dt, rows, vocab, top)
-        ws = new(need, dtype=torch.uint8) if need else None
-        r = TokenLogprobs(new(rows) if tokens is not None else None, new(rows), new(rows),
-                          new(rows, top, dtype=torch.int32) if top else None, new(rows, top) if top else None)
-        gp.gp_token_logprobs(dt, logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip, _ptr(r.logp),
-                             r.lse.data_ptr(), r.entropy.data_ptr(), top, _ptr(r.top_ids), _ptr(r.top_logp), _ptr(ws),
-                             need, _stream(logits))
-    return r
+    dev, dt = _gpu(logits), DTYPE[logits.dtype]
+    _vector("tokens", tokens, rows, torch.int32, dev)
+    need = gp.gp_token_logprobs_workspace(dt, rows, vocab, top)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    logp, lse, entropy = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind(0)
+    if tokens is None:
+        logp = None
+    top_ids = torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None
+    top_logp = torch.empty((rows, top), dtype=torch.float32, device=dev) if top else None
+    _on(dev, lambda stream: gp.gp_token_logprobs(
+        dt, logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip, _ptr(logp), lse.data_ptr(),
+        entropy.data_ptr(), top, _ptr(top_ids), _ptr(top_logp), _ptr(ws), need, stream))
+    return TokenLogprobs(logp, lse, entropy, top_ids, top_logp)
 
 
 def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentropy=None, scale=1.0, clip=0.0,
@@ -87,18 +92,21 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentr
     entropy with respect to the logits.  out: where it goes (may be logits
     itself); allocated otherwise."""
     rows, vocab, ld = _rows("logits", logits)
-    _vector("tokens", tokens, rows, torch.int32, logits.device)
+    dev = _gpu(logits)
+    _vector("tokens", tokens, rows, torch.int32, dev)
     for name, t in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
-        _vector(name, t, rows, torch.float32, logits.device)
-    with _device(logits):
-        if out is None:
-            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-        if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device:
-            raise ValueError("out must have the type, shape and device of the logits")
-        ldd = ld if out.data_ptr() == logits.data_ptr() and rows <= 1 else _rows("out", out)[2]
-        gp.gp_token_logprobs_backward(DTYPE[logits.dtype], logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip,
-                                      _ptr(lse), _ptr(entropy), _ptr(dlogp), _ptr(dentropy), out.data_ptr(), ldd,
-                                      _stream(logits))
+        _vector(name, t, rows, torch.float32, dev)
+    if out is None:
+        out, ldd = torch.empty((rows, vocab), dtype=logits.dtype, device=dev), vocab
+    elif out is logits:
+        ldd = ld
+    elif out.dtype != logits.dtype or out.shape != logits.shape or out.device != dev:
+        raise ValueError("out must have the type, shape and device of the logits")
+    else:
+        ldd = _rows("out", out)[2]
+    _on(dev, lambda stream: gp.gp_token_logprobs_backward(
+        DTYPE[logits.dtype], logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip, _ptr(lse), _ptr(entropy),
+        _ptr(dlogp), _ptr(dentropy), out.data_ptr(), ldd, stream))
     return out
 
 
@@ -131,12 +139,11 @@ def grad_norm(grads: Union[TensorList, Sequence[torch.Tensor]], max_norm=float("
     """fp32 [2] on the device: the 2-norm over all the tensors, and the factor
     min(1, max_norm / norm) that clips them (NaN where the norm is not finite)."""
     g = grads if isinstance(grads, TensorList) else TensorList(grads)
-    t = g.tensors[0]
-    with _device(t):
-        out = torch.empty(2, dtype=torch.float32, device=t.device)
-        need = gp.gp_grad_norm_workspace(len(g.tensors))
-        ws = torch.empty(need, dtype=torch.uint8, device=t.device)
-        gp.gp_grad_norm(g.dtype, g.array, len(g.tensors), max_norm, out.data_ptr(), ws.data_ptr(), need, _stream(t))
+    dev, need = g.tensors[0].device, gp.gp_grad_norm_workspace(len(g.tensors))
+    out = torch.empty(2, dtype=torch.float32, device=dev)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _on(dev, lambda stream: gp.gp_grad_norm(g.dtype, g.array, len(g.tensors), max_norm, out.data_ptr(), ws.data_ptr(),
+                                            need, stream))
     return out
 
 
@@ -220,10 +227,10 @@ class AdamW:
         The host's count ``steps`` goes up either way."""
         if lr is not None:
             self.cfg.lr = lr
-        p = self.params[0]
-        if factor is not None and (factor.dtype != torch.float32 or factor.numel() != 1 or factor.device != p.device):
+        dev = self.params[0].device
+        if factor is not None and (factor.dtype != torch.float32 or factor.numel() != 1 or factor.device != dev):
             raise ValueError("factor must be one float32 on the parameters' device")
-        with _device(p):
-            gp.gp_adamw_step(self.array, len(self.params), self.cfg, 0 if self.step_dev is not None else self.steps + 1,
-                             _ptr(self.step_dev), _ptr(factor), _stream(p))
+        host = 0 if self.step_dev is not None else self.steps + 1
+        _on(dev, lambda stream: gp.gp_adamw_step(self.array, len(self.params), self.cfg, host, _ptr(self.step_dev),
+                                                 _ptr(factor), stream))
         self.steps += 1

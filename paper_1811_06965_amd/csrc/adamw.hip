@@ -3,9 +3,12 @@
 //
 // The tensors of a call travel in the kernel arguments, BATCH of them per
 // launch: no table in device memory, nothing to copy or to keep alive, and a
-// captured launch holds its own.  A workgroup takes one chunk of one tensor
-// (the last tensor whose first chunk is not after the workgroup's index).
+// captured launch holds its own.  A workgroup takes one chunk of one tensor: the
+// lanes of a wave compare its index with the tensors' first chunks, one each, so
+// that it is at its data after two reads of the arguments (a binary search, six reads
+// one after the other, took 10 of the 13 us of an update of 32 small tensors).
 #include <cmath>
+#include <type_traits>
 
 #include "common.hpp"
 
@@ -26,12 +29,11 @@ struct AdamwTensor {
     bf16* c;
     long n;
     float keep;  // 1 - lr weight_decay
-    int chunk0;  // chunks of the launch's tensors before this one
-    int vec;     // every address allows 4-element accesses
 };
 struct AdamwBatch {
-    AdamwTensor t[BATCH];
     int n;
+    int chunk0[BATCH];  // chunks of the launch's tensors before each
+    AdamwTensor t[BATCH];
 };
 struct AdamwScalars {
     float lr, b1, c1, b2, c2, eps;  // c = 1 - b
@@ -43,63 +45,50 @@ struct AdamwScalars {
 };
 constexpr unsigned KEY_SEED = 0x3C6EF372u, KEY_STEP = 0x1E3779B1u;
 
-template <typename Batch> __device__ __forceinline__ int tensor_of(const Batch& b, int id) {
-    int l = 0;
-    for (int hi = b.n; l + 1 < hi;) {
-        const int mid = (l + hi) / 2;
-        if (b.t[mid].chunk0 <= id)
-            l = mid;
-        else
-            hi = mid;
+// The last of n tensors whose first chunk is not after id.
+template <int MOST> __device__ __forceinline__ int tensor_of(const int (&chunk0)[MOST], int n, int id) {
+    int l = -1;
+#pragma unroll
+    for (int i = 0; i < MOST; i += WAVE) {
+        const int k = i + (threadIdx.x & 63);
+        l += __popcll(__ballot(k < n && chunk0[k < MOST ? k : 0] <= id));
     }
-    return l;
+    return __builtin_amdgcn_readfirstlane(l);
 }
 
-template <typename T> __device__ __forceinline__ f32x4 load4(const T* p, long i, long n, int vec) {
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    f32x4 r = {0.f, 0.f, 0.f, 0.f};
-    if (vec && i + 4 <= n) {
-        const T4 x = *reinterpret_cast<const T4*>(p + i);
+// Four elements at any element's address, whole or as many as lie before n.
+template <typename T> struct Four {
+    typedef T vec __attribute__((ext_vector_type(4)));
+    typedef vec at_any __attribute__((aligned(sizeof(T))));
+    static __device__ __forceinline__ vec load(const void* p, long i, long n, bool whole) {
+        const T* t = static_cast<const T*>(p) + i;
+        if (whole) return *reinterpret_cast<const at_any*>(t);
+        vec r;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = to_f32(x[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (i + e < n) r[e] = to_f32(p[i + e]);
+        for (int e = 0; e < 4; ++e) r[e] = i + e < n ? t[e] : (T)0;
+        return r;
     }
-    return r;
-}
-template <typename T> __device__ __forceinline__ void store4(T* p, long i, long n, int vec, f32x4 x) {
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    if (vec && i + 4 <= n) {
-        *reinterpret_cast<T4*>(p + i) = T4{to_elt<T>(x[0]), to_elt<T>(x[1]), to_elt<T>(x[2]), to_elt<T>(x[3])};
-    } else {
+    static __device__ __forceinline__ void store(void* p, long i, long n, bool whole, vec x) {
+        T* t = static_cast<T*>(p) + i;
+        if (whole) {
+            *reinterpret_cast<at_any*>(t) = x;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (i + e < n) p[i + e] = to_elt<T>(x[e]);
+            for (int e = 0; e < 4; ++e)
+                if (i + e < n) t[e] = x[e];
+        }
     }
-}
-__device__ __forceinline__ unsigned load_codes(const unsigned char* p, long i, long n, int vec) {
-    if (vec && i + 4 <= n) return *reinterpret_cast<const unsigned*>(p + i);
-    unsigned r = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (i + e < n) r |= (unsigned)p[i + e] << (8 * e);
-    return r;
-}
-__device__ __forceinline__ void store_codes(unsigned char* p, long i, long n, int vec, unsigned q) {
-    if (vec && i + 4 <= n) {
-        *reinterpret_cast<unsigned*>(p + i) = q;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (i + e < n) p[i + e] = (unsigned char)(q >> (8 * e));
+    static __device__ __forceinline__ f32x4 values(vec x) { return f32x4{to_f32(x[0]), to_f32(x[1]), to_f32(x[2]), to_f32(x[3])}; }
+    static __device__ __forceinline__ vec rounded(f32x4 x) {
+        return vec{to_elt<T>(x[0]), to_elt<T>(x[1]), to_elt<T>(x[2]), to_elt<T>(x[3])};
     }
-}
-// The four values of packed e4m3 codes.
-__device__ __forceinline__ f32x4 e4m3_values(unsigned q) {
-    return f32x4{__builtin_amdgcn_cvt_f32_fp8((int)q, 0), __builtin_amdgcn_cvt_f32_fp8((int)q, 1),
-                 __builtin_amdgcn_cvt_f32_fp8((int)q, 2), __builtin_amdgcn_cvt_f32_fp8((int)q, 3)};
+};
+typedef Four<unsigned char> Codes;
+// The values of four e4m3 codes.
+__device__ __forceinline__ f32x4 e4m3_values(Codes::vec c) {
+    const int q = (int)__builtin_bit_cast(unsigned, c);
+    return f32x4{__builtin_amdgcn_cvt_f32_fp8(q, 0), __builtin_amdgcn_cvt_f32_fp8(q, 1),
+                 __builtin_amdgcn_cvt_f32_fp8(q, 2), __builtin_amdgcn_cvt_f32_fp8(q, 3)};
 }
 // |y| <= 448 to e4m3, rounded up where the 16 random bits exceed what rounding down
 // leaves of a step: 2^-120 brings the e4m3 exponents (and zero and the subnormals) to
@@ -114,97 +103,121 @@ __device__ __forceinline__ void block_scale(float top, float& scale, float& inv)
     scale = tiny ? 0.f : top * (1.f / 448.f);
     inv = tiny ? 0.f : 1.f / top * 448.f;
 }
-// fmaxf drops a NaN; here it has to reach the scale.
-__device__ __forceinline__ float max_nan(float a, float b) { return b > a || b != b ? b : a; }
 __device__ __forceinline__ float wave_max_nan(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max_nan(v, __shfl_xor(v, o, WAVE));
-    return v;
+    return wave_reduce_f(v, 0.f, [](float a, float b) { return max_nan(a, b); });
 }
 
-// Four consecutive elements per lane, so that a wave's 256 are one block of the
-// 8-bit states.  Every product and sum is rounded by itself, in the order of the
-// formulas, so that an update is the same bits wherever it is compiled.
-template <typename P, typename G, int BITS>
-__global__ void __launch_bounds__(256) adamw_kernel(const AdamwBatch b, const AdamwScalars s) {
-#pragma clang fp contract(off)
-    const float factor = s.factor ? s.factor[0] : 1.f;
-    if (factor != factor) return;
-    float step_size = s.step_size, inv_root = s.inv_root;
-    unsigned key = s.key;
-    if (s.step_dev) {
-        const long long t = s.step_dev[0];
-        step_size = s.lr / -expm1f((float)t * s.ln_b1);
-        inv_root = 1.f / sqrtf(-expm1f((float)t * s.ln_b2));
-        key += KEY_STEP * (unsigned)t;
-    }
-    const AdamwTensor& T = b.t[tensor_of(b, blockIdx.x)];
-    const long n = T.n, base = (long)((int)blockIdx.x - T.chunk0) * CHUNK;
-    P* p = static_cast<P*>(T.p);
-    const G* g = static_cast<const G*>(T.g);
-    const int lane = threadIdx.x & 63;
-    const unsigned K[4] = {0x4F1BBCDDu, 0x7A6D2C8Bu, 0x35E9A1F7u, 0x1D872B41u};
-#pragma unroll
-    for (int it = 0; it < CHUNK / 1024; ++it) {
-        const long i = base + it * 1024 + (long)threadIdx.x * 4;
-        const long block = i / GP_STATE_BLOCK;
-        if (i - 4 * lane >= n) return;  // the wave's block is behind the end
-        f32x4 pv = load4(p, i, n, T.vec), gv = load4(g, i, n, T.vec), mv, vv;
-        if constexpr (BITS == 32) {
-            mv = load4(static_cast<const float*>(T.m), i, n, T.vec);
-            vv = load4(static_cast<const float*>(T.v), i, n, T.vec);
-        } else {
-            mv = e4m3_values(load_codes(static_cast<const unsigned char*>(T.m), i, n, T.vec)) * T.ms[block];
-            vv = e4m3_values(load_codes(static_cast<const unsigned char*>(T.v), i, n, T.vec)) * T.vs[block];
-            vv = vv * vv;
+// What four lanes' worth of memory holds before the update.
+template <typename P, typename G, int BITS> struct Quad {
+    typename Four<P>::vec p;
+    typename Four<G>::vec g;
+    typename std::conditional<BITS == 32, f32x4, Codes::vec>::type m, v;
+    float sm, sv;
+    __device__ __forceinline__ void load(const AdamwTensor& T, long i, bool whole) {
+        typedef typename std::conditional<BITS == 32, Four<float>, Codes>::type S;
+        p = Four<P>::load(T.p, i, T.n, whole);
+        g = Four<G>::load(T.g, i, T.n, whole);
+        m = S::load(T.m, i, T.n, whole);
+        v = S::load(T.v, i, T.n, whole);
+        if (BITS == 8) {
+            sm = T.ms[i / GP_STATE_BLOCK];
+            sv = T.vs[i / GP_STATE_BLOCK];
         }
-        f32x4 root;
+    }
+};
+struct Step {
+    float factor, step_size, inv_root;
+    unsigned key;
+};
+// The update of four consecutive elements from i on; the 64 lanes of a wave have one
+// block of the 8-bit states.  Every product and sum is rounded by itself, in the order of
+// the formulas, so that an update is the same bits wherever it is compiled.
+template <typename P, typename G, int BITS>
+__device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars& s, const Step& st,
+                                        const Quad<P, G, BITS>& q, long i, bool whole) {
+#pragma clang fp contract(off)
+    f32x4 pv = Four<P>::values(q.p), mv, vv, root;
+    const f32x4 gv = Four<G>::values(q.g);
+    if constexpr (BITS == 32) {
+        mv = q.m;
+        vv = q.v;
+    } else {
+        mv = e4m3_values(q.m) * q.sm;
+        vv = e4m3_values(q.v) * q.sv;
+        vv = vv * vv;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float ge = gv[e] * st.factor;
+        mv[e] = mv[e] * s.b1 + ge * s.c1;
+        vv[e] = vv[e] * s.b2 + ge * ge * s.c2;
+        root[e] = sqrtf(vv[e]);
+        pv[e] = pv[e] * T.keep - st.step_size * mv[e] / (root[e] * st.inv_root + s.eps);
+    }
+    Four<P>::store(T.p, i, T.n, whole, Four<P>::rounded(pv));
+    if (T.c) Four<bf16>::store(T.c, i, T.n, whole, Four<bf16>::rounded(pv));
+    if constexpr (BITS == 32) {
+        Four<float>::store(T.m, i, T.n, whole, mv);
+        Four<float>::store(T.v, i, T.n, whole, vv);
+    } else {
+        float sm, im, sr, ir;
+        block_scale(wave_max_nan(max_nan(max_nan(fabsf(mv[0]), fabsf(mv[1])), max_nan(fabsf(mv[2]), fabsf(mv[3])))), sm, im);
+        block_scale(wave_max_nan(max_nan(max_nan(root[0], root[1]), max_nan(root[2], root[3]))), sr, ir);
+        unsigned h = (unsigned)(i / 4) + st.key;
+        h ^= h >> 16;
+        h *= 0x6A3F9B15u;
+        h ^= h >> 15;
+        h *= 0x5D47C1E3u;
+        h ^= h >> 16;
+        constexpr unsigned K[4] = {0x4F1BBCDDu, 0x7A6D2C8Bu, 0x35E9A1F7u, 0x1D872B41u};
+        unsigned qm = 0, qr = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float ge = gv[e] * factor;
-            mv[e] = mv[e] * s.b1 + ge * s.c1;
-            vv[e] = vv[e] * s.b2 + ge * ge * s.c2;
-            root[e] = sqrtf(vv[e]);
-            pv[e] = pv[e] * T.keep - step_size * mv[e] / (root[e] * inv_root + s.eps);
+            const unsigned u = h * K[e];
+            const float ym = mv[e] * im, yr = root[e] * ir;
+            unsigned cr = e4m3_code(yr, u >> 16);
+            cr = yr > 0.f && cr == 0 ? 1u : cr;
+            qm |= (e4m3_code(ym, u & 0xFFFFu) | (ym < 0.f ? 128u : 0u)) << (8 * e);
+            qr |= cr << (8 * e);
         }
-        store4(p, i, n, T.vec, pv);
-        if (T.c) store4(T.c, i, n, T.vec, pv);
-        if constexpr (BITS == 32) {
-            store4(static_cast<float*>(T.m), i, n, T.vec, mv);
-            store4(static_cast<float*>(T.v), i, n, T.vec, vv);
-        } else {
-            float tm = 0.f, tr = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                tm = max_nan(tm, fabsf(mv[e]));
-                tr = max_nan(tr, root[e]);
-            }
-            float sm, im, sr, ir;
-            block_scale(wave_max_nan(tm), sm, im);
-            block_scale(wave_max_nan(tr), sr, ir);
-            unsigned h = (unsigned)(i / 4) + key;
-            h ^= h >> 16;
-            h *= 0x6A3F9B15u;
-            h ^= h >> 15;
-            h *= 0x5D47C1E3u;
-            h ^= h >> 16;
-            unsigned qm = 0, qr = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const unsigned u = h * K[e];
-                const float ym = mv[e] * im, yr = root[e] * ir;
-                unsigned cr = e4m3_code(yr, u >> 16);
-                cr = yr > 0.f && cr == 0 ? 1u : cr;
-                qm |= (e4m3_code(ym, u & 0xFFFFu) | (ym < 0.f ? 128u : 0u)) << (8 * e);
-                qr |= cr << (8 * e);
-            }
-            store_codes(static_cast<unsigned char*>(T.m), i, n, T.vec, qm);
-            store_codes(static_cast<unsigned char*>(T.v), i, n, T.vec, qr);
-            if (lane == 0) {
-                T.ms[block] = sm;
-                T.vs[block] = sr;
-            }
+        Codes::store(T.m, i, T.n, whole, __builtin_bit_cast(Codes::vec, qm));
+        Codes::store(T.v, i, T.n, whole, __builtin_bit_cast(Codes::vec, qr));
+        if ((threadIdx.x & 63) == 0) {
+            T.ms[i / GP_STATE_BLOCK] = sm;
+            T.vs[i / GP_STATE_BLOCK] = sr;
         }
+    }
+}
+
+template <typename P, typename G, int BITS>
+__global__ void __launch_bounds__(256) adamw_kernel(const AdamwBatch b, const AdamwScalars s) {
+    Step st = {s.factor ? s.factor[0] : 1.f, s.step_size, s.inv_root, s.key};
+    if (st.factor != st.factor) return;
+    if (s.step_dev) {
+        const long long t = s.step_dev[0];
+        st.step_size = s.lr / -expm1f((float)t * s.ln_b1);
+        st.inv_root = 1.f / sqrtf(-expm1f((float)t * s.ln_b2));
+        st.key += KEY_STEP * (unsigned)t;
+    }
+    const int at = tensor_of(b.chunk0, b.n, blockIdx.x);
+    const AdamwTensor& T = b.t[at];
+    const long base = (long)((int)blockIdx.x - b.chunk0[at]) * CHUNK, i = base + (long)threadIdx.x * 4;
+    constexpr int U = CHUNK / 1024;
+    Quad<P, G, BITS> q[U];
+    if (base + CHUNK <= T.n) {  // every load of the chunk before the first use
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u].load(T, i + u * 1024, true);
+#pragma unroll
+        for (int u = 0; u < U; ++u) update4<P, G, BITS>(T, s, st, q[u], i + u * 1024, true);
+        return;
+    }
+    const int lane4 = 4 * (int)(threadIdx.x & 63);
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {
+        const long k = i + u * 1024;
+        if (k - lane4 >= T.n) break;  // the wave's block is behind the end
+        q[0].load(T, k, k + 4 <= T.n);
+        update4<P, G, BITS>(T, s, st, q[0], k, k + 4 <= T.n);
     }
 }
 
@@ -219,27 +232,35 @@ constexpr int NORM_BLOCKS = 2048;  // workgroups at most, but for the tensors' r
 struct NormTensor {
     const void* g;
     long n;
-    int chunk0;
-    int vec;
 };
 constexpr int NORM_BATCH = 128;
 struct NormBatch {
-    NormTensor t[NORM_BATCH];
     int n;
+    int chunk0[NORM_BATCH];
+    NormTensor t[NORM_BATCH];
 };
 
 template <typename G>
 __global__ void __launch_bounds__(256) norm_kernel(const NormBatch b, long chunk, double* __restrict__ partial) {
     __shared__ double red[4];
-    const NormTensor& T = b.t[tensor_of(b, blockIdx.x)];
-    const long base = (long)((int)blockIdx.x - T.chunk0) * chunk, end = min(T.n, base + chunk);
-    const G* g = static_cast<const G*>(T.g);
+    const int at = tensor_of(b.chunk0, b.n, blockIdx.x);
+    const NormTensor& T = b.t[at];
+    const long base = (long)((int)blockIdx.x - b.chunk0[at]) * chunk, end = min(T.n, base + chunk);
     double s = 0.0;
-    for (long i = base + (long)threadIdx.x * 4; i < end; i += 1024) {
-        const f32x4 x = load4(g, i, end, T.vec);
+    long i = base + (long)threadIdx.x * 4;
+    constexpr int U = 4;
+    auto add = [&](f32x4 x) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += (double)x[e] * (double)x[e];
+        for (int e = 0; e < 4; ++e) s = __builtin_fma((double)x[e], (double)x[e], s);
+    };
+    for (; i + (U - 1) * 1024 + 4 <= end; i += U * 1024) {
+        typename Four<G>::vec x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = Four<G>::load(T.g, i + u * 1024, end, true);
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(Four<G>::values(x[u]));
     }
+    for (; i < end; i += 1024) add(Four<G>::values(Four<G>::load(T.g, i, end, i + 4 <= end)));
     s = wave_sum_d(s);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
@@ -350,7 +371,6 @@ gp_status gp_adamw_step(const gp_adamw_tensor* tensors, int n, const gp_adamw_co
         s.inv_root = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)step)));
         s.key += KEY_STEP * (unsigned)step;
     }
-    const size_t pe = elt_size(cfg->param_dtype), ge = elt_size(cfg->grad_dtype);
     for (int i = 0; i < n;) {
         AdamwBatch b;
         b.n = 0;
@@ -360,11 +380,9 @@ gp_status gp_adamw_step(const gp_adamw_tensor* tensors, int n, const gp_adamw_co
             const long more = (long)((x.count + CHUNK - 1) / CHUNK);
             if (more == 0) continue;
             if (chunks + more > 0x7FFFFFFFL) break;
-            const size_t sb = cfg->state_bits == 32 ? 16 : 4;
-            const bool vec = aligned(x.param, 4 * pe) && aligned(x.grad, 4 * ge) && aligned(x.m, sb) &&
-                             aligned(x.v, sb) && aligned(x.copy, 8);
+            b.chunk0[b.n] = (int)chunks;
             b.t[b.n++] = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, static_cast<bf16*>(x.copy), (long)x.count,
-                          (float)(1.0 - cfg->lr * x.weight_decay), (int)chunks, vec ? 1 : 0};
+                          (float)(1.0 - cfg->lr * x.weight_decay)};
             chunks += more;
         }
         if (b.n == 0) break;
@@ -416,7 +434,8 @@ gp_status gp_grad_norm(int dtype, const gp_grad_tensor* grads, int n, float max_
         for (; i < n && b.n < NORM_BATCH; ++i) {
             const int more = (int)((grads[i].count + chunk - 1) / chunk);
             if (more == 0) continue;
-            b.t[b.n++] = {grads[i].grad, (long)grads[i].count, chunks, aligned(grads[i].grad, 4 * ge) ? 1 : 0};
+            b.chunk0[b.n] = chunks;
+            b.t[b.n++] = {grads[i].grad, (long)grads[i].count};
             chunks += more;
         }
         if (b.n == 0) break;

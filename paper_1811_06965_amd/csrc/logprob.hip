@@ -13,9 +13,6 @@ constexpr float LOG2E = 1.44269504088896341f;
 constexpr float NEVER = -1e30f;  // a logit down here is a mask's, its token cannot occur
 constexpr int SPLIT_MAX = 64;    // workgroups of one row: the lanes of the wave that joins them
 
-__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
-__device__ __forceinline__ float min_nan(float a, float b) { return __builtin_elementwise_minimum(a, b); }
-
 // Sums of a row's terms around a reference logit r: with d = x - r, a = sum exp(scale d)
 // and b = sum d exp(scale d).  Then lse = scale r + log a and the entropy is
 // log a - scale b / a, whatever r is; its term stays within 2^8 of the largest.
@@ -25,29 +22,6 @@ struct Part {
     float r, a, b;
 };
 constexpr float NO_REF = -2e30f;  // below every reference
-// A reduction over the 64 lanes in the data-parallel unit: pairs, quads, eights and
-// sixteens in place, then the four rows of sixteen into lane 63, whose value is given
-// to all.  In rows that a step leaves out, `none` (neutral to op) stands in.
-template <int CTRL, int ROWS> __device__ __forceinline__ unsigned lanes_from(unsigned none, unsigned x) {
-    return (unsigned)__builtin_amdgcn_update_dpp((int)none, (int)x, CTRL, ROWS, 0xF, false);
-}
-template <typename Op> __device__ __forceinline__ unsigned wave_reduce(unsigned x, unsigned none, Op op) {
-    x = op(x, lanes_from<0xB1, 0xF>(none, x));   // lane ^ 1
-    x = op(x, lanes_from<0x4E, 0xF>(none, x));   // lane ^ 2
-    x = op(x, lanes_from<0x141, 0xF>(none, x));  // mirrored within eight
-    x = op(x, lanes_from<0x140, 0xF>(none, x));  // mirrored within sixteen
-    x = op(x, lanes_from<0x142, 0xA>(none, x));  // lane 15 of the row before, in rows 1 and 3
-    x = op(x, lanes_from<0x143, 0xC>(none, x));  // lane 31, in rows 2 and 3
-    return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
-}
-template <typename Op> __device__ __forceinline__ float wave_reduce_f(float x, float none, Op op) {
-    return __uint_as_float(wave_reduce(__float_as_uint(x), __float_as_uint(none), [&](unsigned a, unsigned b) {
-        return __float_as_uint(op(__uint_as_float(a), __uint_as_float(b)));
-    }));
-}
-__device__ __forceinline__ unsigned wave_max_u(unsigned x) {
-    return wave_reduce(x, 0u, [](unsigned a, unsigned b) { return a > b ? a : b; });
-}
 // The parts of 64 lanes as one.  c2 = scale log2 e.
 __device__ __forceinline__ Part wave_join(Part p, float c2) {
     const float r = wave_reduce_f(p.r, NO_REF, [](float a, float b) { return max_nan(a, b); });

@@ -90,21 +90,35 @@ __device__ __forceinline__ f32x4 e4m3_values(Codes::vec c) {
     return f32x4{__builtin_amdgcn_cvt_f32_fp8(q, 0), __builtin_amdgcn_cvt_f32_fp8(q, 1),
                  __builtin_amdgcn_cvt_f32_fp8(q, 2), __builtin_amdgcn_cvt_f32_fp8(q, 3)};
 }
-// |y| <= 448 to e4m3, rounded up where the 16 random bits exceed what rounding down
-// leaves of a step: 2^-120 brings the e4m3 exponents (and zero and the subnormals) to
-// those of fp32, whose bits 20 and up are then the code.
-__device__ __forceinline__ unsigned e4m3_code(float y, unsigned rnd16) {
-    const unsigned c = (__float_as_uint(fabsf(y) * 0x1p-120f) + (rnd16 << 4) + 8u) >> 20;
-    return c < 126u ? c : 126u;
+// A block's scale and its inverse from the largest |x| (as bits, so that a NaN, the
+// largest of all, reaches the scale; then the codes mean nothing).
+__device__ __forceinline__ unsigned largest_bits(f32x4 x) {
+    unsigned b[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+    return wave_max_u(max(max(b[0], b[1]), max(b[2], b[3])));
 }
-// A block's scale and its inverse from the largest |x|; NaN and infinities come through as NaN.
 __device__ __forceinline__ void block_scale(float top, float& scale, float& inv) {
     const bool tiny = top < 0x1p-100f;
     scale = tiny ? 0.f : top * (1.f / 448.f);
     inv = tiny ? 0.f : 1.f / top * 448.f;
 }
-__device__ __forceinline__ float wave_max_nan(float v) {
-    return wave_reduce_f(v, 0.f, [](float a, float b) { return max_nan(a, b); });
+// The bits of |x| inv 2^-120, inv the block's: 2^-120 brings the e4m3 exponents (and zero
+// and the subnormals) to those of fp32, whose bits 20 and up are then the code.
+// FOLDED: inv is that times 2^-120 already (a block below 2^13, where it is no subnormal).
+template <bool FOLDED> __device__ __forceinline__ unsigned code_bits(float x, float inv) {
+    return __float_as_uint(FOLDED ? fabsf(x) * inv : fabsf(x) * inv * 0x1p-120f);
+}
+// Rounded up where the 16 random bits exceed what rounding down leaves of a step.
+__device__ __forceinline__ unsigned e4m3_code(unsigned bits, unsigned rnd16) {
+    return min((bits + (rnd16 << 4) + 8u) >> 20, 126u);
+}
+// The square root rounded to nearest: the device's, off by up to a step, and one correction
+// from its exact remainder (half the instructions of sqrtf, which also serves
+// arguments below 2^-96).
+__device__ __forceinline__ float root_of(float x) {
+    const float s = __builtin_amdgcn_sqrtf(x);
+    return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 1e-30f)), s);
 }
 
 // What four lanes' worth of memory holds before the update.
@@ -151,8 +165,14 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
         const float ge = gv[e] * st.factor;
         mv[e] = mv[e] * s.b1 + ge * s.c1;
         vv[e] = vv[e] * s.b2 + ge * ge * s.c2;
-        root[e] = sqrtf(vv[e]);
-        pv[e] = pv[e] * T.keep - st.step_size * mv[e] / (root[e] * st.inv_root + s.eps);
+        if constexpr (BITS == 32) {
+            root[e] = sqrtf(vv[e]);
+            pv[e] = pv[e] * T.keep - st.step_size * mv[e] / (root[e] * st.inv_root + s.eps);
+        } else {  // the parameter's step by a reciprocal that is off by a step
+            root[e] = root_of(vv[e]);
+            const float den = __builtin_fmaf(root[e], st.inv_root, s.eps);
+            pv[e] = __builtin_fmaf(pv[e], T.keep, -st.step_size * mv[e] * __builtin_amdgcn_rcpf(den));
+        }
     }
     Four<P>::store(T.p, i, T.n, whole, Four<P>::rounded(pv));
     if (T.c) Four<bf16>::store(T.c, i, T.n, whole, Four<bf16>::rounded(pv));
@@ -160,9 +180,10 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
         Four<float>::store(T.m, i, T.n, whole, mv);
         Four<float>::store(T.v, i, T.n, whole, vv);
     } else {
+        const float tm = __uint_as_float(largest_bits(mv)), tr = __uint_as_float(largest_bits(root));
         float sm, im, sr, ir;
-        block_scale(wave_max_nan(max_nan(max_nan(fabsf(mv[0]), fabsf(mv[1])), max_nan(fabsf(mv[2]), fabsf(mv[3])))), sm, im);
-        block_scale(wave_max_nan(max_nan(max_nan(root[0], root[1]), max_nan(root[2], root[3]))), sr, ir);
+        block_scale(tm, sm, im);
+        block_scale(tr, sr, ir);
         unsigned h = (unsigned)(i / 4) + st.key;
         h ^= h >> 16;
         h *= 0x6A3F9B15u;
@@ -171,15 +192,20 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
         h ^= h >> 16;
         constexpr unsigned K[4] = {0x4F1BBCDDu, 0x7A6D2C8Bu, 0x35E9A1F7u, 0x1D872B41u};
         unsigned qm = 0, qr = 0;
+        auto codes = [&](auto folded, float am, float ar) {
+            constexpr bool F = decltype(folded)::value;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned u = h * K[e];
-            const float ym = mv[e] * im, yr = root[e] * ir;
-            unsigned cr = e4m3_code(yr, u >> 16);
-            cr = yr > 0.f && cr == 0 ? 1u : cr;
-            qm |= (e4m3_code(ym, u & 0xFFFFu) | (ym < 0.f ? 128u : 0u)) << (8 * e);
-            qr |= cr << (8 * e);
-        }
+            for (int e = 0; e < 4; ++e) {
+                const unsigned u = h * K[e], bm = code_bits<F>(mv[e], am), br = code_bits<F>(root[e], ar);
+                const unsigned sign = __float_as_uint(mv[e]) >> 24 & 0x80u;
+                qm |= (e4m3_code(bm, u & 0xFFFFu) | sign) << (8 * e);
+                qr |= max(e4m3_code(br, u >> 16), min(br, 1u)) << (8 * e);  // not zero stays not zero
+            }
+        };
+        if (tm < 0x1p13f && tr < 0x1p13f)
+            codes(std::true_type{}, im * 0x1p-120f, ir * 0x1p-120f);
+        else
+            codes(std::false_type{}, im, ir);
         Codes::store(T.m, i, T.n, whole, __builtin_bit_cast(Codes::vec, qm));
         Codes::store(T.v, i, T.n, whole, __builtin_bit_cast(Codes::vec, qr));
         if ((threadIdx.x & 63) == 0) {

@@ -1,8 +1,10 @@
 """AdamW over many tensors and the gradient norm against plain implementations.
 
 The update is held to two references: the same fp32 operations in numpy, one
-rounding each (every output, 8-bit codes and scales included, bit for bit), and
-the formulas in 64 bits.  Tolerances of the latter (u = 2^-24): m and v are two
+rounding each (32-bit states with their parameters, 8-bit codes and scales, bit for
+bit), and the formulas in 64 bits.  With 8-bit states the parameter's step takes a
+reciprocal off by 2 u and fused sums: within 16 u of the step and 3 u of the parameter of
+numpy's, and where either is rounded to bf16, a step (2^-7) of it.  Tolerances of the latter (u = 2^-24): m and v are two
 products and a sum, 3 u of the absolute terms; the parameter's step
 x = lr / bc1 m / (sqrt(v) / sqrt(bc2) + eps) has seven roundings beside those of
 m and v: 16 u |x|, then the sum with the decayed parameter, 3 u of it, and half a
@@ -65,7 +67,7 @@ def quantise(x, rnd, keep):
         c = np.minimum(c, 126)
         if keep:
             c = np.where((y > 0) & (c == 0), 1, c)
-        codes[a:a + 256] = c | np.where(y < 0, 128, 0)
+        codes[a:a + 256] = c | np.where(np.signbit(y), 128, 0)  # a zero keeps its sign
     return codes, np.array(scales, F)
 
 
@@ -145,6 +147,7 @@ class Case:
                          lr=h["lr"], seed=h["seed"], **kw)
 
     def host_step(self, t, factor=1.0):
+        self.old = [x.copy() for x in self.p]
         for i in range(len(self.sizes)):
             if self.sizes[i] == 0:
                 continue
@@ -155,17 +158,28 @@ class Case:
             if self.bits == 8:
                 self.ms[i], self.vs[i] = ms, vs
 
+    def check_params(self, i, got):
+        """With 8-bit states: near numpy's, which then goes on from the device's."""
+        if self.bits == 32:
+            assert np.array_equal(got, self.p[i]), i
+            return
+        fine = np.isfinite(self.p[i])
+        step = np.abs(self.old[i] * (1 - self.h["lr"] * self.decay[i]) - self.p[i])
+        tol = 16 * U * step + 4 * U * np.abs(self.old[i]) + (2.0 ** -7 * np.abs(self.p[i]) if self.param == "bf16" else 0)
+        assert (np.abs(got - self.p[i])[fine] <= tol[fine]).all(), i
+        self.p[i] = got
+
     def check(self):
         bits = lambda x: np.ascontiguousarray(x).view(np.uint8)  # noqa: E731
         for i, n in enumerate(self.sizes):
-            assert np.array_equal(self.params[i].float().cpu().numpy(), self.p[i]), (i, n)
+            self.check_params(i, self.params[i].float().cpu().numpy())
             pairs = [(self.dm[i], self.m[i]), (self.dv[i], self.v[i])]
             if self.bits == 8:
                 pairs += [(self.dms[i], self.ms[i]), (self.dvs[i], self.vs[i])]
             for d, x in pairs:
                 d = d.view(torch.uint8) if d.dtype == torch.float8_e4m3fn else d
                 assert np.array_equal(bits(d.cpu().numpy()), bits(x)), (i, n)
-            if self.copies:
+            if self.copies:  # the fp32 parameter as it was stored, rounded
                 assert np.array_equal(self.copies[i].float().cpu().numpy(), bf16_round(self.p[i])), (i, n)
         for name, (buf, host, a, b) in self.flat.items():
             x, y = buf.cpu(), host
@@ -299,8 +313,8 @@ def test_special_gradients(ops):
         good[512:] = False
         assert bool(((p.cpu()[good] - 0.5).abs() < 1e-4).all())  # the first step is lr against the gradient's sign
         if bits == 8:
-            assert opt.v_scale[0].isnan().tolist() == [True, False, False, False]
-            assert not math.isfinite(float(opt.v_scale[0][1]))
+            assert opt.v_scale[0].isfinite().tolist() == [False, False, True, True]
+            assert opt.m_scale[0].isfinite().tolist() == [False, False, True, True]
             assert opt.m_scale[0][3] == 0.0 and bool((opt.m[0].view(torch.uint8)[768:] == 0).all())
 
 

@@ -87,8 +87,10 @@ typedef enum {
  * bytes per parameter because it trains with RMSProp (Table 1 caption):
  * the parameter, its gradient and the running mean square. */
 typedef enum {
-    GP_OPT_SGD = 0,    /* W <- W - lr G */
-    GP_OPT_RMSPROP = 1 /* ms <- rho ms + (1 - rho) G^2;  W <- W - lr G / sqrt(ms + eps);  ms starts at 0 */
+    GP_OPT_SGD = 0,     /* W <- W - lr G */
+    GP_OPT_RMSPROP = 1, /* ms <- rho ms + (1 - rho) G^2;  W <- W - lr G / sqrt(ms + eps);  ms starts at 0 */
+    GP_OPT_ADAMW = 2    /* gp_adamw_step's rule with fp32 moments that start at 0; matrices decay, biases and
+                           LayerNorm parameters do not */
 } gp_optimizer;
 
 typedef struct {
@@ -113,6 +115,13 @@ typedef struct {
     float logit_clip;        /* GP_LOSS_XENT_LS: c > 0 clips every logit to [-c, c] before the softmax
                                 (Section 5 bounds the magnitude of the softmax pre-activations for
                                 trainability); the gradient passes where |z| <= c.  0 = off */
+    float adam_beta1;        /* GP_OPT_ADAMW: in [0, 1) */
+    float adam_beta2;
+    float adam_eps;          /* GP_OPT_ADAMW: > 0, outside the square root */
+    float weight_decay;      /* GP_OPT_ADAMW: >= 0, decoupled (lr weight_decay <= 1 at every step) */
+    float max_grad_norm;     /* GP_OPT_ADAMW: > 0 clips the mini-batch gradient's 2-norm over the partition's
+                                parameters (gp_grad_norm); the update then follows the last backward as a
+                                whole.  0 = off */
 } gp_config;
 
 /* Parameter tensors.  Matrices are logical [in, out] (y = x W + b); attention
@@ -309,12 +318,42 @@ gp_status gp_stream_destroy(gp_stream stream);
  *              and the call synchronises the stream.
  * With check_finite set the call synchronises, and if any gradient is
  * non-finite the update is skipped and GP_ERR_NONFINITE returned.
+ * GP_OPT_ADAMW counts its updates on the device, so that a captured step may be
+ * replayed.  With max_grad_norm a norm that is not finite skips the update on the
+ * device; a call with loss_out then returns GP_ERR_NONFINITE.
  * GP_LOSS_XENT_LS: a label outside [0, V) is read as class 0 on the device
  * and flagged; the next call that synchronises (loss_out non-NULL or
  * check_finite) then skips the update and returns GP_ERR_INVALID_ARG.
  * GP_ERR_STATE: not all M backward micro-batches done.
+ * GP_ERR_INVALID_ARG: GP_OPT_ADAMW with lr < 0, not finite, or lr weight_decay > 1.
  */
 gp_status gp_accumulate_and_step(gp_partition* p, float lr, double* loss_out, gp_stream stream);
+
+/*
+ * The 2-norm of the last step's gradient (before clipping) of a partition with
+ * max_grad_norm.  Synchronises the device.
+ * GP_ERR_INVALID_ARG: p or norm NULL.  GP_ERR_STATE: not configured, or no
+ *   max_grad_norm.
+ */
+gp_status gp_get_grad_norm(gp_partition* p, float* norm);
+
+/*
+ * Log probabilities under the vocabulary head of a GP_LOSS_XENT_LS partition: the forward
+ * pass of one micro-batch's worth of sequences (n, of seq_len tokens), the head's logits
+ * (clipped as configured) and gp_token_logprobs of them, for evaluation and
+ * scoring between mini-batches.  Nothing is kept: no gradient, no stash.
+ *   x, mem : as gp_forward_microbatch.
+ *   tokens, scale, logp, lse, entropy, top, top_ids, top_logp : as gp_token_logprobs,
+ *            with rows = n seq_len in token order.
+ * Ordered after the last update and before the next mini-batch's work by the
+ * library, whatever streams they are issued on.
+ * GP_ERR_STATE: not configured, or inside a mini-batch.
+ * GP_ERR_UNSUPPORTED: the partition has no vocabulary head.
+ * GP_ERR_INVALID_ARG: as gp_forward_microbatch and gp_token_logprobs.
+ */
+gp_status gp_score_sequences(gp_partition* p, const void* x, const void* mem, const int* tokens, float scale,
+                             float* logp, float* lse, float* entropy, int top, int* top_ids, float* top_logp,
+                             gp_stream stream);
 
 /*
  * Launch timers (instrumentation; not part of the method).  Selecting a role

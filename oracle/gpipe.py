@@ -114,9 +114,39 @@ def optimizer_state(layers, head):
     return _zeros_like_grads(layers, head)
 
 
+def adamw_update(cfg, layers, head, g_layers, g_head, lr, state=None):
+    """AdamW with bias corrections and decoupled decay of the matrices; the
+    gradient clipped to a 2-norm of max_grad_norm (0: not) over all tensors.
+    ``state``: (updates done, first moments, second moments), the moments as
+    a list of one dict per layer and the head's."""
+    groups, grads = list(layers) + [head], list(g_layers) + [{k: g_head[k] for k in head}]
+    if state is None:
+        state = (0, *([{k: np.zeros_like(v) for k, v in p.items()} for p in groups] for _ in range(2)))
+    t, ms, vs = state[0] + 1, [], []
+    factor = 1.0
+    if cfg.max_grad_norm > 0:
+        norm = np.sqrt(sum(float((g[k] ** 2).sum()) for p, g in zip(groups, grads) for k in p))
+        factor = min(1.0, cfg.max_grad_norm / norm) if norm > 0 else 1.0
+    new = []
+    for p, g, m0, v0 in zip(groups, grads, state[1], state[2]):
+        m = {k: cfg.adam_beta1 * m0[k] + (1 - cfg.adam_beta1) * factor * g[k] for k in p}
+        v = {k: cfg.adam_beta2 * v0[k] + (1 - cfg.adam_beta2) * (factor * g[k]) ** 2 for k in p}
+        out = {}
+        for k in p:
+            decay = cfg.weight_decay if k.lstrip("x").startswith("w") else 0.0
+            step = m[k] / (1 - cfg.adam_beta1 ** t) / (np.sqrt(v[k] / (1 - cfg.adam_beta2 ** t)) + cfg.adam_eps)
+            out[k] = p[k] - lr * decay * p[k] - lr * step
+        new.append(out)
+        ms.append(m)
+        vs.append(v)
+    return new[:-1], new[-1], (t, ms, vs)
+
+
 def apply_update(cfg, layers, head, g_layers, g_head, lr, state=None):
     """The one synchronous update of the configured optimizer.  Returns
     (layers', head', state') -- state' is None for SGD."""
+    if cfg.optimizer == "adamw":
+        return adamw_update(cfg, layers, head, g_layers, g_head, lr, state)
     if cfg.optimizer == "sgd":
         return (*sgd_update(layers, head, g_layers, g_head, lr), None)
     if cfg.optimizer != "rmsprop":

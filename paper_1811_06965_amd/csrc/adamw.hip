@@ -10,7 +10,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "common.hpp"
+#include "adamw.hpp"
 
 namespace gp {
 
@@ -35,16 +35,6 @@ struct AdamwBatch {
     int chunk0[BATCH];  // chunks of the launch's tensors before each
     AdamwTensor t[BATCH];
 };
-struct AdamwScalars {
-    float lr, b1, c1, b2, c2, eps;  // c = 1 - b
-    float ln_b1, ln_b2;             // step_dev: the bias corrections are computed on the device
-    float step_size, inv_root;      // else: lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
-    unsigned key;                   // of the random bits: the seed's part, and with a host step t's
-    const long long* step_dev;
-    const float* factor;
-};
-constexpr unsigned KEY_SEED = 0x3C6EF372u, KEY_STEP = 0x1E3779B1u;
-
 // The last of n tensors whose first chunk is not after id.
 template <int MOST> __device__ __forceinline__ int tensor_of(const int (&chunk0)[MOST], int n, int id) {
     int l = -1;
@@ -139,15 +129,10 @@ template <typename P, typename G, int BITS> struct Quad {
         }
     }
 };
-struct Step {
-    float factor, step_size, inv_root;
-    unsigned key;
-};
 // The update of four consecutive elements from i on; the 64 lanes of a wave have one
-// block of the 8-bit states.  Every product and sum is rounded by itself, in the order of
-// the formulas, so that an update is the same bits wherever it is compiled.
+// block of the 8-bit states.
 template <typename P, typename G, int BITS>
-__device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars& s, const Step& st,
+__device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars& s, const AdamwStep& st,
                                         const Quad<P, G, BITS>& q, long i, bool whole) {
 #pragma clang fp contract(off)
     f32x4 pv = Four<P>::values(q.p), mv, vv, root;
@@ -162,16 +147,16 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float ge = gv[e] * st.factor;
-        mv[e] = mv[e] * s.b1 + ge * s.c1;
-        vv[e] = vv[e] * s.b2 + ge * ge * s.c2;
+        float m = mv[e], v = vv[e];
+        adamw_moments(gv[e], m, v, s, st);
+        mv[e] = m;
+        vv[e] = v;
         if constexpr (BITS == 32) {
-            root[e] = sqrtf(vv[e]);
-            pv[e] = pv[e] * T.keep - st.step_size * mv[e] / (root[e] * st.inv_root + s.eps);
+            pv[e] = adamw_param(pv[e], m, v, T.keep, s, st);
         } else {  // the parameter's step by a reciprocal that is off by a step
-            root[e] = root_of(vv[e]);
+            root[e] = root_of(v);
             const float den = __builtin_fmaf(root[e], st.inv_root, s.eps);
-            pv[e] = __builtin_fmaf(pv[e], T.keep, -st.step_size * mv[e] * __builtin_amdgcn_rcpf(den));
+            pv[e] = __builtin_fmaf(pv[e], T.keep, -st.step_size * m * __builtin_amdgcn_rcpf(den));
         }
     }
     Four<P>::store(T.p, i, T.n, whole, Four<P>::rounded(pv));
@@ -217,14 +202,8 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
 
 template <typename P, typename G, int BITS>
 __global__ void __launch_bounds__(256) adamw_kernel(const AdamwBatch b, const AdamwScalars s) {
-    Step st = {s.factor ? s.factor[0] : 1.f, s.step_size, s.inv_root, s.key};
-    if (st.factor != st.factor) return;
-    if (s.step_dev) {
-        const long long t = s.step_dev[0];
-        st.step_size = s.lr / -expm1f((float)t * s.ln_b1);
-        st.inv_root = 1.f / sqrtf(-expm1f((float)t * s.ln_b2));
-        st.key += KEY_STEP * (unsigned)t;
-    }
+    AdamwStep st;
+    if (!adamw_begin(s, st)) return;
     const int at = tensor_of(b.chunk0, b.n, blockIdx.x);
     const AdamwTensor& T = b.t[at];
     const long base = (long)((int)blockIdx.x - b.chunk0[at]) * CHUNK, i = base + (long)threadIdx.x * 4;
@@ -365,6 +344,12 @@ void launch_adamw(const AdamwBatch& b, const AdamwScalars& s, int chunks, int bi
 
 } // namespace
 
+gp_status adamw_advance(long long* step, const float* factor, hipStream_t st) {
+    klaunch(advance_kernel, 1, 1, 0, st, step, factor);
+    GP_LAUNCH_CHECK();
+    return GP_OK;
+}
+
 } // namespace gp
 
 using namespace gp;
@@ -378,24 +363,11 @@ gp_status gp_adamw_step(const gp_adamw_tensor* tensors, int n, const gp_adamw_co
     hipStream_t st = (hipStream_t)stream;
     if (!step_dev && capturing(st))
         return set_error(GP_ERR_STATE, "adamw: a captured update needs step_dev (a replay would repeat its step)");
-    AdamwScalars s{};
-    s.lr = (float)cfg->lr;
-    s.b1 = (float)cfg->beta1;
-    s.c1 = (float)(1.0 - cfg->beta1);
-    s.b2 = (float)cfg->beta2;
-    s.c2 = (float)(1.0 - cfg->beta2);
-    s.eps = (float)cfg->eps;
-    s.key = KEY_SEED * cfg->seed;
-    s.step_dev = step_dev;
-    s.factor = factor;
+    const AdamwScalars s =
+        adamw_scalars(cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->seed, step, step_dev, factor);
     if (step_dev) {
-        s.ln_b1 = (float)std::log(cfg->beta1);
-        s.ln_b2 = (float)std::log(cfg->beta2);
-        klaunch(advance_kernel, 1, 1, 0, st, step_dev, factor);
-    } else {
-        s.step_size = (float)(cfg->lr / (1.0 - std::pow(cfg->beta1, (double)step)));
-        s.inv_root = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, (double)step)));
-        s.key += KEY_STEP * (unsigned)step;
+        const gp_status advanced = adamw_advance(step_dev, factor, st);
+        if (advanced != GP_OK) return advanced;
     }
     for (int i = 0; i < n;) {
         AdamwBatch b;

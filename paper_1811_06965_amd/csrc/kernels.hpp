@@ -175,6 +175,12 @@ gp_status quantize_rows_fp4(const void* nk, int out, int in, void* q4, void* q4s
 gp_status update_linears(int dtype, float* master, const float* grads, float* ms, float lr, float rho, float eps,
                          void* welt, const UpdateLinear* table, int l0, int l1, int tiles, const long* ranges,
                          int nranges, int apart, hipStream_t st);
+// The same with the AdamW step (m, v: its moments; keep: 1 - lr weight_decay, of the
+// linears' weights alone).
+struct AdamwScalars;
+gp_status update_linears_adamw(int dtype, float* master, const float* grads, float* m, float* v, const AdamwScalars& s,
+                               float keep, void* welt, const UpdateLinear* table, int l0, int l1, int tiles,
+                               const long* ranges, int nranges, hipStream_t st);
 // An empty launch labelled by its grid (role x (edge + 1) workgroups of one
 // wave): edge 0 before, 1 after a timed launch, so that per-dispatch profiler
 // records can be attributed to launch roles.

@@ -3,6 +3,7 @@
 //
 // All reductions are two-stage with a fixed order (per-block partials, then
 // one finalising block), so every result is reproducible bit for bit.
+#include "adamw.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -354,16 +355,34 @@ __device__ __forceinline__ float update_one(float w, float g, float& m, float lr
 // copies); for small ones by the launches, which one per linear, plus one for
 // the rest, cost 5 us of host time each: the smallest fp32 step 1085 -> 959 us,
 // two ragged layers 1495 -> 1361.
-template <typename T>
+// ADAMW: the AdamW step instead, m1 its first moments and ms its second; weights
+// decay by `keep`, the parameters of the ranges do not (32 bytes per bf16 weight).
+template <typename T, bool ADAMW>
 __global__ void __launch_bounds__(256) update_kernel(float* __restrict__ master, const float* __restrict__ grads,
                                                      float* __restrict__ ms, float lr, float rho, float eps, int rms,
                                                      T* __restrict__ welt, const UpdateLinear* __restrict__ tab, int l0,
-                                                     int l1, int tiles, const long* __restrict__ ranges, int apart) {
+                                                     int l1, int tiles, const long* __restrict__ ranges, int apart,
+                                                     float* __restrict__ m1, const AdamwScalars as, float keep) {
     __shared__ float tile[64][65];
     const int t = threadIdx.x;
+    AdamwStep st;
+    if constexpr (ADAMW) {
+        if (!adamw_begin(as, st)) return;
+    }
+    auto adamw = [&](float w, float g, float& m, float& v, float k) {
+        adamw_moments(g, m, v, as, st);
+        return adamw_param(w, m, v, k, as, st);
+    };
     if ((int)blockIdx.x >= tiles) {
         const long r = blockIdx.x - tiles, off = ranges[2 * r], n = ranges[2 * r + 1];
         for (long i = off + t; i < off + n; i += 256) {
+            if constexpr (ADAMW) {
+                float m = m1[i], v = ms[i];
+                master[i] = adamw(master[i], grads[i], m, v, 1.f);
+                m1[i] = m;
+                ms[i] = v;
+                continue;
+            }
             float m = rms ? ms[i] : 0.f;
             master[i] = update_one(master[i], grads[i], m, lr, rho, eps, rms, apart);
             if (rms) ms[i] = m;
@@ -384,6 +403,7 @@ __global__ void __launch_bounds__(256) update_kernel(float* __restrict__ master,
     float* w = master + u.w;
     const float* g = grads + u.w;
     float* mm = ms + u.w;
+    float* mf = m1 + u.w;
     T* kn = welt + u.kn;
     T* nk = welt + u.nk;
     if (u.in % 64 == 0 && u.out % 64 == 0) {
@@ -394,14 +414,26 @@ __global__ void __launch_bounds__(256) update_kernel(float* __restrict__ master,
             f32x4 v = *reinterpret_cast<const f32x4*>(w + o);
             const f32x4 gv = *reinterpret_cast<const f32x4*>(g + o);
             f32x4 m = {0.f, 0.f, 0.f, 0.f};
-            if (rms) m = *reinterpret_cast<const f32x4*>(mm + o);
+            if (ADAMW || rms) m = *reinterpret_cast<const f32x4*>(mm + o);
+            if constexpr (ADAMW) {
+                f32x4 f = *reinterpret_cast<const f32x4*>(mf + o);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float me = m[e];
-                v[e] = update_one(v[e], gv[e], me, lr, rho, eps, rms, 0);
-                m[e] = me;
+                for (int e = 0; e < 4; ++e) {
+                    float fe = f[e], me = m[e];
+                    v[e] = adamw(v[e], gv[e], fe, me, keep);
+                    f[e] = fe;
+                    m[e] = me;
+                }
+                *reinterpret_cast<f32x4*>(mf + o) = f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float me = m[e];
+                    v[e] = update_one(v[e], gv[e], me, lr, rho, eps, rms, 0);
+                    m[e] = me;
+                }
             }
-            if (rms) *reinterpret_cast<f32x4*>(mm + o) = m;
+            if (ADAMW || rms) *reinterpret_cast<f32x4*>(mm + o) = m;
             *reinterpret_cast<f32x4*>(w + o) = v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) tile[r][c + j] = v[j];
@@ -425,9 +457,15 @@ __global__ void __launch_bounds__(256) update_kernel(float* __restrict__ master,
         const int row = r0 + r, col = c0 + tx;
         if (row < u.in && col < u.out) {
             const long o = (long)row * u.out + col;
-            float m = rms ? mm[o] : 0.f;
-            const float v = update_one(w[o], g[o], m, lr, rho, eps, rms, 0);
-            if (rms) mm[o] = m;
+            float m = ADAMW || rms ? mm[o] : 0.f, v;
+            if constexpr (ADAMW) {
+                float f = mf[o];
+                v = adamw(w[o], g[o], f, m, keep);
+                mf[o] = f;
+            } else {
+                v = update_one(w[o], g[o], m, lr, rho, eps, rms, 0);
+            }
+            if (ADAMW || rms) mm[o] = m;
             w[o] = v;
             tile[r][tx] = v;
             kn[o] = to_elt<T>(v);
@@ -636,11 +674,25 @@ gp_status update_linears(int dtype, float* master, const float* grads, float* ms
                          int nranges, int apart, hipStream_t st) {
     if (tiles + nranges <= 0) return GP_OK;
     if (dtype == GP_BF16)
-        klaunch(update_kernel<bf16>, tiles + nranges, 256, 0, st, master, grads, ms, lr, rho, eps, ms ? 1 : 0,
-                static_cast<bf16*>(welt), table, l0, l1, tiles, ranges, apart);
+        klaunch(update_kernel<bf16, false>, tiles + nranges, 256, 0, st, master, grads, ms, lr, rho, eps, ms ? 1 : 0,
+                static_cast<bf16*>(welt), table, l0, l1, tiles, ranges, apart, nullptr, AdamwScalars{}, 0.f);
     else
-        klaunch(update_kernel<float>, tiles + nranges, 256, 0, st, master, grads, ms, lr, rho, eps, ms ? 1 : 0,
-                static_cast<float*>(welt), table, l0, l1, tiles, ranges, apart);
+        klaunch(update_kernel<float, false>, tiles + nranges, 256, 0, st, master, grads, ms, lr, rho, eps, ms ? 1 : 0,
+                static_cast<float*>(welt), table, l0, l1, tiles, ranges, apart, nullptr, AdamwScalars{}, 0.f);
+    GP_LAUNCH_CHECK();
+    return GP_OK;
+}
+
+gp_status update_linears_adamw(int dtype, float* master, const float* grads, float* m, float* v, const AdamwScalars& s,
+                               float keep, void* welt, const UpdateLinear* table, int l0, int l1, int tiles,
+                               const long* ranges, int nranges, hipStream_t st) {
+    if (tiles + nranges <= 0) return GP_OK;
+    if (dtype == GP_BF16)
+        klaunch(update_kernel<bf16, true>, tiles + nranges, 256, 0, st, master, grads, v, 0.f, 0.f, 0.f, 0,
+                static_cast<bf16*>(welt), table, l0, l1, tiles, ranges, 0, m, s, keep);
+    else
+        klaunch(update_kernel<float, true>, tiles + nranges, 256, 0, st, master, grads, v, 0.f, 0.f, 0.f, 0,
+                static_cast<float*>(welt), table, l0, l1, tiles, ranges, 0, m, s, keep);
     GP_LAUNCH_CHECK();
     return GP_OK;
 }

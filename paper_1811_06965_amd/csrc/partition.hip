@@ -33,6 +33,7 @@
 #include <utility>
 #include <vector>
 
+#include "adamw.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
 #include "sched.hpp"
@@ -309,7 +310,15 @@ struct gp_partition {
     hipEvent_t tail_done = nullptr;
     unsigned long long tail_capture = 0;
     bool dw_started = false;   // a weight-gradient GEMM of this mini-batch was launched
-    float* opt_ms = nullptr;  // RMSProp: running mean square of every gradient [n32]
+    float* opt_ms = nullptr;  // RMSProp: running mean square of every gradient [n32]; AdamW: second moments
+    float* opt_m = nullptr;   // AdamW: first moments [n32]
+    long long* opt_step = nullptr;  // AdamW: updates done, on the device (a captured step is replayed)
+    // AdamW with max_grad_norm: the parameter blocks' gradients, the norm's scratch, and
+    // the norm with the factor that clips it
+    std::vector<gp_grad_tensor> norm_list;
+    void* norm_ws = nullptr;
+    size_t norm_ws_bytes = 0;
+    float* norm_factor = nullptr;
     // The update's tables in device memory: the linears in plan order (their
     // weights are updated fused with the refresh of their working copies) and
     // the rest -- biases, LayerNorm parameters -- as (offset, count) float
@@ -648,6 +657,18 @@ void plan_workspace(gp_partition* p, Arena& a) {
         b.h = a.take_elt(T * D, e);
         b.z = a.take_elt(T * (long)g.V, e);
         p->head_span = span_from(h0);
+    }
+    p->opt_step = nullptr;
+    p->norm_ws = nullptr;
+    p->norm_factor = nullptr;
+    if (g.optimizer == GP_OPT_ADAMW) {
+        p->opt_step = a.take<long long>(1);
+        if (g.max_grad_norm > 0.f) {
+            p->norm_ws_bytes = 0;
+            (void)gp_grad_norm_workspace((int)(p->plan.linears().size() + norms.size()), &p->norm_ws_bytes);
+            p->norm_ws = a.take<char>(p->norm_ws_bytes);
+            p->norm_factor = a.take<float>(2);
+        }
     }
     // the odd backward lane's head scratch; the loss partials and the flags are shared
     p->head1_span = Span{};
@@ -1487,9 +1508,9 @@ void free_all(gp_partition* p) {
     p->timer = LaunchTimer();
     p->timer.markers = markers;
     for (void* x : {(void*)p->master, (void*)p->grads, (void*)p->welt, (void*)p->stash_x, (void*)p->stash_m,
-                    (void*)p->ws, (void*)p->opt_ms, (void*)p->upd_ranges, (void*)p->upd_tab})
+                    (void*)p->ws, (void*)p->opt_ms, (void*)p->opt_m, (void*)p->upd_ranges, (void*)p->upd_tab})
         if (x) (void)hipFree(x);
-    p->master = p->grads = p->opt_ms = nullptr;
+    p->master = p->grads = p->opt_ms = p->opt_m = nullptr;
     p->upd_ranges = nullptr;
     p->upd_tab = nullptr;
     p->n_upd_ranges = 0;
@@ -1585,11 +1606,17 @@ void plan_partition(gp_partition* p, const gp_config* cfg) {
     g.rms_decay = cfg->rms_decay;
     g.rms_eps = cfg->rms_eps;
     g.logit_clip = cfg->logit_clip;
+    g.beta1 = cfg->adam_beta1;
+    g.beta2 = cfg->adam_beta2;
+    g.adam_eps = cfg->adam_eps;
+    g.weight_decay = cfg->weight_decay;
+    g.max_grad_norm = cfg->max_grad_norm;
     p->esz = g.dtype == GP_BF16 ? 2 : 4;
     if (const char* e = std::getenv("GP_TIMER_MARKERS")) p->timer.markers = std::atoi(e) != 0;
     if (const char* e = std::getenv("GP_SIDE_STREAM")) p->use_side = std::atoi(e) != 0;
     p->layer_update = (4L * p->d.D + 2L * p->d.F) * p->d.D >= 2000000;
     if (const char* e = std::getenv("GP_LAYER_UPDATE")) p->layer_update = std::atoi(e) != 0;
+    if (g.max_grad_norm > 0.f) p->layer_update = false;  // every gradient before the first update
     if (const char* e = std::getenv("GP_REMAT_AHEAD")) p->remat_ahead = std::atoi(e) != 0;
     // Early recompute by default where a micro-batch has at most 1024 rows:
     // with 2048 (enc1024, M = 8) the recompute of the last pair competes with
@@ -1641,8 +1668,8 @@ void plan_partition(gp_partition* p, const gp_config* cfg) {
     p->plan = plan_params(p->d, g);
     Arena measure;
     plan_workspace(p, measure);
-    const bool rms = g.optimizer == GP_OPT_RMSPROP;
-    p->bytes_params = p->plan.n32 * 4 * (rms ? 2 : 1) + p->plan.nelt * p->esz;
+    const int states = g.optimizer == GP_OPT_ADAMW ? 2 : g.optimizer == GP_OPT_RMSPROP ? 1 : 0;
+    p->bytes_params = p->plan.n32 * 4 * (1 + states) + p->plan.nelt * p->esz;
     p->bytes_grads = p->plan.n32 * 4;
     p->bytes_stash = (size_t)g.M * (g.T() + g.Tm()) * p->d.D * p->esz;
     p->bytes_ws = measure.off;
@@ -1698,7 +1725,7 @@ gp_status gp_partition_configure(gp_partition* p, const gp_config* cfg) {
     if (s != GP_OK) return set_error(s, msg.c_str());
     plan_partition(p, cfg);
     const Geometry& g = p->g;
-    const bool rms = g.optimizer == GP_OPT_RMSPROP;
+    const bool adamw = g.optimizer == GP_OPT_ADAMW, moment2 = adamw || g.optimizer == GP_OPT_RMSPROP;
     void *m = nullptr, *gr = nullptr, *we = nullptr, *sx = nullptr, *sm = nullptr, *ws = nullptr;
     s = alloc(&m, p->plan.n32 * 4);
     if (s == GP_OK) s = alloc(&gr, p->plan.n32 * 4);
@@ -1707,8 +1734,11 @@ gp_status gp_partition_configure(gp_partition* p, const gp_config* cfg) {
     if (s == GP_OK && g.Tm() > 0) s = alloc(&sm, (size_t)g.M * g.Tm() * p->d.D * p->esz);
     if (s == GP_OK) s = alloc(&ws, p->bytes_ws);
     void* ms = nullptr;
-    if (s == GP_OK && rms) s = alloc(&ms, p->plan.n32 * 4);
+    if (s == GP_OK && moment2) s = alloc(&ms, p->plan.n32 * 4);
+    void* m1 = nullptr;
+    if (s == GP_OK && adamw) s = alloc(&m1, p->plan.n32 * 4);
     p->opt_ms = (float*)ms;
+    p->opt_m = (float*)m1;
     p->master = (float*)m;
     p->grads = (float*)gr;
     p->welt = (char*)we;
@@ -1730,11 +1760,18 @@ gp_status gp_partition_configure(gp_partition* p, const gp_config* cfg) {
     if (e == hipSuccess) e = hipMemset(p->grads, 0, p->plan.n32 * 4);
     if (e == hipSuccess) e = hipMemset(p->ws, 0, p->bytes_ws);
     if (e == hipSuccess && p->opt_ms) e = hipMemset(p->opt_ms, 0, p->plan.n32 * 4);
+    if (e == hipSuccess && p->opt_m) e = hipMemset(p->opt_m, 0, p->plan.n32 * 4);
     if (e != hipSuccess) {
         free_all(p);
         return hip_fail(e, __FILE__, __LINE__);
     }
     s = build_update_tables(p);
+    p->norm_list.clear();
+    if (p->norm_factor) {  // blocks without the padding between them
+        for (const Linear* l : p->plan.linears())
+            p->norm_list.push_back({p->grads + l->w, (long long)((size_t)l->in * l->out + l->out)});
+        for (const Norm* n : p->plan.norms()) p->norm_list.push_back({p->grads + n->g, 2LL * n->n});
+    }
     if (s != GP_OK) {
         free_all(p);
         return s;
@@ -1810,8 +1847,8 @@ static gp_status param_io(gp_partition* p, int layer, int id, float* host, size_
     gp_status s = resolve_param(p->plan, p->d, layer, id, r, msg);
     if (s != GP_OK) return set_error(s, msg.c_str());
     if (count != (size_t)r.rows * r.cols) return set_error(GP_ERR_INVALID_ARG, "count does not match the parameter's size");
+    GP_HIP(hipDeviceSynchronize());  // work on a non-blocking stream may still read what is written here
     if (what == 0) return upload_param_block(p, r, host);
-    GP_HIP(hipDeviceSynchronize());
     const float* src = (what == 1 ? p->master : p->grads) + r.off;
     GP_HIP(hipMemcpy2D(host, (size_t)r.cols * 4, src, (size_t)r.ld * 4, (size_t)r.cols * 4, r.rows,
                        hipMemcpyDeviceToHost));
@@ -2259,6 +2296,10 @@ gp_status gp_accumulate_and_step(gp_partition* p, float lr, double* loss_out, gp
     std::string msg;
     gp_status s = p->sched.can_step(msg);
     if (s != GP_OK) return set_error(s, msg.c_str());
+    const Geometry& g = p->g;
+    const bool adamw = g.optimizer == GP_OPT_ADAMW;
+    if (adamw && !(lr >= 0.f && lr < 1e30f && (double)lr * g.weight_decay <= 1.0))
+        return set_error(GP_ERR_INVALID_ARG, "AdamW needs a finite lr >= 0 and lr weight_decay <= 1");
     hipStream_t st = (hipStream_t)stream;
     const int dt = p->g.dtype;
     // both backward lanes' last calls (their weight gradients included)
@@ -2293,9 +2334,18 @@ gp_status gp_accumulate_and_step(gp_partition* p, float lr, double* loss_out, gp
     }
     const bool rms = p->g.optimizer == GP_OPT_RMSPROP;
     const int nlin = (int)p->upd_tile0.size() - 1;
+    AdamwScalars as{};
+    const float* factor = p->norm_factor ? p->norm_factor + 1 : nullptr;
+    if (adamw) as = adamw_scalars(lr, g.beta1, g.beta2, g.adam_eps, 0, 0, p->opt_step, factor);
+    const float keep = (float)(1.0 - (double)lr * g.weight_decay);
     // linears l0 .. l1 - 1 in one launch, with the biases and LayerNorm parameters or without
     auto update = [&](int l0, int l1, bool rest, hipStream_t us) -> gp_status {
-        GP_TRY(update_linears(dt, p->master, p->grads, rms ? p->opt_ms : nullptr, lr, p->g.rms_decay, p->g.rms_eps,
+        if (adamw)
+            GP_TRY(update_linears_adamw(dt, p->master, p->grads, p->opt_m, p->opt_ms, as, keep, p->welt, p->upd_tab, l0,
+                                        l1, p->upd_tile0[l1] - p->upd_tile0[l0], p->upd_ranges,
+                                        rest ? p->n_upd_ranges : 0, us));
+        else
+            GP_TRY(update_linears(dt, p->master, p->grads, rms ? p->opt_ms : nullptr, lr, p->g.rms_decay, p->g.rms_eps,
                               p->welt, p->upd_tab, l0, l1, p->upd_tile0[l1] - p->upd_tile0[l0], p->upd_ranges,
                               rest ? p->n_upd_ranges : 0, p->upd_apart, us));
         if (!p->plan.layers[0].ffn1.split) return GP_OK;
@@ -2313,6 +2363,8 @@ gp_status gp_accumulate_and_step(gp_partition* p, float lr, double* loss_out, gp
         const hipStream_t us = p->remat;
         for (int l = p->d.L - 1; l >= 0; --l) {
             GP_HIP(hipStreamWaitEvent(us, p->lay_main[l], 0));
+            // the last update's launches, which read the counter, are behind that event
+            if (adamw && l == p->d.L - 1) GP_TRY(adamw_advance(p->opt_step, nullptr, us));
             if (p->lay_side[l]) GP_HIP(hipStreamWaitEvent(us, p->lay_side[l], 0));
             GP_TRY(update(p->upd_layer[l], p->upd_layer[l + 1], false, us));
         }
@@ -2321,10 +2373,16 @@ gp_status gp_accumulate_and_step(gp_partition* p, float lr, double* loss_out, gp
         GP_HIP(hipStreamWaitEvent(st, upd, 0));
         GP_TRY(update(p->upd_layer[p->d.L], nlin, true, st));
     } else {
+        if (p->norm_factor)
+            GP_TRY(gp_grad_norm(GP_F32, p->norm_list.data(), (int)p->norm_list.size(), g.max_grad_norm, p->norm_factor,
+                                p->norm_ws, p->norm_ws_bytes, stream));
+        if (adamw) GP_TRY(adamw_advance(p->opt_step, factor, st));
         GP_TRY(update(0, nlin, true, st));
     }
+    float clip[2] = {0.f, 1.f};  // the norm and its factor, where the call synchronises anyway
     if (loss_out) {
         double v = 0.0;
+        if (p->norm_factor) GP_HIP(hipMemcpyAsync(clip, p->norm_factor, sizeof clip, hipMemcpyDeviceToHost, st));
         if (p->g.loss != GP_LOSS_NONE) {
             GP_TRY(loss_finalize(p->bw.loss_partial, (long)p->loss_rows, p->loss_used(), p->g.M, p->bw.loss_acc, st));
             GP_HIP(hipMemcpyAsync(&v, p->bw.loss_acc, sizeof(double), hipMemcpyDeviceToHost, st));
@@ -2341,7 +2399,56 @@ gp_status gp_accumulate_and_step(gp_partition* p, float lr, double* loss_out, gp
     }
     give_streams(p);
     p->sched.did_step();
+    if (clip[1] != clip[1]) return set_error(GP_ERR_NONFINITE, "the gradient norm is not finite: update skipped");
     return GP_OK;
+}
+
+gp_status gp_get_grad_norm(gp_partition* p, float* norm) {
+    if (!p || !norm) return set_error(GP_ERR_INVALID_ARG, "partition and norm must not be NULL");
+    if (!p->sched.configured()) return set_error(GP_ERR_STATE, "partition not configured");
+    if (!p->norm_factor) return set_error(GP_ERR_STATE, "the partition clips no gradient norm (max_grad_norm is 0)");
+    GP_HIP(hipDeviceSynchronize());
+    GP_HIP(hipMemcpy(norm, p->norm_factor, sizeof(float), hipMemcpyDeviceToHost));
+    return GP_OK;
+}
+
+gp_status gp_score_sequences(gp_partition* p, const void* x, const void* mem, const int* tokens, float scale,
+                             float* logp, float* lse, float* entropy, int top, int* top_ids, float* top_logp,
+                             gp_stream stream) {
+    if (!p) return set_error(GP_ERR_INVALID_ARG, "partition must not be NULL");
+    std::string msg;
+    const gp_status s = p->sched.can_score(msg);
+    if (s != GP_OK) return set_error(s, msg.c_str());
+    if (p->g.loss != GP_LOSS_XENT_LS)
+        return set_error(GP_ERR_UNSUPPORTED, "scoring needs the vocabulary head of a cross-entropy partition");
+    if (!x) return set_error(GP_ERR_INVALID_ARG, "x must not be NULL");
+    const bool dec = p->g.kind == GP_DECODER_CROSS;
+    if (dec && !mem) return set_error(GP_ERR_INVALID_ARG, "decoder partitions need the memory input");
+    if (!dec && mem) return set_error(GP_ERR_INVALID_ARG, "encoder partitions take no memory input");
+    const long T = p->g.T(), V = p->g.V, D = p->d.D;
+    BwdWs& b = p->bw;
+    // the operator's own checks before anything is enqueued (no rows: nothing is)
+    GP_TRY(gp_token_logprobs(p->g.dtype, b.z, 0, (int)V, V, tokens, scale, p->g.logit_clip, logp, lse, entropy, top,
+                             top_ids, top_logp, nullptr, 0, stream));
+    if ((logp && !tokens) || (top > 0 && (!top_ids || !top_logp)))
+        return set_error(GP_ERR_INVALID_ARG, "logp needs tokens, top needs top_ids and top_logp");
+    Ctx c = first_pass_ctx(p, (hipStream_t)stream, 0);
+    GP_TRY(order_first_pass(p, c, true));
+    if (p->poison) {
+        GP_TRY(poison_span(p, p->splitk_span[0], c.st));
+        GP_TRY(poison_first_pass_slot(p, 0, c.st));
+        GP_TRY(poison_span(p, p->head_span, c.st));
+        GP_TRY(poison_span(p, p->bwd_span, c.st));
+    }
+    GP_TRY(partition_forward(c, 0, false, x, mem, nullptr));
+    const HeadPlan& Hd = p->plan.head;
+    const float* y = p->fpass[0].xs[p->d.L & 1];
+    GP_TRY(timed_ln_fwd(c, y, T, (int)D, p->master + Hd.lnf.g, p->master + Hd.lnf.b, p->g.eps, b.h, b.sth));
+    GP_TRY(linear_fwd(c, Hd.out, b.h, T, b.z, V, EPI_STORE, 0, nullptr, nullptr));
+    // the backward's scratch is free between mini-batches
+    GP_TRY(gp_token_logprobs(p->g.dtype, b.z, T, (int)V, V, tokens, scale, p->g.logit_clip, logp, lse, entropy, top,
+                             top_ids, top_logp, b.dn, (size_t)T * D * sizeof(float), stream));
+    return record_first_pass(p, c);
 }
 
 } // extern "C"

@@ -35,6 +35,8 @@ struct Geometry {
     int optimizer = GP_OPT_SGD;
     float rms_decay = 0.f, rms_eps = 0.f;
     float logit_clip = 0.f;
+    float beta1 = 0.f, beta2 = 0.f, adam_eps = 0.f, weight_decay = 0.f;  // AdamW
+    float max_grad_norm = 0.f;
     int ffn_fp4 = 1;  // bf16: fp4 correction of the feed-forward input projection (see Linear::split)
     int ffn_f16 = 1;  // bf16: that projection with fp16 operands instead, where the widths allow (Linear::f16)
     long long T() const { return (long long)n * S; }     // token rows of one micro-batch
@@ -73,11 +75,24 @@ inline gp_status check_config(const Dims& d, const gp_config& c, std::string& ms
     if (!(c.label_smoothing >= 0.f && c.label_smoothing < 1.f)) { msg = "label_smoothing must be in [0, 1)"; return GP_ERR_INVALID_ARG; }
     if (!(c.ln_eps > 0.f)) { msg = "ln_eps must be positive"; return GP_ERR_INVALID_ARG; }
     if (c.keep_activations != 0 && c.keep_activations != 1) { msg = "keep_activations must be 0 or 1"; return GP_ERR_INVALID_ARG; }
-    if (c.optimizer != GP_OPT_SGD && c.optimizer != GP_OPT_RMSPROP) { msg = "unknown optimizer"; return GP_ERR_INVALID_ARG; }
+    if (c.optimizer != GP_OPT_SGD && c.optimizer != GP_OPT_RMSPROP && c.optimizer != GP_OPT_ADAMW) {
+        msg = "unknown optimizer"; return GP_ERR_INVALID_ARG;
+    }
+    if (c.optimizer == GP_OPT_ADAMW &&
+        !(c.adam_beta1 >= 0.f && c.adam_beta1 < 1.f && c.adam_beta2 >= 0.f && c.adam_beta2 < 1.f && c.adam_eps > 0.f &&
+          c.adam_eps < 1e30f && c.weight_decay >= 0.f && c.weight_decay < 1e30f && c.max_grad_norm >= 0.f)) {
+        msg = "AdamW needs adam_beta1 and adam_beta2 in [0, 1), adam_eps > 0, weight_decay and max_grad_norm >= 0";
+        return GP_ERR_INVALID_ARG;
+    }
+    if (c.optimizer != GP_OPT_ADAMW && (c.adam_beta1 != 0.f || c.adam_beta2 != 0.f || c.adam_eps != 0.f ||
+                                        c.weight_decay != 0.f || c.max_grad_norm != 0.f)) {
+        msg = "adam_beta1, adam_beta2, adam_eps, weight_decay and max_grad_norm are only used by AdamW";
+        return GP_ERR_INVALID_ARG;
+    }
     if (c.optimizer == GP_OPT_RMSPROP && !(c.rms_decay >= 0.f && c.rms_decay < 1.f && c.rms_eps > 0.f)) {
         msg = "RMSProp needs rms_decay in [0, 1) and rms_eps > 0"; return GP_ERR_INVALID_ARG;
     }
-    if (c.optimizer == GP_OPT_SGD && (c.rms_decay != 0.f || c.rms_eps != 0.f)) {
+    if (c.optimizer != GP_OPT_RMSPROP && (c.rms_decay != 0.f || c.rms_eps != 0.f)) {
         msg = "rms_decay and rms_eps are only used by RMSProp"; return GP_ERR_INVALID_ARG;
     }
     if (!(c.logit_clip >= 0.f) || (c.logit_clip > 0.f && c.loss != GP_LOSS_XENT_LS)) {
@@ -486,6 +501,12 @@ class Sched {
     void did_backward() {
         --next_bwd;
         if (next_bwd < 0) phase = Phase::Ready;
+    }
+    // Scoring uses a first-pass slot and the head's buffers: between mini-batches only.
+    gp_status can_score(std::string& msg) const {
+        if (phase == Phase::Created) { msg = "partition not configured"; return GP_ERR_STATE; }
+        if (phase != Phase::Idle) { msg = "scoring runs between mini-batches"; return GP_ERR_STATE; }
+        return GP_OK;
     }
     gp_status can_step(std::string& msg) const {
         if (phase == Phase::Created) { msg = "partition not configured"; return GP_ERR_STATE; }

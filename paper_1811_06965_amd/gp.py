@@ -20,7 +20,7 @@ STATUS_NAMES = {0: "GP_OK", 1: "GP_ERR_INVALID_ARG", 2: "GP_ERR_STATE", 3: "GP_E
 GP_F32, GP_BF16 = 0, 1
 GP_ENCODER, GP_DECODER_CROSS = 0, 1
 GP_LOSS_NONE, GP_LOSS_MSE, GP_LOSS_XENT_LS = 0, 1, 2
-GP_OPT_SGD, GP_OPT_RMSPROP = 0, 1
+GP_OPT_SGD, GP_OPT_RMSPROP, GP_OPT_ADAMW = 0, 1, 2
 
 PARAM_IDS = ["ln1_g", "ln1_b", "wq", "bq", "wk", "bk", "wv", "bv", "wo", "bo", "ln2_g", "ln2_b",
              "w1", "b1", "w2", "b2", "xwq", "xbq", "xwk", "xbk", "xwv", "xbv", "xwo", "xbo",
@@ -41,7 +41,7 @@ EXPORTS = ["gp_partition_create", "gp_partition_configure", "gp_partition_destro
            "gp_timer_reset", "gp_timer_sample", "gp_mfma_peak", "gp_recomputed_output", "gp_memory_plan",
            "gp_forward_microbatch_noalloc", "gp_plan_cells", "gp_stream_create", "gp_stream_destroy",
            "gp_token_logprobs", "gp_token_logprobs_workspace", "gp_token_logprobs_backward", "gp_grad_norm",
-           "gp_grad_norm_workspace", "gp_adamw_step", "gp_last_error"]
+           "gp_grad_norm_workspace", "gp_adamw_step", "gp_get_grad_norm", "gp_score_sequences", "gp_last_error"]
 
 GP_TOP_MAX, GP_NO_TOKEN, GP_STATE_BLOCK = 32, -1, 256
 
@@ -52,7 +52,9 @@ class gp_config(ctypes.Structure):
                 ("mem_seq_len", ctypes.c_int), ("loss", ctypes.c_int), ("vocab", ctypes.c_int),
                 ("label_smoothing", ctypes.c_float), ("ln_eps", ctypes.c_float),
                 ("check_finite", ctypes.c_int), ("keep_activations", ctypes.c_int), ("optimizer", ctypes.c_int),
-                ("rms_decay", ctypes.c_float), ("rms_eps", ctypes.c_float), ("logit_clip", ctypes.c_float)]
+                ("rms_decay", ctypes.c_float), ("rms_eps", ctypes.c_float), ("logit_clip", ctypes.c_float),
+                ("adam_beta1", ctypes.c_float), ("adam_beta2", ctypes.c_float), ("adam_eps", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("max_grad_norm", ctypes.c_float)]
 
 
 class gp_grad_tensor(ctypes.Structure):
@@ -121,6 +123,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.gp_grad_norm_workspace.argtypes = [I, ctypes.POINTER(SZ)]
     lib.gp_adamw_step.argtypes = [ctypes.POINTER(gp_adamw_tensor), I, ctypes.POINTER(gp_adamw_config),
                                   ctypes.c_longlong, VP, VP, VP]
+    lib.gp_get_grad_norm.argtypes = [P, ctypes.POINTER(F)]
+    lib.gp_score_sequences.argtypes = [P, VP, VP, VP, F, VP, VP, VP, I, VP, VP, VP]
     lib.gp_last_error.argtypes = []
     lib.gp_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -221,6 +225,16 @@ def gp_accumulate_and_step(h, lr, want_loss, stream):
         return v.value
     _check(load().gp_accumulate_and_step(h, lr, None, stream))
     return None
+
+
+def gp_get_grad_norm(h):
+    v = ctypes.c_float()
+    _check(load().gp_get_grad_norm(h, ctypes.byref(v)))
+    return v.value
+
+
+def gp_score_sequences(h, x, mem, tokens, scale, logp, lse, entropy, top, top_ids, top_logp, stream):
+    _check(load().gp_score_sequences(h, x, mem, tokens, scale, logp, lse, entropy, top, top_ids, top_logp, stream))
 
 
 def gp_timer_select(h, role):

@@ -13,6 +13,7 @@ import numpy as np
 import torch
 
 from . import gp
+from .ops import TokenLogprobs
 
 # One second stream per device for the odd micro-batches, created by the
 # library once per process (a stream from torch's pool may share a hardware
@@ -30,7 +31,7 @@ def second_stream():
 DTYPES = {"f32": (gp.GP_F32, torch.float32), "bf16": (gp.GP_BF16, torch.bfloat16)}
 KINDS = {"encoder": gp.GP_ENCODER, "decoder": gp.GP_DECODER_CROSS}
 LOSSES = {"none": gp.GP_LOSS_NONE, "mse": gp.GP_LOSS_MSE, "xent_ls": gp.GP_LOSS_XENT_LS}
-OPTIMIZERS = {"sgd": gp.GP_OPT_SGD, "rmsprop": gp.GP_OPT_RMSPROP}
+OPTIMIZERS = {"sgd": gp.GP_OPT_SGD, "rmsprop": gp.GP_OPT_RMSPROP, "adamw": gp.GP_OPT_ADAMW}
 
 
 def make_config(cfg, micro: Optional[int] = None, check_finite: bool = False,
@@ -56,6 +57,9 @@ def make_config(cfg, micro: Optional[int] = None, check_finite: bool = False,
         c.rms_decay = cfg.rms_decay
         c.rms_eps = cfg.rms_eps
     c.logit_clip = cfg.logit_clip
+    if cfg.optimizer == "adamw":
+        c.adam_beta1, c.adam_beta2, c.adam_eps = cfg.adam_beta1, cfg.adam_beta2, cfg.adam_eps
+        c.weight_decay, c.max_grad_norm = cfg.weight_decay, cfg.max_grad_norm
     return c
 
 
@@ -212,6 +216,33 @@ class Partition:
             self.step(x, mem, dy, lr=lr, want_y=want_y, want_dx=dx is not None, want_dmem=dmem is not None,
                       want_loss=False, y=y, dx=dx, dmem=dmem, fwd_streams=1, bwd_streams=1)
         return g
+
+    def score(self, x, tokens=None, mem=None, scale=1.0, top=0, stream=None):
+        """Log probabilities, entropies and alternatives under the vocabulary
+        head (gp_score_sequences) for n S tokens: x [n, S, D] and mem in the
+        partition dtype, tokens int32 [n, S].  An ops.TokenLogprobs of rows n S."""
+        rows, dev = self.cfg.batch // self.M * self.cfg.seq, x.device
+        if tokens is not None and (tokens.dtype != torch.int32 or tokens.numel() != rows or not tokens.is_contiguous()):
+            raise ValueError("tokens must be contiguous int32, one per position")
+        want = {"x": (x, rows * self.cfg.d_model)}
+        if mem is not None:
+            want["mem"] = (mem, self.cfg.batch // self.M * self.cfg.mem_seq * self.cfg.d_model)
+        for name, (t, count) in want.items():
+            if t.dtype != self.tdtype or t.numel() != count or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {self.tdtype} of {count} elements")
+        st = torch.cuda.current_stream().cuda_stream if stream is None else stream
+        logp, lse, entropy = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind(0)
+        top_ids = torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None
+        top_logp = torch.empty((rows, top), dtype=torch.float32, device=dev) if top else None
+        ptr = lambda t: None if t is None else t.data_ptr()
+        gp.gp_score_sequences(self.h, x.data_ptr(), ptr(mem), ptr(tokens), scale,
+                              logp.data_ptr() if tokens is not None else None, lse.data_ptr(), entropy.data_ptr(), top,
+                              ptr(top_ids), ptr(top_logp), st)
+        return TokenLogprobs(logp if tokens is not None else None, lse, entropy, top_ids, top_logp)
+
+    def grad_norm(self):
+        """The last step's gradient norm, before clipping (max_grad_norm)."""
+        return gp.gp_get_grad_norm(self.h)
 
     # ------------------------------------------------------------ timers
     def timer_select(self, role):

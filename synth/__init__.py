@@ -63,10 +63,16 @@ class PartitionConfig:
     label_smoothing: float = 0.0
     mem_seq: int = 0
     ln_eps: float = 1e-5
-    # the one synchronous update: "sgd" or "rmsprop" (decay rho, eps inside the square root)
+    # the one synchronous update: "sgd", "rmsprop" (decay rho, eps inside the square root) or
+    # "adamw" (matrices decay; max_grad_norm > 0 clips the gradient's norm first)
     optimizer: str = "sgd"
     rms_decay: float = 0.9
     rms_eps: float = 1e-10
+    adam_beta1: float = 0.9
+    adam_beta2: float = 0.999
+    adam_eps: float = 1e-8
+    weight_decay: float = 0.0
+    max_grad_norm: float = 0.0
     # cross-entropy head: clip the logits to [-logit_clip, logit_clip] (0 = off)
     logit_clip: float = 0.0
     # initialisation: > 0 divides the Xavier-uniform draws of the feed-forward

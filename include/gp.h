@@ -293,6 +293,24 @@ gp_status gp_backward_microbatch_remat(gp_partition* p, int mb, const void* dy_o
                                        void* dmem, gp_stream stream);
 
 /*
+ * gp_backward_microbatch_remat of a GP_LOSS_XENT_LS partition with weights of the
+ * caller's in the place of the label-smoothed cross-entropy (policy gradients, masked
+ * or weighted likelihoods): the mini-batch objective is any function of the tokens'
+ * log probabilities and entropies (gp_score_sequences), given by its gradient.
+ *   tokens   : device int32 [n, S] in [0, V), or GP_NO_TOKEN; any other value makes
+ *              the gradients NaN.
+ *   dlogp, dentropy : device fp32 [n, S], the objective's derivatives, not
+ *              normalised any further; one of them may be NULL.
+ * The loss that the step reports is sum dlogp logp + dentropy entropy over the micro-batches
+ * that went this way, plus the cross-entropy of the others.
+ * GP_ERR_UNSUPPORTED: no vocabulary head.  GP_ERR_INVALID_ARG: also tokens NULL,
+ *   both weights NULL, a misaligned address.  Otherwise as
+ *   gp_backward_microbatch_remat.
+ */
+gp_status gp_backward_microbatch_weighted(gp_partition* p, int mb, const int* tokens, const float* dlogp,
+                                          const float* dentropy, void* dx, void* dmem, gp_stream stream);
+
+/*
  * A non-blocking HIP stream of default priority on the current device, for a
  * caller that issues micro-batches on a second stream (a helper, not a step
  * of the method).  HIP maps streams onto a small pool of hardware queues

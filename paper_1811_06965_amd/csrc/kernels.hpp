@@ -154,6 +154,9 @@ gp_status loss_finalize(const double* partial, long stride, int used, int M, dou
 gp_status xent_ls(int dtype, void* z, long rows, int V, const int* labels, float ls, float clip, double norm,
                   double* partial, int* bad_label, hipStream_t st);
 int xent_partials(long rows);
+// partial[row] = dlogp logp + dentropy entropy (either pair may be nullptr), in fp64
+gp_status token_objective(const float* logp, const float* entropy, const float* dlogp, const float* dentropy, long rows,
+                          double* partial, hipStream_t st);
 
 // --------------------------------------------------------------- update
 // Sustained bf16 MFMA rate of a register-only 32x32x16 loop on every CU

@@ -258,6 +258,21 @@ __global__ void __launch_bounds__(256) xent_rows_kernel(bf16* __restrict__ z, in
     }
 }
 
+// A token's share of the linear objective of gp_backward_microbatch_weighted; a
+// weight of 0 takes no part (a padded token's log probability may be anything).
+__global__ void __launch_bounds__(256) token_objective_kernel(const float* __restrict__ logp,
+                                                              const float* __restrict__ entropy,
+                                                              const float* __restrict__ dlogp,
+                                                              const float* __restrict__ dentropy, long rows,
+                                                              double* __restrict__ partial) {
+    const long r = (long)blockIdx.x * 256 + threadIdx.x;
+    if (r >= rows) return;
+    double s = 0.0;
+    if (dlogp && dlogp[r] != 0.f) s += (double)dlogp[r] * logp[r];
+    if (dentropy && dentropy[r] != 0.f) s += (double)dentropy[r] * entropy[r];
+    partial[r] = s;
+}
+
 // kn = W, nk = W^T through a 64 x 64 LDS tile (both writes coalesced).
 template <typename T>
 __global__ void __launch_bounds__(256) refresh_kernel(const float* __restrict__ w, int in, int out,
@@ -633,6 +648,14 @@ gp_status xent_ls(int dtype, void* z, long rows, int V, const int* labels, float
     else
         klaunch(xent_kernel<float>, (unsigned)rows, 256, 0, st, reinterpret_cast<float*>(z), V, labels, ls, clip, norm,
                 partial, bad_label);
+    GP_LAUNCH_CHECK();
+    return GP_OK;
+}
+
+gp_status token_objective(const float* logp, const float* entropy, const float* dlogp, const float* dentropy, long rows,
+                          double* partial, hipStream_t st) {
+    klaunch(token_objective_kernel, (unsigned)((rows + 255) / 256), 256, 0, st, logp, entropy, dlogp, dentropy, rows,
+            partial);
     GP_LAUNCH_CHECK();
     return GP_OK;
 }

@@ -1395,7 +1395,15 @@ gp_status layer_backward(const Ctx& c, int set, int half, int l, bool first, flo
     return GP_OK;
 }
 
-gp_status head_backward(const Ctx& c, int set, bool first, const int* labels, void* dy_elt, double* loss_partial) {
+// What gp_backward_microbatch_weighted takes in the place of the label-smoothed
+// cross-entropy: the objective's gradients with respect to every token's log
+// probability and entropy.
+struct TokenWeights {
+    const float *dlogp, *dentropy;
+};
+
+gp_status head_backward(const Ctx& c, int set, bool first, const int* labels, const TokenWeights* tw, void* dy_elt,
+                        double* loss_partial) {
     gp_partition* p = c.p;
     const HeadPlan& Hd = p->plan.head;
     BwdWs& b = c.bw ? *c.bw : p->bw;
@@ -1405,7 +1413,18 @@ gp_status head_backward(const Ctx& c, int set, bool first, const int* labels, vo
     GP_TRY(timed_ln_fwd(c, y, T, (int)D, p->master + Hd.lnf.g, p->master + Hd.lnf.b, p->g.eps, b.h, b.sth));
     GP_TRY(linear_fwd(c, Hd.out, b.h, T, b.z, V, EPI_STORE, 0, nullptr, nullptr));
     const double norm = (double)p->g.n * p->g.M * p->g.S;
-    GP_TRY(xent_ls(c.dt, b.z, T, (int)V, labels, p->g.ls, p->g.logit_clip, norm, loss_partial, b.bad_label, c.st));
+    if (tw) {
+        // logp, lse, entropy in the scratch that the head's input gradient takes next
+        float *logp = b.dn, *lse = logp + T, *entropy = lse + T;
+        const gp_stream st = c.st;
+        GP_TRY(gp_token_logprobs(c.dt, b.z, T, (int)V, V, labels, 1.f, p->g.logit_clip, logp, lse, entropy, 0, nullptr,
+                                 nullptr, nullptr, 0, st));
+        GP_TRY(token_objective(logp, entropy, tw->dlogp, tw->dentropy, T, loss_partial, c.st));
+        GP_TRY(gp_token_logprobs_backward(c.dt, b.z, T, (int)V, V, labels, 1.f, p->g.logit_clip, lse, entropy, tw->dlogp,
+                                          tw->dentropy, b.z, V, st));
+    } else {
+        GP_TRY(xent_ls(c.dt, b.z, T, (int)V, labels, p->g.ls, p->g.logit_clip, norm, loss_partial, b.bad_label, c.st));
+    }
     GP_TRY(linear_dw(c, DwJob{&Hd.out, b.h, b.z, T}, acc));
     GP_TRY(linear_dx(c, Hd.out, b.z, T, b.dn, EPI_F32, nullptr, 0));
     return norm_bwd(c, Hd.lnf, b.dn, y, b.sth, T, nullptr, b.p32, dy_elt, acc);
@@ -2031,8 +2050,8 @@ gp_status gp_forward_microbatch_noalloc(gp_partition* p, int mb, const void* x, 
     return GP_OK;
 }
 
-gp_status gp_backward_microbatch_remat(gp_partition* p, int mb, const void* dy_or_target, void* dx, void* dmem,
-                                       gp_stream stream) {
+static gp_status backward_microbatch(gp_partition* p, int mb, const void* dy_or_target, const TokenWeights* tw, void* dx,
+                                     void* dmem, gp_stream stream) {
     if (!p) return set_error(GP_ERR_INVALID_ARG, "partition must not be NULL");
     std::string msg;
     gp_status s = p->sched.can_backward(mb, msg);
@@ -2162,7 +2181,7 @@ gp_status gp_backward_microbatch_remat(gp_partition* p, int mb, const void* dy_o
         const double norm = (double)p->g.n * p->g.M * p->g.S * D;
         s = mse_grad(c.dt, p->xs[set][p->d.L], dy_or_target, T * D, norm, b.p32, top, loss_partial, &nb, c.st);
     } else {
-        s = head_backward(c, set, first, reinterpret_cast<const int*>(dy_or_target), top, loss_partial);
+        s = head_backward(c, set, first, reinterpret_cast<const int*>(dy_or_target), tw, top, loss_partial);
     }
     if (s != GP_OK) return s;
     if (head_order && record_hi) {
@@ -2266,6 +2285,23 @@ gp_status gp_backward_microbatch_remat(gp_partition* p, int mb, const void* dy_o
     }
     p->sched.did_backward();
     return GP_OK;
+}
+
+gp_status gp_backward_microbatch_remat(gp_partition* p, int mb, const void* dy_or_target, void* dx, void* dmem,
+                                       gp_stream stream) {
+    return backward_microbatch(p, mb, dy_or_target, nullptr, dx, dmem, stream);
+}
+
+gp_status gp_backward_microbatch_weighted(gp_partition* p, int mb, const int* tokens, const float* dlogp,
+                                          const float* dentropy, void* dx, void* dmem, gp_stream stream) {
+    if (!p) return set_error(GP_ERR_INVALID_ARG, "partition must not be NULL");
+    if (p->sched.configured() && p->g.loss != GP_LOSS_XENT_LS)
+        return set_error(GP_ERR_UNSUPPORTED, "token weights need the vocabulary head of a cross-entropy partition");
+    if (!dlogp && !dentropy) return set_error(GP_ERR_INVALID_ARG, "dlogp or dentropy must be given");
+    for (const void* q : {(const void*)tokens, (const void*)dlogp, (const void*)dentropy})
+        if (reinterpret_cast<uintptr_t>(q) & 3) return set_error(GP_ERR_INVALID_ARG, "a misaligned address");
+    const TokenWeights tw = {dlogp, dentropy};
+    return backward_microbatch(p, mb, tokens, &tw, dx, dmem, stream);
 }
 
 gp_status gp_stream_create(gp_stream* out) {

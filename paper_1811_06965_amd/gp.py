@@ -41,7 +41,8 @@ EXPORTS = ["gp_partition_create", "gp_partition_configure", "gp_partition_destro
            "gp_timer_reset", "gp_timer_sample", "gp_mfma_peak", "gp_recomputed_output", "gp_memory_plan",
            "gp_forward_microbatch_noalloc", "gp_plan_cells", "gp_stream_create", "gp_stream_destroy",
            "gp_token_logprobs", "gp_token_logprobs_workspace", "gp_token_logprobs_backward", "gp_grad_norm",
-           "gp_grad_norm_workspace", "gp_adamw_step", "gp_get_grad_norm", "gp_score_sequences", "gp_last_error"]
+           "gp_grad_norm_workspace", "gp_adamw_step", "gp_get_grad_norm", "gp_score_sequences",
+           "gp_backward_microbatch_weighted", "gp_last_error"]
 
 GP_TOP_MAX, GP_NO_TOKEN, GP_STATE_BLOCK = 32, -1, 256
 
@@ -123,6 +124,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.gp_grad_norm_workspace.argtypes = [I, ctypes.POINTER(SZ)]
     lib.gp_adamw_step.argtypes = [ctypes.POINTER(gp_adamw_tensor), I, ctypes.POINTER(gp_adamw_config),
                                   ctypes.c_longlong, VP, VP, VP]
+    lib.gp_backward_microbatch_weighted.argtypes = [P, I, VP, VP, VP, VP, VP, VP]
     lib.gp_get_grad_norm.argtypes = [P, ctypes.POINTER(F)]
     lib.gp_score_sequences.argtypes = [P, VP, VP, VP, F, VP, VP, VP, I, VP, VP, VP]
     lib.gp_last_error.argtypes = []
@@ -216,6 +218,10 @@ def gp_forward_microbatch_noalloc(h, mb, x, mem, y, stream):
 
 def gp_backward_microbatch_remat(h, mb, dy_or_target, dx, dmem, stream):
     _check(load().gp_backward_microbatch_remat(h, mb, dy_or_target, dx, dmem, stream))
+
+
+def gp_backward_microbatch_weighted(h, mb, tokens, dlogp, dentropy, dx, dmem, stream):
+    _check(load().gp_backward_microbatch_weighted(h, mb, tokens, dlogp, dentropy, dx, dmem, stream))
 
 
 def gp_accumulate_and_step(h, lr, want_loss, stream):

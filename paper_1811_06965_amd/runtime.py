@@ -141,7 +141,7 @@ class Partition:
 
     def step(self, x, mem, dy, lr=0.0, want_y=True, want_dx=True, want_dmem=True, want_loss=True,
              stream=None, y=None, dx=None, dmem=None, want_recomputed=False, noalloc=False, fwd_streams=2,
-             bwd_streams=2):
+             bwd_streams=2, dlogp=None, dentropy=None):
         """One mini-batch through GPipe's schedule.  x/mem/dy: device tensors
         of the whole mini-batch (dim 0 = sequences).  Returns dict(y, dx, dmem,
         loss); with want_recomputed also "y_remat", the partition output as
@@ -154,7 +154,9 @@ class Partition:
         likewise the odd micro-batches' backwards (the library runs the two
         members of a recompute pair side by side where it has two backward
         lanes, and orders them itself otherwise); the launch stream waits for
-        the second stream before the update."""
+        the second stream before the update.  dlogp, dentropy (fp32 [N, S]):
+        dy holds tokens, and the backwards go through
+        gp_backward_microbatch_weighted with these weights."""
         M = self.M
         main = torch.cuda.current_stream() if stream is None else torch.cuda.ExternalStream(stream)
         st = main.cuda_stream
@@ -174,6 +176,12 @@ class Partition:
         ms = mem.chunk(M) if mem is not None else [None] * M
         ys = y.chunk(M) if y is not None else [None] * M
         dys = dy.chunk(M)
+        weights = None
+        if dlogp is not None or dentropy is not None:
+            for w in (dlogp, dentropy):
+                if w is not None and (w.dtype != torch.float32 or w.shape != dy.shape or not w.is_contiguous()):
+                    raise ValueError("dlogp and dentropy must be contiguous float32 of the tokens' shape")
+            weights = [[None] * M if w is None else w.chunk(M) for w in (dlogp, dentropy)]
         dxs = dx.chunk(M) if dx is not None else [None] * M
         dms = dmem.chunk(M) if dmem is not None else [None] * M
         ptr = lambda t: None if t is None else t.data_ptr()
@@ -190,7 +198,11 @@ class Partition:
             blanes.append(self._lane.cuda_stream)
         for m in range(M - 1, -1, -1):
             bs = blanes[m % len(blanes)]
-            gp.gp_backward_microbatch_remat(self.h, m, ptr(dys[m]), ptr(dxs[m]), ptr(dms[m]), bs)
+            if weights is None:
+                gp.gp_backward_microbatch_remat(self.h, m, ptr(dys[m]), ptr(dxs[m]), ptr(dms[m]), bs)
+            else:
+                gp.gp_backward_microbatch_weighted(self.h, m, ptr(dys[m]), *(ptr(w[m]) for w in weights), ptr(dxs[m]),
+                                                   ptr(dms[m]), bs)
             if want_recomputed:
                 gp.gp_recomputed_output(self.h, ptr(yr[m]), bs)
         if len(blanes) > 1:
@@ -201,7 +213,7 @@ class Partition:
             out["y_remat"] = y_remat
         return out
 
-    def capture_step(self, x, mem, dy, lr=0.0, dx=None, dmem=None, want_y=False, y=None):
+    def capture_step(self, x, mem, dy, lr=0.0, dx=None, dmem=None, want_y=False, y=None, dlogp=None, dentropy=None):
         """Capture one whole mini-batch step (M forwards, M backwards, the
         update) into a HIP graph on a capture stream and return it; replay()
         runs the step again on the same buffers.  The capture itself runs no
@@ -214,7 +226,7 @@ class Partition:
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
             self.step(x, mem, dy, lr=lr, want_y=want_y, want_dx=dx is not None, want_dmem=dmem is not None,
-                      want_loss=False, y=y, dx=dx, dmem=dmem, fwd_streams=1, bwd_streams=1)
+                      want_loss=False, y=y, dx=dx, dmem=dmem, fwd_streams=1, bwd_streams=1, dlogp=dlogp, dentropy=dentropy)
         return g
 
     def score(self, x, tokens=None, mem=None, scale=1.0, top=0, stream=None):

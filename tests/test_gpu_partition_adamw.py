@@ -328,3 +328,117 @@ def test_scoring_is_refused_inside_a_mini_batch():
             with pytest.raises((gp.GpError, ValueError, RuntimeError)):
                 part.score(x, tok, mem, **bad)
         torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------- token weights
+def oracle_weighted_step(cfg, case, tok, a, b):
+    """Loss, dx and gradients of sum a logp + b H over a mini-batch in one pass (float64), the head's gradient through
+    the oracle's own layers."""
+    from oracle import gpipe, transformer as tf
+    y, caches = gpipe.partition_forward(cfg, case["layers"], case["x"], case["mem"])
+    hd = case["head"]
+    h, ln = tf.layer_norm(y, hd["lnf_g"], hd["lnf_b"], cfg.ln_eps)
+    raw = tf.linear(h, hd["wout"], hd["bout"])
+    z = np.clip(raw, -cfg.logit_clip, cfg.logit_clip) if cfg.logit_clip > 0 else raw
+    m = z.max(-1, keepdims=True)
+    logp = z - m - np.log(np.exp(z - m).sum(-1, keepdims=True))
+    p = np.exp(logp)
+    H = -(p * logp).sum(-1, keepdims=True)
+    one = (np.arange(cfg.vocab) == tok[..., None]).astype(float)
+    aa = np.where(tok < 0, 0.0, a)[..., None]
+    dz = aa * (one - p) - b[..., None] * p * (logp + H)
+    if cfg.logit_clip > 0:
+        dz = dz * (np.abs(raw) <= cfg.logit_clip)
+    loss = float((aa * (one * logp).sum(-1, keepdims=True)).sum() + (b[..., None] * H).sum())
+    g = {"wout": np.einsum("nsd,nsv->dv", h, dz), "bout": dz.sum((0, 1))}
+    dh = dz @ hd["wout"].T
+    dy, dg, db = tf.layer_norm_backward(dh, ln, hd["lnf_g"])
+    g["lnf_g"], g["lnf_b"] = dg, db
+    dx, dmem, gl = gpipe.partition_backward(cfg, case["layers"], caches, dy)
+    return loss, dx, gl, g
+
+
+@pytest.mark.parametrize("clip", [0.0, 0.7])
+@pytest.mark.parametrize("cfg", [DEC_F32, DEC_BF16, DEC_BF16.with_(name="m4", batch=8, micro=4)], ids=lambda c: c.name)
+def test_weighted_tokens_match_oracle(cfg, clip):
+    """A policy-like objective (weights of both signs, padding, an entropy bonus): loss, input gradient and every
+    parameter gradient against the oracle, and the same bits on one stream and on two."""
+    from parity import compare_grads, cosine, to_np
+    from paper_1811_06965_amd.runtime import Partition
+    cfg = cfg.with_(logit_clip=clip)
+    case = synth.make_case(cfg, 51, perturb=True)
+    case["head"] = dict(case["head"], wout=synth.round_storage(4.0 * case["head"]["wout"], cfg.dtype))
+    rng = np.random.default_rng(3)
+    tok = np.array(case["labels"])
+    tok[rng.random(tok.shape) < 0.2] = -1
+    a = (rng.standard_normal(tok.shape) / tok.size).astype(np.float32)
+    b = (-0.1 * rng.random(tok.shape) / tok.size).astype(np.float32)
+    loss, dx, gl, gh = oracle_weighted_step(cfg, case, tok, a.astype(float), b.astype(float))
+    t = lambda v, k: torch.tensor(v, dtype=k, device="cuda")  # noqa: E731
+    res = []
+    for streams in (1, 2):
+        with Partition(cfg) as part:
+            part.load_params(case["layers"], case["head"])
+            inp = part.device_inputs(case)
+            out = part.step(inp["x"], inp["mem"], t(tok, torch.int32), lr=0.0, dlogp=t(a, torch.float32),
+                            dentropy=t(b, torch.float32), fwd_streams=streams, bwd_streams=streams)
+            torch.cuda.synchronize()
+            res.append((out["loss"], out["dx"], part.grads()))
+    (l1, d1, g1), (l2, d2, g2) = res
+    assert l1 == l2 and torch.equal(d1, d2)
+    assert all(np.array_equal(u, v) for (_, u), (_, v) in zip(tensors(g1), tensors(g2)))
+    mode, tol = ("rel", 1e-4) if cfg.dtype == "f32" else ("cos", 0.999)
+    # the loss adds and cancels terms of both signs: against the sum of their magnitudes
+    size = np.abs(a).sum() * np.log(cfg.vocab) + np.abs(b).sum() * np.log(cfg.vocab)
+    assert abs(l1 - loss) <= (1e-4 if mode == "rel" else 2e-2) * size
+    assert (rel_err(to_np(d1), dx) <= tol) if mode == "rel" else (cosine(to_np(d1), dx) >= tol)
+    compare_grads(*g1, gl, gh, mode, tol)
+
+
+def test_weights_of_the_likelihood_are_the_cross_entropy():
+    """dlogp = -1 / (N S) is the head's own loss without label smoothing: the same loss and gradients within fp32."""
+    from parity import compare_grads
+    from paper_1811_06965_amd import gp
+    from paper_1811_06965_amd.runtime import Partition
+    cfg = DEC_F32.with_(label_smoothing=0.0)
+    case = synth.make_case(cfg, 52, perturb=True)
+    res = []
+    for weighted in (False, True):
+        with Partition(cfg) as part:
+            part.load_params(case["layers"], case["head"])
+            inp = part.device_inputs(case)
+            kw = dict(dlogp=torch.full(inp["dy"].shape, -1.0 / inp["dy"].numel(), device="cuda")) if weighted else {}
+            out = part.step(inp["x"], inp["mem"], inp["dy"], **kw)
+            res.append((out["loss"], part.grads()))
+            if weighted:
+                with pytest.raises(ValueError):
+                    part.step(inp["x"], inp["mem"], inp["dy"], dlogp=torch.zeros(3, device="cuda"))
+    with Partition(TINY) as part:
+        with pytest.raises(gp.GpError) as err:
+            gp.gp_backward_microbatch_weighted(part.h, 0, 64, 64, None, None, None, None)
+        assert err.value.status == gp.GP_ERR_UNSUPPORTED
+    assert abs(res[0][0] - res[1][0]) <= 1e-5 * abs(res[0][0])
+    compare_grads(*res[1][1], *res[0][1], "rel", 1e-4)
+
+
+def test_a_weighted_step_replays():
+    from paper_1811_06965_amd.runtime import Partition
+    cfg = DEC_BF16.with_(**ADAMW, max_grad_norm=0.5)
+    case = synth.make_case(cfg, 53, perturb=True)
+    res = []
+    for graph in (False, True):
+        with Partition(cfg) as part:
+            part.load_params(case["layers"], case["head"])
+            inp = part.device_inputs(case)
+            w = torch.linspace(-1, 1, inp["dy"].numel(), device="cuda").view(inp["dy"].shape) / 100
+            kw = dict(dlogp=w, dentropy=w * 0.1)
+            if graph:
+                g = part.capture_step(inp["x"], inp["mem"], inp["dy"], lr=1e-3, **kw)
+                for _ in range(3):
+                    g.replay()
+                    torch.cuda.synchronize()
+            else:
+                for _ in range(3):
+                    part.step(inp["x"], inp["mem"], inp["dy"], lr=1e-3, want_loss=False, **kw)
+            res.append(tensors(part.params()))
+    assert all(np.array_equal(u, v) for (_, u), (_, v) in zip(*res))

@@ -64,6 +64,11 @@ def test_null_partitions(gp):
     assert lib.gp_get_grad_norm(h, None) == gp.GP_ERR_INVALID_ARG
     assert lib.gp_get_grad_norm(h, ctypes.byref(f)) == gp.GP_ERR_STATE
     assert lib.gp_score_sequences(h, None, None, None, 1.0, None, None, None, 0, None, None, None) == gp.GP_ERR_STATE
+    back = lib.gp_backward_microbatch_weighted
+    assert back(None, 0, None, None, None, None, None, None) == 1
+    assert back(h, 0, 64, None, None, None, None, None) == 1  # neither weight
+    assert back(h, 0, 64, 66, None, None, None, None) == 1    # misaligned
+    assert back(h, 0, 64, 64, None, None, None, None) == gp.GP_ERR_STATE
     gp.gp_partition_destroy(h)
 
 

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple, Optional, Sequence, Union
 
+import numpy as np
 import torch
 
 from . import gp
@@ -111,14 +112,27 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentr
 
 
 def _same(name, tensors, like=None):
-    """Tensors of one type on one device, each contiguous (and of the shapes of `like`)."""
+    """Tensors of one type on one GPU, each contiguous (and of the sizes of `like`)."""
     tensors = list(tensors)
-    for t in tensors:
-        if t.dtype != tensors[0].dtype or t.device != tensors[0].device or not t.is_cuda or not t.is_contiguous():
+    if tensors:
+        kind, dev = tensors[0].dtype, tensors[0].get_device()
+        if dev < 0 or any(t.dtype != kind or t.get_device() != dev or not t.is_contiguous() for t in tensors):
             raise ValueError(f"{name} must be contiguous tensors of one type on one GPU")
-    if like is not None and (len(like) != len(tensors) or any(a.numel() != b.numel() for a, b in zip(like, tensors))):
+    if like is not None and [t.numel() for t in tensors] != [t.numel() for t in like]:
         raise ValueError(f"{name} must match the parameters one by one")
     return tensors
+
+
+def _records(struct, n, **columns):
+    """An array of n ctypes structures from columns of whole numbers or floats, and what keeps it alive."""
+    rows = np.zeros(n, dtype=np.dtype(struct))
+    for name, values in columns.items():
+        rows[name] = values
+    return rows, ctypes.cast(rows.ctypes.data, ctypes.POINTER(struct))
+
+
+def _addresses(tensors):
+    return [t.data_ptr() for t in tensors]
 
 
 class TensorList:
@@ -130,16 +144,16 @@ class TensorList:
         if not self.tensors or self.tensors[0].dtype not in DTYPE:
             raise ValueError("a TensorList needs float32 or bfloat16 tensors")
         self.dtype = DTYPE[self.tensors[0].dtype]
-        self.array = (gp.gp_grad_tensor * len(self.tensors))()
-        for a, t in zip(self.array, self.tensors):
-            a.grad, a.count = t.data_ptr(), t.numel()
+        self.scratch = gp.gp_grad_norm_workspace(len(self.tensors))  # bytes that grad_norm takes
+        self._rows, self.array = _records(gp.gp_grad_tensor, len(self.tensors), grad=_addresses(self.tensors),
+                                          count=[t.numel() for t in self.tensors])
 
 
 def grad_norm(grads: Union[TensorList, Sequence[torch.Tensor]], max_norm=float("inf")):
     """fp32 [2] on the device: the 2-norm over all the tensors, and the factor
     min(1, max_norm / norm) that clips them (NaN where the norm is not finite)."""
     g = grads if isinstance(grads, TensorList) else TensorList(grads)
-    dev, need = g.tensors[0].device, gp.gp_grad_norm_workspace(len(g.tensors))
+    dev, need = g.tensors[0].device, g.scratch
     out = torch.empty(2, dtype=torch.float32, device=dev)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _on(dev, lambda stream: gp.gp_grad_norm(g.dtype, g.array, len(g.tensors), max_norm, out.data_ptr(), ws.data_ptr(),
@@ -198,14 +212,16 @@ class AdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         if len(decay) != n:
             raise ValueError("weight_decay must be a number or one per parameter")
-        self.array = (gp.gp_adamw_tensor * n)()
-        for i, (a, p) in enumerate(zip(self.array, self.params)):
-            a.param, a.count, a.weight_decay = p.data_ptr(), p.numel(), decay[i]
-            a.m, a.v = self.m[i].data_ptr(), self.v[i].data_ptr()
-            if state_bits == 8:
-                a.m_scale, a.v_scale = self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()
-            if self.copies:
-                a.copy = self.copies[i].data_ptr()
+        columns = dict(param=_addresses(self.params), count=[p.numel() for p in self.params], weight_decay=decay,
+                       m=_addresses(self.m), v=_addresses(self.v))
+        if state_bits == 8:
+            columns.update(m_scale=_addresses(self.m_scale), v_scale=_addresses(self.v_scale))
+        if self.copies:
+            columns["copy"] = _addresses(self.copies)
+        live = [a for k in ("param", "m", "v") for a, c in zip(columns[k], columns["count"]) if c]
+        if len(set(live)) < len(live):
+            raise ValueError("a parameter or a state is given twice")
+        self._rows, self.array = _records(gp.gp_adamw_tensor, n, **columns)
         self.cfg = gp.gp_adamw_config(DTYPE[self.params[0].dtype], 0, state_bits, seed, lr, betas[0], betas[1], eps)
         self.steps = steps
         self.step_dev = torch.full((1,), steps, dtype=torch.int64, device=dev) if capturable else None
@@ -218,8 +234,7 @@ class AdamW:
             raise ValueError("grads must be float32 or bfloat16 on the parameters' device")
         self.grads = grads
         self.cfg.grad_dtype = DTYPE[grads[0].dtype]
-        for a, g in zip(self.array, grads):
-            a.grad = g.data_ptr()
+        self._rows["grad"] = _addresses(grads)
 
     def step(self, lr: Optional[float] = None, factor: Optional[torch.Tensor] = None):
         """One update.  factor: fp32 on the device, multiplied into every

@@ -11,7 +11,7 @@ namespace {
 
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float NEVER = -1e30f;  // a logit down here is a mask's, its token cannot occur
-constexpr int SPLIT_MAX = 64;    // workgroups of one row: the lanes of the wave that joins them
+constexpr int SPLIT_MAX = 32;    // workgroups of one row: at most the lanes of the wave that joins them
 
 // Sums of a row's terms around a reference logit r: with d = x - r, a = sum exp(scale d)
 // and b = sum d exp(scale d).  Then lse = scale r + log a and the entropy is
@@ -445,15 +445,17 @@ int chunk_count(int dtype, int vocab) {
     const int n = dtype == GP_BF16 ? 8 : 4;
     return vocab / n + (vocab % n ? 1 : 0);
 }
-// Workgroups of a row, joined by a second launch: several for up to 32 rows of 128 KB or
-// more, each over 16 KB or more of it, while one workgroup's loads, at 60 GB/s, take
-// longer than the joining.  us, split / whole: one row of 131072 bf16 with 5
-// alternatives 9.4 / 14.8, 32 such rows 10.9 / 15.3, one of 262144 fp32 9.3 / 25.2; but
-// one of 32000 bf16 8.4 / 7.4 and 64 of 131072 17.3 / 16.4.
+// Workgroups of a row, joined by a second launch: several for up to 96 rows of 256 KB or
+// more, each over 16 KB or more of it and 768 in all, while one workgroup per row
+// leaves most CUs without work and takes longer for its row than the joining does.  us,
+// split / whole, bf16 with 5 alternatives: one row of 131072 9.1 / 14.8, 32 rows 10.8 / 15.3,
+// 64 rows 12.2 / 15.0 (7.4 / 11.6 with none, 16.6 / 16.2 with 20), 96 rows 13.3 / 15.2; but 128
+// rows 15.7 / 15.8, one row of 32000 8.4 / 7.4, 64 of 65536 10.6 / 10.3, and 93 of 50021 fp32
+// with 20 15.8 / 10.5.
 int row_splits(int dtype, long rows, int vocab) {
     const long chunks = chunk_count(dtype, vocab);
-    if (rows < 1 || rows > 32 || chunks < 8192) return 1;
-    return (int)std::min<long>(SPLIT_MAX, std::min(1024 / rows, chunks / 1024));
+    if (rows < 1 || rows > 96 || chunks < 16384) return 1;
+    return (int)std::min<long>(SPLIT_MAX, std::min(768 / rows, chunks / 1024));
 }
 // Threads of a workgroup.  Short rows take one wave, whose joins and rankings wait for
 // nobody; few rows, or rows over 128 KB, the most loads in flight; in between many rows

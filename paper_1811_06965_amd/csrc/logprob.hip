@@ -11,6 +11,7 @@ namespace {
 
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float NEVER = -1e30f;  // a logit down here is a mask's, its token cannot occur
+__host__ __device__ inline float lower_bound(float clip) { return -clip > NEVER ? -clip : NEVER; }
 constexpr int SPLIT_MAX = 32;    // workgroups of one row: at most the lanes of the wave that joins them
 
 // Sums of a row's terms around a reference logit r: with d = x - r, a = sum exp(scale d)
@@ -20,14 +21,20 @@ constexpr int SPLIT_MAX = 32;    // workgroups of one row: at most the lanes of 
 // so a term that vanishes adds no 0 inf.
 struct Part {
     float r, a, b;
+    // The same sums around another reference.  c2 = scale log2 e; f comes before the
+    // product with d, which alone could pass the largest float.
+    __device__ __forceinline__ Part around(float to, float c2) const {
+        const float d = r - to, f = __builtin_amdgcn_exp2f(d * c2), fa = a * f;
+        return {to, fa, __builtin_fmaf(fa, d, f * b)};
+    }
 };
 constexpr float NO_REF = -2e30f;  // below every reference
-// The parts of 64 lanes as one.  c2 = scale log2 e.
+// The parts of 64 lanes as one.
 __device__ __forceinline__ Part wave_join(Part p, float c2) {
     const float r = wave_reduce_f(p.r, NO_REF, [](float a, float b) { return max_nan(a, b); });
-    const float d = p.r - r, f = __builtin_amdgcn_exp2f(d * c2);
+    p = p.around(r, c2);
     auto add = [](float a, float b) { return a + b; };
-    return {r, wave_reduce_f(p.a * f, 0.f, add), wave_reduce_f(f * (p.b + p.a * d), 0.f, add)};
+    return {r, wave_reduce_f(p.a, 0.f, add), wave_reduce_f(p.b, 0.f, add)};
 }
 
 // The order of alternatives as integers: the code of a logit (larger first, a NaN
@@ -114,8 +121,8 @@ __device__ __forceinline__ void write_row(const RowOut& o, long row, Part p, con
 // reached by at least `top` logits, and only by logits of the groups whose largest
 // does: those groups' chunks are read a second time and what reaches the bound, a few
 // more than `top` logits, is ranked.  One wave finds the bound bit by bit from the
-// groups' largest, as coarse as OWNERS groups above it allow.  Where more than
-// OWNERS groups are equal at the bound, the logits above it come from
+// groups' largest, until a quarter more than `top` reach it.  Where more than
+// OWNERS groups do, equal at the last bit, the logits above it come from
 // the groups that have any, and those at it from the row's start on, until there are
 // enough.  A row with a NaN, or with more than CAND logits that reach the bound, goes
 // through its logits once per alternative instead.
@@ -254,7 +261,7 @@ __global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, in
     const T* zr = z + row * ld;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int chunks = V / N + (V % N ? 1 : 0), c0 = min(split * per, chunks), c1 = min(c0 + per, chunks);
-    const float c2 = scale * LOG2E, near = 8.f / c2, lo = CLIP ? -clip : NEVER, hi = CLIP ? clip : INFINITY;
+    const float c2 = scale * LOG2E, near = 8.f / c2, lo = CLIP ? lower_bound(clip) : NEVER, hi = CLIP ? clip : INFINITY;
     auto bounded = [&](float x) { return CLIP ? min_nan(max_nan(x, lo), hi) : max_nan(x, lo); };
 
     Part p = {NO_REF, 0.f, 0.f};
@@ -263,10 +270,7 @@ __global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, in
         float cm = x[0];
 #pragma unroll
         for (int e = 1; e < N; ++e) cm = max_nan(cm, x[e]);
-        if (!(cm <= p.r + near)) {  // NaN too
-            const float d = p.r - cm, f = __builtin_amdgcn_exp2f(d * c2);
-            p = {cm, p.a * f, f * (p.b + p.a * d)};
-        }
+        if (!(cm <= p.r + near)) p = p.around(cm, c2);  // NaN too
         if (TOP) most = max_nan(most, cm);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -527,8 +531,8 @@ gp_status launch_rows(const T* z, long rows, int V, long ld, const int* tokens, 
 #undef GP_ROWS
 #undef GP_ROWS_NT
     if (splits > 1)
-        klaunch(logprob_join_kernel<T>, (unsigned)rows, 64, 0, st, z, V, ld, tokens, scale, clipped ? -clip : NEVER,
-                clipped ? clip : INFINITY, out, top, splits, parts, lists);
+        klaunch(logprob_join_kernel<T>, (unsigned)rows, 64, 0, st, z, V, ld, tokens, scale,
+                clipped ? lower_bound(clip) : NEVER, clipped ? clip : INFINITY, out, top, splits, parts, lists);
     GP_LAUNCH_CHECK();
     return GP_OK;
 }

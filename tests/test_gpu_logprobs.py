@@ -164,6 +164,43 @@ def test_masks(ops, dtype, vocab, low):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("clip", [0.0, 1e29, 1e31, 3e38])
+def test_the_largest_values(ops, dtype, clip):
+    """Logits at both ends of their type beside ordinary ones and masks, unclipped and with clips past every mask."""
+    big = float(torch.finfo(DT[dtype]).max)
+    z = torch.zeros(5, 700)
+    z[0, 3], z[0, 5] = big, -big
+    z[1, 3:9] = big
+    z[2], z[2, 699] = -math.inf, -big
+    z[3], z[3, 2], z[3, 4] = -big, -1e28, 5.0
+    z[4, ::2], z[4, 1::4] = -math.inf, big
+    z = z.to(DT[dtype]).cuda()
+    tok = torch.tensor([3, 4, 699, 4, 1], dtype=torch.int32, device="cuda")
+    r = ops.token_logprobs(z, tok, clip=clip, top=6)
+    x = z.double().cpu()
+    x = x.clamp(-clip, clip) if clip else x
+    s = torch.where(x <= -1e30, -math.inf, x)
+    none = (s == -math.inf).all(1)
+    s = s - torch.where(none, 0.0, s.amax(1))[:, None]  # (the largest first: its logarithm is lost beside 1e38)
+    ref = torch.where(none[:, None], -math.inf, s - torch.where(none, 0.0, torch.logsumexp(s, 1))[:, None])
+    p = ref.exp()
+    h = -torch.where(p > 0, p * ref, 0.0).sum(1)
+    # sums of up to 700 equal terms: 2 (700 / 64 + 32) u, and the logarithm's rounding
+    assert torch.allclose(r.entropy.double().cpu(), h, rtol=0, atol=1e-5)
+    want = ref[torch.arange(5), tok.cpu().long()]
+    got = r.logp.double().cpu()
+    assert torch.equal(torch.isinf(got), torch.isinf(want))
+    fine = ~torch.isinf(want)
+    assert ((got - want)[fine].abs() <= 1e-5 + want[fine].abs() * U).all()
+    for i in range(5):
+        order = sorted(range(700), key=lambda v: (-max(float(x[i, v]), -1e30), v))[:6]
+        assert r.top_ids[i].tolist() == order, i
+    one = torch.ones(5, device="cuda")
+    dz = ops.token_logprobs_backward(z, tok, r.lse, r.entropy, one, one, clip=clip)
+    assert not dz.isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("vocab", [9, 5000, 70001])
 def test_special_values_and_tokens(ops, dtype, vocab):
     _, z, tok = make(8, vocab, 0, dtype, 3 + vocab)

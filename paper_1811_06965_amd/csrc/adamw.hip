@@ -90,8 +90,10 @@ __device__ __forceinline__ unsigned largest_bits(f32x4 x) {
 }
 __device__ __forceinline__ void block_scale(float top, float& scale, float& inv) {
     const bool tiny = top < 0x1p-100f;
+    // 1 / top rounded to nearest: the device's reciprocal, off by up to a step, and one correction
+    const float r = __builtin_amdgcn_rcpf(top), one_over = __builtin_fmaf(__builtin_fmaf(-top, r, 1.f), r, r);
     scale = tiny ? 0.f : top * (1.f / 448.f);
-    inv = tiny ? 0.f : 1.f / top * 448.f;
+    inv = tiny ? 0.f : one_over * 448.f;
 }
 // The bits of |x| inv 2^-120, inv the block's: 2^-120 brings the e4m3 exponents (and zero
 // and the subnormals) to those of fp32, whose bits 20 and up are then the code.
@@ -189,8 +191,8 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
         };
         if (tm < 0x1p13f && tr < 0x1p13f)
             codes(std::true_type{}, im * 0x1p-120f, ir * 0x1p-120f);
-        else
-            codes(std::false_type{}, im, ir);
+        else  // (a reciprocal that could be subnormal takes the whole division)
+            codes(std::false_type{}, tm < 0x1p-100f ? 0.f : 1.f / tm * 448.f, tr < 0x1p-100f ? 0.f : 1.f / tr * 448.f);
         Codes::store(T.m, i, T.n, whole, __builtin_bit_cast(Codes::vec, qm));
         Codes::store(T.v, i, T.n, whole, __builtin_bit_cast(Codes::vec, qr));
         if ((threadIdx.x & 63) == 0) {

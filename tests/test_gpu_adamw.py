@@ -318,6 +318,21 @@ def test_special_gradients(ops):
             assert opt.m_scale[0][3] == 0.0 and bool((opt.m[0].view(torch.uint8)[768:] == 0).all())
 
 
+@pytest.mark.parametrize("top", [1e-29, 1e-20, 1.0, 8191.0, 8193.0, 1e18, 3e38])
+def test_blocks_of_every_magnitude(ops, top):
+    """8-bit first moments from the smallest block that is kept to the largest floats: each value within a step of
+    e4m3 (an eighth of it, or 2^-9 of the block's 448th), the block's largest exact."""
+    g = torch.linspace(-1, 1, 1024, device="cuda") * top
+    p = torch.zeros(1024, device="cuda")
+    opt = ops.AdamW([p], [g], state_bits=8, betas=(0.0, 0.5), lr=0.0)
+    opt.step()
+    m = (opt.m[0].double().view(-1, 256) * opt.m_scale[0].double()[:, None]).view(-1)
+    step = (g.double().abs() / 8).clamp(min=0) + opt.m_scale[0].double().repeat_interleave(256) * 2.0 ** -9
+    assert bool(((m - g.double()).abs() <= step).all())
+    most = g.view(-1, 256).abs().amax(1).double()
+    assert bool(((m.view(-1, 256).abs().amax(1) / most - 1).abs() < 1e-6).all())
+
+
 def test_random_rounding_keeps_small_changes(ops):
     """A constant gradient g of 1: v grows by a thousandth of what is left each step, a tenth of what rounding to
     nearest in e4m3 would need to see.  After 400 steps from v = 0.01 the mean root over many elements is that of the

@@ -202,6 +202,10 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
     }
 }
 
+// A workgroup per chunk of 4096 elements, whose loads all come before their first use.
+// Bound by HBM: 336M fp32 parameters with bf16 copies 1.90 ms (10.1 GB, 5.3 TB/s); 336M bf16
+// with 8-bit states 620 us (3.4 GB, 5.45 TB/s), where the 65 vector instructions a value
+// are near their limit too (1.8 times as many took 920 us).
 template <typename P, typename G, int BITS>
 __global__ void __launch_bounds__(256) adamw_kernel(const AdamwBatch b, const AdamwScalars s) {
     AdamwStep st;
@@ -247,6 +251,9 @@ struct NormBatch {
     NormTensor t[NORM_BATCH];
 };
 
+// Bound by HBM: 336M fp32 gradients 243 us (1.34 GB, 5.5 TB/s), four loads ahead of their
+// use; a conversion and a product-sum in fp64 per value, which the vector units do at half
+// their fp32 rate, stay hidden.
 template <typename G>
 __global__ void __launch_bounds__(256) norm_kernel(const NormBatch b, long chunk, double* __restrict__ partial) {
     __shared__ double red[4];

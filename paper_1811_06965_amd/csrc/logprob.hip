@@ -247,7 +247,11 @@ __device__ __forceinline__ void find_top(TopShared<NT>& sh, const T* zr, int V, 
 }
 
 // A workgroup of NT threads per row, or `splits` of them, each over `per` chunks of it;
-// thread t takes the chunks t, t + NT, ..
+// thread t takes the chunks t, t + NT, .., four loads ahead of their use (eight made
+// long rows 3% slower).  Bound by HBM where rows are many: 1024 rows of 32000 bf16
+// 14.0 us (4.7 TB/s, the launch included), 4096 of 128000 with 8 alternatives 191 us (5.5
+// TB/s), close to what its 11 vector instructions a logit take; for few rows by the chain
+// of reductions: one row of 32000 4.4 us, with 5 alternatives 7.4.
 template <typename T, bool CLIP, bool TOP, int NT>
 __global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, int V, long ld,
                                                      const int* __restrict__ tokens, float scale, float clip, RowOut out,
@@ -340,6 +344,7 @@ __global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, in
 
 // The parts of a row's splits joined by one wave, lane s taking split s; its list of
 // alternatives is sorted, so the next one is always the largest of the lists' heads.
+// 2 us, and 0.15 us per alternative.
 template <typename T>
 __global__ void __launch_bounds__(64) logprob_join_kernel(const T* __restrict__ z, int V, long ld,
                                                           const int* __restrict__ tokens, float scale, float lo, float hi,
@@ -369,7 +374,9 @@ __global__ void __launch_bounds__(64) logprob_join_kernel(const T* __restrict__ 
 
 // The gradient: with d = s - lse, dz = -p (A + B d) + [v = t] scale a,
 // A = scale (a + b H), B = scale b.  d is held above -200, where p is 0 and the product
-// with it finite.
+// with it finite.  Rows are split until there are 4096 workgroups or 512 chunks in each.  Bound by
+// HBM: 1024 rows of 32000 bf16 24 us (131 MB, 5.45 TB/s), 93 rows of 50021 fp32 between
+// strides of 50048 and 50021 7.7 us (4.8 TB/s).
 template <typename T, bool CLIP>
 __global__ void __launch_bounds__(256) logprob_grad_kernel(const T* z, int V, long ld, const int* __restrict__ tokens,
                                                            float scale, float clip, const float* __restrict__ lse,

@@ -179,8 +179,23 @@ gp_status gp_set_param(gp_partition* p, int layer, int id, const float* host, si
 gp_status gp_get_param(gp_partition* p, int layer, int id, float* host, size_t count);
 gp_status gp_get_grad(gp_partition* p, int layer, int id, float* host, size_t count);
 
+/*
+ * The optimizer's state, for checkpoints: a moment of one parameter tensor, in the
+ * layout of gp_get_param (which = 1: AdamW's first moment; 2: its second, or RMSProp's
+ * running mean square), and the number of updates that AdamW has done.  A
+ * partition that takes parameters, moments and updates of another continues as that
+ * one would, bit for bit.  These calls synchronise the device.
+ * GP_ERR_INVALID_ARG: as gp_get_param; a moment or count that the optimizer does not
+ *   hold; updates < 0.
+ * GP_ERR_STATE: not configured, or a set inside a mini-batch.
+ */
+gp_status gp_get_moment(gp_partition* p, int layer, int id, int which, float* host, size_t count);
+gp_status gp_set_moment(gp_partition* p, int layer, int id, int which, const float* host, size_t count);
+gp_status gp_get_updates(gp_partition* p, long long* updates);
+gp_status gp_set_updates(gp_partition* p, long long updates);
+
 /* Bytes held in device memory for parameters (masters, working copies and,
- * with RMSProp, the running mean squares), gradient accumulators, the
+ * with RMSProp and AdamW, the moments), gradient accumulators, the
  * boundary stash, and all workspaces.  Any pointer
  * may be NULL.  Requires a configured partition. */
 gp_status gp_partition_memory(gp_partition* p, size_t* params, size_t* grads, size_t* stash,

@@ -35,6 +35,8 @@ struct AdamwBatch {
     int chunk0[BATCH];  // chunks of the launch's tensors before each
     AdamwTensor t[BATCH];
 };
+static_assert(sizeof(AdamwBatch) + sizeof(AdamwScalars) <= 4096, "kernel arguments");
+
 // The last of n tensors whose first chunk is not after id.
 template <int MOST> __device__ __forceinline__ int tensor_of(const int (&chunk0)[MOST], int n, int id) {
     int l = -1;

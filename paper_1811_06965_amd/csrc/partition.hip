@@ -1874,6 +1874,53 @@ static gp_status param_io(gp_partition* p, int layer, int id, float* host, size_
     return GP_OK;
 }
 
+// A moment of one parameter tensor: to the partition (set) or from it.
+static gp_status moment_io(gp_partition* p, int layer, int id, int which, float* host, size_t count, bool set) {
+    if (!p || !host) return set_error(GP_ERR_INVALID_ARG, "partition and host buffer must not be NULL");
+    std::string msg;
+    if (!p->sched.configured()) return set_error(GP_ERR_STATE, "partition not configured");
+    gp_status s = set ? p->sched.can_set_param(msg) : GP_OK;
+    if (s != GP_OK) return set_error(s, msg.c_str());
+    float* base = which == 1 ? p->opt_m : which == 2 ? p->opt_ms : nullptr;
+    if (!base) return set_error(GP_ERR_INVALID_ARG, "the partition's optimizer holds no such moment");
+    ParamRef r;
+    s = resolve_param(p->plan, p->d, layer, id, r, msg);
+    if (s != GP_OK) return set_error(s, msg.c_str());
+    if (count != (size_t)r.rows * r.cols) return set_error(GP_ERR_INVALID_ARG, "count does not match the parameter's size");
+    GP_HIP(hipDeviceSynchronize());
+    float* dev = base + r.off;
+    const size_t row = (size_t)r.cols * 4, ld = (size_t)r.ld * 4;
+    GP_HIP(set ? hipMemcpy2D(dev, ld, host, row, row, r.rows, hipMemcpyHostToDevice)
+               : hipMemcpy2D(host, row, dev, ld, row, r.rows, hipMemcpyDeviceToHost));
+    GP_HIP(hipDeviceSynchronize());
+    return GP_OK;
+}
+
+gp_status gp_get_moment(gp_partition* p, int layer, int id, int which, float* host, size_t count) {
+    return moment_io(p, layer, id, which, host, count, false);
+}
+gp_status gp_set_moment(gp_partition* p, int layer, int id, int which, const float* host, size_t count) {
+    return moment_io(p, layer, id, which, const_cast<float*>(host), count, true);
+}
+
+static gp_status updates_io(gp_partition* p, long long* updates, bool set) {
+    if (!p || !updates || (set && *updates < 0))
+        return set_error(GP_ERR_INVALID_ARG, "partition and updates must not be NULL, updates not negative");
+    std::string msg;
+    if (!p->sched.configured()) return set_error(GP_ERR_STATE, "partition not configured");
+    const gp_status s = set ? p->sched.can_set_param(msg) : GP_OK;
+    if (s != GP_OK) return set_error(s, msg.c_str());
+    if (!p->opt_step) return set_error(GP_ERR_INVALID_ARG, "only AdamW counts its updates");
+    GP_HIP(hipDeviceSynchronize());
+    GP_HIP(set ? hipMemcpy(p->opt_step, updates, sizeof *updates, hipMemcpyHostToDevice)
+               : hipMemcpy(updates, p->opt_step, sizeof *updates, hipMemcpyDeviceToHost));
+    GP_HIP(hipDeviceSynchronize());
+    return GP_OK;
+}
+
+gp_status gp_get_updates(gp_partition* p, long long* updates) { return updates_io(p, updates, false); }
+gp_status gp_set_updates(gp_partition* p, long long updates) { return updates_io(p, &updates, true); }
+
 gp_status gp_set_param(gp_partition* p, int layer, int id, const float* host, size_t count) {
     return param_io(p, layer, id, const_cast<float*>(host), count, 0);
 }

@@ -42,7 +42,8 @@ EXPORTS = ["gp_partition_create", "gp_partition_configure", "gp_partition_destro
            "gp_forward_microbatch_noalloc", "gp_plan_cells", "gp_stream_create", "gp_stream_destroy",
            "gp_token_logprobs", "gp_token_logprobs_workspace", "gp_token_logprobs_backward", "gp_grad_norm",
            "gp_grad_norm_workspace", "gp_adamw_step", "gp_get_grad_norm", "gp_score_sequences",
-           "gp_backward_microbatch_weighted", "gp_last_error"]
+           "gp_backward_microbatch_weighted", "gp_get_moment", "gp_set_moment", "gp_get_updates", "gp_set_updates",
+           "gp_last_error"]
 
 GP_TOP_MAX, GP_NO_TOKEN, GP_STATE_BLOCK = 32, -1, 256
 
@@ -98,6 +99,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.gp_partition_destroy.argtypes = [P]
     for f in (lib.gp_set_param, lib.gp_get_param, lib.gp_get_grad):
         f.argtypes = [P, I, I, FP, SZ]
+    for f in (lib.gp_get_moment, lib.gp_set_moment):
+        f.argtypes = [P, I, I, I, FP, SZ]
+    lib.gp_get_updates.argtypes = [P, ctypes.POINTER(ctypes.c_longlong)]
+    lib.gp_set_updates.argtypes = [P, ctypes.c_longlong]
     lib.gp_partition_memory.argtypes = [P] + [ctypes.POINTER(SZ)] * 4
     lib.gp_param_count.argtypes = [P, ctypes.POINTER(SZ)]
     lib.gp_forward_microbatch.argtypes = [P, I, VP, VP, VP, VP]
@@ -175,6 +180,25 @@ def gp_get_param(h, layer, pid, host):
 
 def gp_get_grad(h, layer, pid, host):
     _check(load().gp_get_grad(h, layer, pid, _fptr(host), host.size))
+
+
+def gp_get_moment(h, layer, pid, which, host):
+    _check(load().gp_get_moment(h, layer, pid, which, _fptr(host), host.size))
+
+
+def gp_set_moment(h, layer, pid, which, host):
+    """host: C-contiguous float32 numpy array."""
+    _check(load().gp_set_moment(h, layer, pid, which, _fptr(host), host.size))
+
+
+def gp_get_updates(h):
+    v = ctypes.c_longlong()
+    _check(load().gp_get_updates(h, ctypes.byref(v)))
+    return v.value
+
+
+def gp_set_updates(h, updates):
+    _check(load().gp_set_updates(h, updates))
 
 
 def gp_partition_memory(h):

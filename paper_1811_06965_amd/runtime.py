@@ -120,6 +120,27 @@ class Partition:
     def params(self):
         return self._read(gp.gp_get_param, self.cfg.param_shapes(), self.cfg.head_shapes())
 
+    def optimizer_state(self):
+        """AdamW's (updates, first moments, second moments) or RMSProp's (0, None,
+        mean squares), each moment a (layers, head) pair like params()."""
+        def read(which):
+            return self._read(lambda h, l, pid, a: gp.gp_get_moment(h, l, pid, which, a), self.cfg.param_shapes(),
+                              self.cfg.head_shapes())
+        adamw = self.cfg.optimizer == "adamw"
+        return gp.gp_get_updates(self.h) if adamw else 0, read(1) if adamw else None, read(2)
+
+    def load_optimizer_state(self, state):
+        """What optimizer_state() gave, of a partition of the same configuration."""
+        updates, *moments = state
+        for which, pair in enumerate(moments, 1):
+            if pair is None:
+                continue
+            for l, tensors in [*enumerate(pair[0]), (-1, pair[1])]:
+                for name, arr in tensors.items():
+                    gp.gp_set_moment(self.h, l, gp.PARAM_ID[name], which, np.ascontiguousarray(arr, dtype=np.float32))
+        if self.cfg.optimizer == "adamw":
+            gp.gp_set_updates(self.h, updates)
+
     def memory(self):
         return gp.gp_partition_memory(self.h)
 

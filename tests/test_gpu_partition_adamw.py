@@ -233,6 +233,45 @@ def test_memory_and_refusals():
             gp.gp_accumulate_and_step(a.h, 0.0, False, torch.cuda.current_stream().cuda_stream)  # the step is still owed
 
 
+@pytest.mark.parametrize("cfg", [TINY.with_(**ADAMW), ENC.with_(**ADAMW, max_grad_norm=0.05),
+                                 DEC_BF16.with_(optimizer="rmsprop", rms_eps=1e-8)], ids=["tiny", "enc", "rmsprop"])
+def test_resume_with_the_optimizer_state(cfg):
+    """Two steps, everything read, a new partition that takes it, two more: the bits of four steps in one."""
+    from paper_1811_06965_amd import gp
+    from paper_1811_06965_amd.runtime import Partition
+    case = synth.make_case(cfg, 38, perturb=True)
+    with Partition(cfg) as part:
+        part.load_params(case["layers"], case["head"])
+        inp = part.device_inputs(case)
+        for k in range(4):
+            if k == 2:
+                mid, state = part.params(), part.optimizer_state()
+            part.step(inp["x"], inp["mem"], inp["dy"], lr=1e-3)
+        want, end = tensors(part.params()), part.optimizer_state()
+    with Partition(cfg) as part:
+        part.load_params(*mid)
+        part.load_optimizer_state(state)
+        inp = part.device_inputs(case)
+        for _ in range(2):
+            part.step(inp["x"], inp["mem"], inp["dy"], lr=1e-3)
+        assert all(np.array_equal(a, b) for (_, a), (_, b) in zip(want, tensors(part.params())))
+        got = part.optimizer_state()
+        assert got[0] == end[0] == (4 if cfg.optimizer == "adamw" else 0)
+        for a, b in zip(end[1:], got[1:]):
+            assert (a is None and b is None) or all(np.array_equal(x, y) for (_, x), (_, y) in zip(tensors(a), tensors(b)))
+        assert max(np.abs(x).max() for _, x in tensors(got[2])) > 0
+        host = np.zeros(3, dtype=np.float32)
+        bad = [lambda: gp.gp_get_moment(part.h, 0, gp.PARAM_ID["bq"], 2, host), lambda: gp.gp_set_updates(part.h, -1),
+               lambda: gp.gp_get_moment(part.h, 0, gp.PARAM_ID["bq"], 3, host),
+               lambda: gp.gp_set_moment(part.h, 99, 0, 2, host)]
+        if cfg.optimizer == "rmsprop":
+            bad += [lambda: gp.gp_get_updates(part.h), lambda: gp.gp_get_moment(part.h, 0, 0, 1, host)]
+        for f in bad:
+            with pytest.raises(gp.GpError) as err:
+                f()
+            assert err.value.status == gp.GP_ERR_INVALID_ARG
+
+
 # -------------------------------------------------------------------- scoring
 def oracle_scores(cfg, case, sl):
     from oracle import gpipe, transformer as tf

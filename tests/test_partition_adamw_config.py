@@ -69,6 +69,12 @@ def test_null_partitions(gp):
     assert back(h, 0, 64, None, None, None, None, None) == 1  # neither weight
     assert back(h, 0, 64, 66, None, None, None, None) == 1    # misaligned
     assert back(h, 0, 64, 64, None, None, None, None) == gp.GP_ERR_STATE
+    n = ctypes.c_longlong()
+    host = (ctypes.c_float * 4)()
+    for call in (lambda q: lib.gp_get_moment(q, 0, 0, 1, host, 4), lambda q: lib.gp_set_moment(q, 0, 0, 1, host, 4),
+                 lambda q: lib.gp_get_updates(q, ctypes.byref(n)), lambda q: lib.gp_set_updates(q, 1)):
+        assert call(None) == 1 and call(h) == gp.GP_ERR_STATE
+    assert lib.gp_get_updates(h, None) == 1 and lib.gp_get_moment(h, 0, 0, 1, None, 4) == 1
     gp.gp_partition_destroy(h)
 
 

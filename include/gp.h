@@ -515,7 +515,7 @@ gp_status gp_token_logprobs_workspace(int dtype, long rows, int vocab, int top, 
  * (the bracket only with clip > 0).  dlogp and dentropy: device fp32 [rows];
  * either may be NULL, and then tokens or entropy may be.  A row whose token is
  * GP_NO_TOKEN takes dlogp as 0, a row with lse = -inf has a zero gradient, a token
- * outside [0, vocab) gives a row of NaN.
+ * outside [0, vocab) gives a row of NaN.  A p below 2^-126 counts as 0.
  *   dlogits : device [rows, vocab] in dtype, rows ldd apart; may be logits itself
  *             (with ldd = ld), and must not overlap it otherwise.  The ldd - vocab
  *             elements behind a row are left as they were.

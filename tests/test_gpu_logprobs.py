@@ -315,7 +315,9 @@ def check_backward(ops, buf, z, tok, scale, clip, seed, use=(True, True), inplac
             want = np.where(np.abs(raw) <= clip, want, 0.0)
         mag = np.where(s == -np.inf, 0.0, np.abs(s)) + np.where(np.isfinite(lv), np.abs(lv), 0.0)
         terms = p * (np.abs(av) + np.abs(bv) * (np.abs(d) + np.abs(hv) + 1))
-        tol = scale * (terms * (4 * mag + 16) * U + np.abs(av) * one * 8 * U)
+        # a probability below the smallest normal float, 2^-126, counts as 0
+        flush = 2.0 ** -126 * (np.abs(av) + np.abs(bv) * (np.abs(d) + np.abs(hv)))
+        tol = scale * (terms * (4 * mag + 16) * U + np.abs(av) * one * 8 * U + flush)
     half = 2.0 ** -8 if z.dtype == torch.bfloat16 else U
     # below the normal range a step is 2^-133 (bf16) or 2^-149
     tol = tol * (1 + half) + np.abs(want) * half + 2.0 ** (-133 if z.dtype == torch.bfloat16 else -126)

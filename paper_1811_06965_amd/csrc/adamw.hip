@@ -283,6 +283,14 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormBatch b, long chunk
     if (threadIdx.x == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// The norm and the factor that clips it.
+__device__ __forceinline__ void write_norm(double sum, float max_norm, float* __restrict__ out) {
+    const double norm = sqrt(sum);
+    const double f = norm > (double)max_norm ? (double)max_norm / norm : 1.0;
+    out[0] = (float)norm;
+    out[1] = isfinite(norm) ? (float)f : NAN;
+}
+
 __global__ void __launch_bounds__(256) norm_finish_kernel(const double* __restrict__ partial, int n, float max_norm,
                                                           float* __restrict__ out) {
     __shared__ double red[4];
@@ -291,11 +299,51 @@ __global__ void __launch_bounds__(256) norm_finish_kernel(const double* __restri
     s = wave_sum_d(s);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
+    if (threadIdx.x == 0) write_norm((red[0] + red[1]) + (red[2] + red[3]), max_norm, out);
+}
+
+// The whole of a short list in one workgroup and launch: wave w takes the chunks w, w + 16,
+// .. of SMALL_CHUNK elements.  A wave's chunks are a chain of reads, so it is for lists whose
+// second launch costs the host more than that: up to SMALL_CHUNKS chunks.  us a call, so /
+// in two launches: one tensor of 100 7.2 / 9.4, of 100000 6.6 / 9.4, 32 of 1000 6.8 / 9.3, 100 of 64
+// 8.5 / 9.5, 100 of 1000 10.4 / 9.7; past the limit, 160 chunks, 8.6 to 9.9 / 9.2.
+constexpr int SMALL_CHUNK = 1024, SMALL_CHUNKS = 120;
+template <typename G>
+__global__ void __launch_bounds__(1024) norm_small_kernel(const NormBatch b, int chunks, float max_norm,
+                                                          float* __restrict__ out) {
+    __shared__ double red[16];
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    double s = 0.0;
+    for (int id = w; id < chunks; id += 16) {
+        const int at = tensor_of(b.chunk0, b.n, id);
+        const NormTensor& T = b.t[at];
+        const long base = (long)(id - b.chunk0[at]) * SMALL_CHUNK, i = base + lane * 4;
+        constexpr int U = SMALL_CHUNK / 256;
+        typename Four<G>::vec x[U];
+        if (base + SMALL_CHUNK <= T.n) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = Four<G>::load(T.g, i + u * 256, T.n, true);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                x[u] = typename Four<G>::vec{};
+                if (base + u * 256 < T.n) x[u] = Four<G>::load(T.g, i + u * 256, T.n, i + u * 256 + 4 <= T.n);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const f32x4 v = Four<G>::values(x[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
+        }
+    }
+    s = wave_sum_d(s);
+    if (lane == 0) red[w] = s;
+    __syncthreads();
     if (threadIdx.x == 0) {
-        const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3]));
-        const double f = norm > (double)max_norm ? (double)max_norm / norm : 1.0;
-        out[0] = (float)norm;
-        out[1] = isfinite(norm) ? (float)f : NAN;
+        double t = red[0];
+        for (int i = 1; i < 16; ++i) t += red[i];
+        write_norm(t, max_norm, out);
     }
 }
 
@@ -432,6 +480,26 @@ gp_status gp_grad_norm(int dtype, const gp_grad_tensor* grads, int n, float max_
         total += grads[i].count;
     }
     hipStream_t st = (hipStream_t)stream;
+    long small = 0;  // chunks, if the list is short enough for one workgroup
+    for (int i = 0; i < n && n <= NORM_BATCH && small <= SMALL_CHUNKS; ++i)
+        small += (long)((grads[i].count + SMALL_CHUNK - 1) / SMALL_CHUNK);
+    if (n <= NORM_BATCH && small <= SMALL_CHUNKS) {
+        NormBatch b;
+        b.n = 0;
+        int chunks = 0;
+        for (int i = 0; i < n; ++i) {
+            if (grads[i].count == 0) continue;
+            b.chunk0[b.n] = chunks;
+            b.t[b.n++] = {grads[i].grad, (long)grads[i].count};
+            chunks += (int)((grads[i].count + SMALL_CHUNK - 1) / SMALL_CHUNK);
+        }
+        if (dtype == GP_BF16)
+            klaunch(norm_small_kernel<bf16>, 1, 1024, 0, st, b, chunks, max_norm, norm_factor);
+        else
+            klaunch(norm_small_kernel<float>, 1, 1024, 0, st, b, chunks, max_norm, norm_factor);
+        GP_LAUNCH_CHECK();
+        return GP_OK;
+    }
     // chunks of one size, so many that a tensor's last one is the only short one
     const long chunk = std::max<long>(4096, (long)((total / NORM_BLOCKS + 4096) / 4096 * 4096));
     double* partial = static_cast<double*>(ws);

@@ -365,7 +365,9 @@ def test_random_rounding_keeps_small_changes(ops):
 
 # -------------------------------------------------------------- gradient norm
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("sizes", [[1], [3, 0, 5], SIZES, [7 * i % 97 for i in range(300)], [9000001, 17, 4096]])
+@pytest.mark.parametrize("sizes", [[1], [3, 0, 5], SIZES, [7 * i % 97 for i in range(300)], [9000001, 17, 4096],
+                                   [120 * 1024], [120 * 1024 + 1], [1023, 1024, 1025] * 29, [3] * 120, [3] * 121,
+                                   [0, 5] * 64, [0, 5] * 65])
 @pytest.mark.parametrize("offset", [0, 1])
 def test_grad_norm(ops, dtype, sizes, offset):
     """Squares are summed in fp64, so the norm is rounded once to fp32: u of it, and the factor twice."""

@@ -306,7 +306,8 @@ __global__ void __launch_bounds__(256) norm_finish_kernel(const double* __restri
 // .. of SMALL_CHUNK elements.  A wave's chunks are a chain of reads, so it is for lists whose
 // second launch costs the host more than that: up to SMALL_CHUNKS chunks.  us a call, so /
 // in two launches: one tensor of 100 7.2 / 9.4, of 100000 6.6 / 9.4, 32 of 1000 6.8 / 9.3, 100 of 64
-// 8.5 / 9.5, 100 of 1000 10.4 / 9.7; past the limit, 160 chunks, 8.6 to 9.9 / 9.2.
+// 8.5 / 9.5, and the one loss within the limit, 100 of 1000, 10.4 / 9.7; past it, 160 chunks, 8.6 to
+// 9.9 / 9.2.
 constexpr int SMALL_CHUNK = 1024, SMALL_CHUNKS = 120;
 template <typename G>
 __global__ void __launch_bounds__(1024) norm_small_kernel(const NormBatch b, int chunks, float max_norm,

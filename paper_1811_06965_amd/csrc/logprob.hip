@@ -469,15 +469,18 @@ int row_splits(int dtype, long rows, int vocab) {
     return (int)std::min<long>(SPLIT_MAX, std::min(768 / rows, chunks / 1024));
 }
 // Threads of a workgroup.  Short rows take one wave, whose joins and rankings wait for
-// nobody; few rows, or rows over 128 KB, the most loads in flight; in between many rows
+// nobody; few rows, or rows over 128 KB, the most loads in flight, from 32 KB a row on where
+// a CU has one row at most, else from 50 KB on; in between many rows
 // share a CU, and alternatives are ranked faster by more threads.  us at 64 / 256 / 512 / 1024
 // threads: 4096 x 1000 bf16 with 5 alternatives 8.6 / 15.1 / 24.7 / 42.6; 3000 x 4111
 // with 1 12.4 / 15.3 / 23.3 / 36.3; 512 x 9000 fp32 with 20 18.0 / 7.8 / 8.1 / 9.3; 93 x
 // 50021 fp32 with 20 69 / 15.7 / 11.7 / 10.6; 1024 x 32000 bf16 20.2 / 14.4 / 14.5 / 15.7,
-// with 20 46 / 20.0 / 19.1 / 23.0; 4096 x 128000 with 8 319 / 216 / 191 / 193.
+// with 20 46 / 20.0 / 19.1 / 23.0; 4096 x 128000 with 8 319 / 216 / 191 / 193.  At 256 / 1024
+// threads, bf16 with 20: 256 x 14000 8.0 / 8.1, 256 x 21000 9.3 / 8.5; 512 x 24000 11.4 / 11.8,
+// 512 x 27000 12.6 / 12.2.
 int row_threads(long rows, int chunks, int splits, int top) {
     if (chunks <= 256 || (chunks <= 1024 && rows >= 1024)) return 64;
-    if (splits > 1 || chunks <= 3072) return 256;
+    if (splits > 1 || chunks <= (rows <= 256 ? 2048 : 3200)) return 256;
     if (rows < 768 || chunks > 8192) return 1024;
     return top ? 512 : 256;
 }

@@ -116,6 +116,12 @@ template <> struct Vec16<float> {
         if (e_ != hipSuccess) return ::gp::hip_fail(e_, __FILE__, __LINE__); \
     } while (0)
 
+#define GP_TRY(x)                    \
+    do {                             \
+        gp_status s_ = (x);          \
+        if (s_ != GP_OK) return s_;  \
+    } while (0)
+
 #define GP_HIP(call)                                                        \
     do {                                                                    \
         hipError_t e_ = (call);                                             \

@@ -501,6 +501,12 @@ gp_status check_rows(int dtype, const void* logits, long rows, int vocab, long l
     return GP_OK;
 }
 
+// Rows of a launch at most: a launch holds fewer than 2^32 threads, a workgroup of a row
+// up to 1024 of them.
+constexpr long LAUNCH_ROWS = 1L << 21;
+
+template <typename P> P* past(P* p, long n) { return p ? p + n : nullptr; }
+
 template <typename T>
 gp_status launch_rows(const T* z, long rows, int V, long ld, const int* tokens, float scale, float clip,
                       const RowOut& out, int top, void* ws, size_t ws_bytes, hipStream_t st) {
@@ -595,12 +601,18 @@ gp_status gp_token_logprobs(int dtype, const void* logits, long rows, int vocab,
         if (!aligned(p, 4)) return bad("token_logprobs: a misaligned address");
     if (!aligned(ws, 16)) return bad("token_logprobs: the workspace must be 16-byte aligned");
     if (rows == 0) return GP_OK;
-    const RowOut out = {logp, lse, entropy, top_ids, top_logp};
-    if (dtype == GP_BF16)
-        return launch_rows(static_cast<const bf16*>(logits), rows, vocab, ld, tokens, scale, clip, out, top, ws, ws_bytes,
-                           (hipStream_t)stream);
-    return launch_rows(static_cast<const float*>(logits), rows, vocab, ld, tokens, scale, clip, out, top, ws, ws_bytes,
-                       (hipStream_t)stream);
+    for (long r = 0; r < rows; r += LAUNCH_ROWS) {
+        const long n = std::min(LAUNCH_ROWS, rows - r);
+        const RowOut out = {past(logp, r), past(lse, r), past(entropy, r), past(top_ids, r * top), past(top_logp, r * top)};
+        const int* t = past(tokens, r);
+        if (dtype == GP_BF16)
+            GP_TRY(launch_rows(static_cast<const bf16*>(logits) + r * ld, n, vocab, ld, t, scale, clip, out, top, ws,
+                               ws_bytes, (hipStream_t)stream));
+        else
+            GP_TRY(launch_rows(static_cast<const float*>(logits) + r * ld, n, vocab, ld, t, scale, clip, out, top, ws,
+                               ws_bytes, (hipStream_t)stream));
+    }
+    return GP_OK;
 }
 
 gp_status gp_token_logprobs_backward(int dtype, const void* logits, long rows, int vocab, long ld, const int* tokens,
@@ -625,11 +637,18 @@ gp_status gp_token_logprobs_backward(int dtype, const void* logits, long rows, i
     const uintptr_t z1 = z0 + ((size_t)(rows - 1) * ld + vocab) * es, d1 = d0 + ((size_t)(rows - 1) * ldd + vocab) * es;
     if (!(z0 == d0 && ld == ldd) && z0 < d1 && d0 < z1)
         return bad("token_logprobs_backward: dlogits overlaps the logits without being them");
-    if (dtype == GP_BF16)
-        return launch_grad(static_cast<const bf16*>(logits), rows, vocab, ld, tokens, scale, clip, lse, entropy, dlogp,
-                           dentropy, static_cast<bf16*>(dlogits), ldd, (hipStream_t)stream);
-    return launch_grad(static_cast<const float*>(logits), rows, vocab, ld, tokens, scale, clip, lse, entropy, dlogp,
-                       dentropy, static_cast<float*>(dlogits), ldd, (hipStream_t)stream);
+    for (long r = 0; r < rows; r += LAUNCH_ROWS) {
+        const long n = std::min(LAUNCH_ROWS, rows - r);
+        const int* t = past(tokens, r);
+        const float *h = past(entropy, r), *a = past(dlogp, r), *b = past(dentropy, r);
+        if (dtype == GP_BF16)
+            GP_TRY(launch_grad(static_cast<const bf16*>(logits) + r * ld, n, vocab, ld, t, scale, clip, lse + r, h, a, b,
+                               static_cast<bf16*>(dlogits) + r * ldd, ldd, (hipStream_t)stream));
+        else
+            GP_TRY(launch_grad(static_cast<const float*>(logits) + r * ld, n, vocab, ld, t, scale, clip, lse + r, h, a, b,
+                               static_cast<float*>(dlogits) + r * ldd, ldd, (hipStream_t)stream));
+    }
+    return GP_OK;
 }
 
 } // extern "C"

@@ -747,12 +747,6 @@ Ctx make_ctx(gp_partition* p, hipStream_t st, Lane lane = Lane::Main) {
     return c;
 }
 
-#define GP_TRY(x)                    \
-    do {                             \
-        gp_status s_ = (x);          \
-        if (s_ != GP_OK) return s_;  \
-    } while (0)
-
 // A role's algorithmic work in a launch.
 struct RoleWork {
     int role;

@@ -280,6 +280,29 @@ def test_rows_past_32_bits(ops):
     assert (sums.abs() < 1e-2).all() and float(dz[-1, int(tok[-1])]) > 0.9
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_rows_than_a_launch_holds(ops, dtype):
+    """More workgroups than one launch can have, 64 threads of the forward's and 256 of the
+    gradient's each: every row, the last ones and those at a launch's seam too."""
+    rows, vocab = 2 ** 26 + 5, 3
+    z = torch.empty(rows, vocab, dtype=DT[dtype], device="cuda")
+    z.copy_(torch.arange(rows * vocab, device="cuda", dtype=torch.int32).view(rows, vocab).remainder_(61).sub_(30))
+    tok = torch.arange(rows, dtype=torch.int32, device="cuda").remainder_(3)
+    r = ops.token_logprobs(z, tok, scale=0.1, top=2)
+    one = torch.ones(rows, device="cuda")
+    dz = ops.token_logprobs_backward(z, tok, r.lse, r.entropy, one, one, scale=0.1)
+    # every row is one of 61 * 3 (the first value's remainder by 61, the token's by 3), to the bit
+    for got in (r.logp, r.entropy, r.top_ids, r.top_logp, dz):
+        whole = got[:rows // 183 * 183].view(-1, 183, *got.shape[1:])
+        assert bool((whole == whole[:1]).all()) and torch.equal(got[rows // 183 * 183:], got[:rows % 183])
+    check_forward(ops, z[:183], tok[:183], 0.1, 0.0, 2)
+    part = ops.token_logprobs(z[:183], tok[:183], scale=0.1, top=2)
+    for got, want in zip(r, part):
+        assert torch.equal(got[:183], want)
+    want = ops.token_logprobs_backward(z[:183], tok[:183], part.lse, part.entropy, one[:183], one[:183], scale=0.1)
+    assert torch.equal(dz[:183], want)  # test_gradient holds such rows to the formula
+
+
 # ------------------------------------------------------------------- gradient
 def check_backward(ops, buf, z, tok, scale, clip, seed, use=(True, True), inplace=False, pad_out=0):
     rows, V = z.shape

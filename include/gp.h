@@ -577,7 +577,9 @@ typedef struct {
  *   g = factor grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2
  *   param <- (1 - lr weight_decay) param
  *            - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, the parameter rounded once (round to nearest even).  t is `step` (>= 1),
+ * in fp32, the parameter rounded once (round to nearest even).  A v that passes the
+ * largest float is infinite and the step 0; with 8-bit states its block's scale is infinite
+ * too, and the block's v is lost.  t is `step` (>= 1),
  * or, with step_dev given (device int64; step is then 0), step_dev[0] + 1, and the call
  * stores it back: what a captured step needs, since a replay repeats `step`.
  *   factor  : device fp32 [1] that every gradient is multiplied with (gp_grad_norm's

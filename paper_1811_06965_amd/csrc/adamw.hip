@@ -107,12 +107,36 @@ template <bool FOLDED> __device__ __forceinline__ unsigned code_bits(float x, fl
 __device__ __forceinline__ unsigned e4m3_code(unsigned bits, unsigned rnd16) {
     return min((bits + (rnd16 << 4) + 8u) >> 20, 126u);
 }
-// The square root rounded to nearest: the device's, off by up to a step, and one correction
-// from its exact remainder (half the instructions of sqrtf, which also serves
-// arguments below 2^-96).
+// The square root rounded to nearest, of 0 and of what lies from 2^-96 to the largest float:
+// the device's, off by up to a step, and one correction from its exact remainder (half the
+// instructions of sqrtf).
 __device__ __forceinline__ float root_of(float x) {
     const float s = __builtin_amdgcn_sqrtf(x);
     return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * __builtin_amdgcn_rcpf(fmaxf(s, 1e-30f)), s);
+}
+// Of four values that are not negative, any of them: below 2^-96, where the device's root
+// drops subnormals and the remainder has no bits left, that of 2^64 as much; of an infinity itself.
+// Two instructions a value tell the ordinary four.
+__device__ __forceinline__ f32x4 roots_of(f32x4 x) {
+    unsigned least = ~0u, most = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        least = min(least, __float_as_uint(x[e]) - 1u);  // a zero comes last
+        most = max(most, __float_as_uint(x[e]));
+    }
+    f32x4 r;
+    if (least >= 0x0F7FFFFFu && most < 0x7F800000u) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = root_of(x[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool low = x[e] < 0x1p-96f;
+            const float s = root_of(low ? x[e] * 0x1p64f : x[e]);
+            r[e] = x[e] == INFINITY ? x[e] : low ? s * 0x1p-32f : s;
+        }
+    }
+    return r;
 }
 
 // What four lanes' worth of memory holds before the update.
@@ -155,12 +179,14 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
         adamw_moments(gv[e], m, v, s, st);
         mv[e] = m;
         vv[e] = v;
-        if constexpr (BITS == 32) {
-            pv[e] = adamw_param(pv[e], m, v, T.keep, s, st);
-        } else {  // the parameter's step by a reciprocal that is off by a step
-            root[e] = root_of(v);
+        if constexpr (BITS == 32) pv[e] = adamw_param(pv[e], m, v, T.keep, s, st);
+    }
+    if constexpr (BITS == 8) {  // the parameter's step by a reciprocal that is off by a step
+        root = roots_of(vv);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
             const float den = __builtin_fmaf(root[e], st.inv_root, s.eps);
-            pv[e] = __builtin_fmaf(pv[e], T.keep, -st.step_size * m * __builtin_amdgcn_rcpf(den));
+            pv[e] = __builtin_fmaf(pv[e], T.keep, -st.step_size * mv[e] * __builtin_amdgcn_rcpf(den));
         }
     }
     Four<P>::store(T.p, i, T.n, whole, Four<P>::rounded(pv));

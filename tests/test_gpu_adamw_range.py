@@ -1,0 +1,50 @@
+"""AdamW's 8-bit update and the gradient norm at the ends of the fp32 range, against
+the same fp32 operations in numpy (tolerances as in test_gpu_adamw.py)."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_adamw import F, U, numpy_step, quantise, random_bits  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_1811_06965_amd import ops as o
+    return o
+
+
+@pytest.mark.parametrize("top", [1e-21, 1e-20, 1e-19, 3e-18, 1e-15, 1e-14, 1.0, 1e4, 1e18, 1.8e19, 2e19, 3e38])
+def test_second_moments_of_every_magnitude(ops, top):
+    """v below the normal range (|g| up to 3e-18 and beta2 = 0.999) keeps its root, and a v that passes the largest float
+    has an infinite root and a step of 0, as in 32 bits: codes, scales and the parameter's step as numpy's.  The
+    parameters start at 0 and eps is far below every root, so that the step is all there is to see."""
+    n = 1024
+    r = np.random.default_rng(5)
+    g = (np.linspace(-1, 1, n) * top).astype(F)
+    g[r.random(n) < 0.05] = 0
+    h = dict(lr=1e-3, b1=0.9, b2=0.999, eps=1e-30, seed=7)
+    p, m, v = np.zeros(n, F), np.zeros(n, np.uint8), np.zeros(n, np.uint8)
+    ms, vs = np.zeros(n // 256, F), np.zeros(n // 256, F)
+    dp, dg = torch.zeros(n, device="cuda"), torch.from_numpy(g).cuda()
+    opt = ops.AdamW([dp], [dg], state_bits=8, lr=h["lr"], eps=h["eps"], betas=(h["b1"], h["b2"]), seed=h["seed"])
+    for t in (1, 2, 3):
+        old = p
+        opt.step()
+        with np.errstate(all="ignore"):
+            p, m, v, ms, vs = numpy_step(p, g, m, v, ms, vs, h, t, 0.0, 1.0, 8, "f32")
+        got = dp.cpu().numpy()
+        assert np.array_equal(np.isfinite(got), np.isfinite(p)), t
+        assert (np.abs(got - p) <= 16 * U * np.abs(p - old) + 4 * U * np.abs(old)).all(), t
+        assert np.array_equal(opt.m_scale[0].cpu().numpy(), ms) and np.array_equal(opt.v_scale[0].cpu().numpy(), vs), t
+        kept = np.repeat(np.isfinite(vs), 256)  # the codes of a block with an infinite scale mean nothing
+        assert np.array_equal(opt.m[0].view(torch.uint8).cpu().numpy()[kept], m[kept]), t
+        assert np.array_equal(opt.v[0].view(torch.uint8).cpu().numpy()[kept], v[kept]), t
+        if not kept.all():
+            assert top > 1e19
+            break
+        p = got  # numpy goes on from the device's

@@ -569,7 +569,7 @@ typedef struct {
     int param_dtype, grad_dtype; /* gp_dtype, of every tensor of the call */
     int state_bits;              /* 32 or 8 */
     unsigned seed;               /* 8-bit states: of the random bits they are rounded with */
-    double lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps > 0 */
+    double lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps > 0 (8-bit states: >= 2^-126) */
 } gp_adamw_config;
 
 /*

@@ -397,6 +397,8 @@ gp_status check_adamw(const gp_adamw_tensor* t, int n, const gp_adamw_config* c,
     if (!(c->lr >= 0.0 && std::isfinite(c->lr)) || !(c->beta1 >= 0.0 && c->beta1 < 1.0) ||
         !(c->beta2 >= 0.0 && c->beta2 < 1.0) || !((float)c->eps > 0.f && std::isfinite(c->eps)))
         return bad("adamw: lr must be >= 0, betas in [0, 1), eps > 0, all finite");
+    // the 8-bit form's reciprocal of a subnormal is infinite, and 0 times it (no gradient yet) a NaN
+    if (c->state_bits == 8 && (float)c->eps < 0x1p-126f) return bad("adamw: 8-bit states need eps >= 2^-126");
     if (step_dev ? step != 0 : step < 1) return bad("adamw: give a step >= 1, or step_dev and step 0");
     if (!aligned(step_dev, 8) || !aligned(factor, 4)) return bad("adamw: misaligned step_dev or factor");
     for (int i = 0; i < n; ++i) {

@@ -48,3 +48,11 @@ def test_second_moments_of_every_magnitude(ops, top):
             assert top > 1e19
             break
         p = got  # numpy goes on from the device's
+
+
+def test_the_smallest_eps(ops):
+    """No gradient yet and the smallest eps that 8-bit states take: nothing moves."""
+    p, g = torch.ones(300, device="cuda"), torch.zeros(300, device="cuda")
+    opt = ops.AdamW([p], [g], state_bits=8, lr=1.0, eps=2.0 ** -126)
+    opt.step()
+    assert bool((p == 1.0).all()) and bool((opt.v_scale[0] == 0).all())

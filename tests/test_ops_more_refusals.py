@@ -1,0 +1,11 @@
+"""Further refusals of the operators on the caller's own tensors, by the host alone
+(the addresses are made up, as in test_ops_refusals.py)."""
+import pytest
+
+from test_ops_refusals import A, INVALID, adamw, gp  # noqa: F401 (gp: the fixture)
+
+
+@pytest.mark.parametrize("eps", [1e-39, 1e-45, 2.0 ** -127])
+def test_a_subnormal_eps_with_8_bit_states(gp, eps):  # noqa: F811
+    assert adamw(gp, cfg={"state_bits": 8, "eps": eps}, tensor={"m_scale": A, "v_scale": A}) == INVALID
+    assert "eps" in gp.gp_last_error()

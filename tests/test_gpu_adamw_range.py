@@ -56,3 +56,20 @@ def test_the_smallest_eps(ops):
     opt = ops.AdamW([p], [g], state_bits=8, lr=1.0, eps=2.0 ** -126)
     opt.step()
     assert bool((p == 1.0).all()) and bool((opt.v_scale[0] == 0).all())
+
+
+@pytest.mark.parametrize("spread", [[1e4, 1e-2, 1e-9, 1e-14], [1e18, 1e-18], [1.0, 1e-11, 1e-12, 1e-13], [1e-2, 1e-14]])
+def test_a_second_moment_beside_a_far_larger_one(ops, spread):
+    """What is not zero in v does not become zero, however much larger its block's largest is."""
+    n = 1024
+    r = np.random.default_rng(6)
+    g = (np.array(spread)[r.integers(0, len(spread), n)] * r.uniform(1, 2, n)).astype(F)
+    g[::17] = 0
+    opt = ops.AdamW([torch.zeros(n, device="cuda")], [torch.from_numpy(g).cuda()], state_bits=8, lr=0.0, betas=(0.0, 0.0),
+                    seed=3)
+    opt.step()
+    codes, scales = quantise(np.sqrt(g * g), random_bits(n, 3, 1)[1], True)
+    got = opt.v[0].view(torch.uint8).cpu().numpy()
+    assert np.array_equal(opt.v_scale[0].cpu().numpy(), scales)
+    assert np.array_equal(got == 0, g * g == 0)
+    assert np.array_equal(got, codes)

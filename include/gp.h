@@ -536,7 +536,7 @@ typedef struct {
 /*
  * The 2-norm over n tensors (host array, dtype all of them) and the factor that
  * clips it: norm_factor (device fp32 [2]) receives the norm and
- * min(1, max_norm / norm); 1 for a norm of 0, and NaN where the norm is not finite,
+ * min(1, max_norm / norm); 1 for a norm of 0, and NaN where the fp32 norm is not finite,
  * which makes gp_adamw_step leave everything as it was.  Squares are summed in
  * fp64 in a fixed order.  max_norm > 0; INFINITY gives the norm alone.
  *   ws : device scratch, 8-byte aligned, of at least the bytes that

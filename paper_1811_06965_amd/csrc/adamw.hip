@@ -312,12 +312,12 @@ __global__ void __launch_bounds__(256) norm_kernel(const NormBatch b, long chunk
     if (threadIdx.x == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// The norm and the factor that clips it.
+// The norm and the factor that clips it: a NaN where the norm, as it is stored, is not finite.
 __device__ __forceinline__ void write_norm(double sum, float max_norm, float* __restrict__ out) {
     const double norm = sqrt(sum);
     const double f = norm > (double)max_norm ? (double)max_norm / norm : 1.0;
     out[0] = (float)norm;
-    out[1] = isfinite(norm) ? (float)f : NAN;
+    out[1] = isfinite((float)norm) ? (float)f : NAN;
 }
 
 __global__ void __launch_bounds__(256) norm_finish_kernel(const double* __restrict__ partial, int n, float max_norm,

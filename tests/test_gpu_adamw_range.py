@@ -73,3 +73,14 @@ def test_a_second_moment_beside_a_far_larger_one(ops, spread):
     assert np.array_equal(opt.v_scale[0].cpu().numpy(), scales)
     assert np.array_equal(got == 0, g * g == 0)
     assert np.array_equal(got, codes)
+
+
+@pytest.mark.parametrize("count", [4, 4000, 400000])
+def test_a_norm_past_the_largest_float(ops, count):
+    """The norm is stored in fp32: where that is infinite the factor is a NaN, though fp64 holds the sum of the squares.
+    (One launch for the short lists, two for the long one.)"""
+    big = torch.full((count,), 3e38, device="cuda")
+    r = ops.grad_norm([big], max_norm=1.0)
+    assert float(r[0]) == math.inf and math.isnan(float(r[1]))
+    r = ops.grad_norm([big[:1]], max_norm=1.0)
+    assert abs(float(r[0]) / 3e38 - 1) < 1e-6 and abs(float(r[1]) * 3e38 - 1) < 1e-6

@@ -517,8 +517,8 @@ gp_status gp_token_logprobs_workspace(int dtype, long rows, int vocab, int top, 
  * GP_NO_TOKEN takes dlogp as 0, a row with lse = -inf has a zero gradient, a token
  * outside [0, vocab) gives a row of NaN.  A p below 2^-126 counts as 0.
  *   dlogits : device [rows, vocab] in dtype, rows ldd apart; may be logits itself
- *             (with ldd = ld), and must not overlap it otherwise.  The ldd - vocab
- *             elements behind a row are left as they were.
+ *             (with ldd = ld), and must not overlap it otherwise (columns of one buffer, ldd = ld,
+ *             may lie beside each other).  The ldd - vocab elements behind a row are left as they were.
  * GP_ERR_INVALID_ARG: as gp_token_logprobs; NULL lse or dlogits, neither dlogp
  *   nor dentropy, an overlap.
  */

@@ -488,6 +488,13 @@ size_t split_bytes(long rows, int splits, int top) { return (size_t)rows * split
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Rows of `row` bytes, `pitch` apart, from two starts lie between each other (the columns of one
+// buffer) without overlapping.
+bool side_by_side(uintptr_t a, uintptr_t b, size_t row, size_t pitch) {
+    const size_t off = pitch ? (a < b ? b - a : a - b) % pitch : 0;
+    return off >= row && off + row <= pitch;
+}
+
 gp_status check_rows(int dtype, const void* logits, long rows, int vocab, long ld, float scale, float clip) {
     auto bad = [](const char* m) { return set_error(GP_ERR_INVALID_ARG, m); };
     if (dtype != GP_F32 && dtype != GP_BF16) return bad("token_logprobs: unknown dtype");
@@ -635,7 +642,8 @@ gp_status gp_token_logprobs_backward(int dtype, const void* logits, long rows, i
     if (rows == 0) return GP_OK;
     const uintptr_t z0 = reinterpret_cast<uintptr_t>(logits), d0 = reinterpret_cast<uintptr_t>(dlogits);
     const uintptr_t z1 = z0 + ((size_t)(rows - 1) * ld + vocab) * es, d1 = d0 + ((size_t)(rows - 1) * ldd + vocab) * es;
-    if (!(z0 == d0 && ld == ldd) && z0 < d1 && d0 < z1)
+    const bool same = z0 == d0 && (ld == ldd || rows == 1);
+    if (!same && z0 < d1 && d0 < z1 && !side_by_side(z0, d0, (size_t)vocab * es, ld == ldd ? (size_t)ld * es : 0))
         return bad("token_logprobs_backward: dlogits overlaps the logits without being them");
     for (long r = 0; r < rows; r += LAUNCH_ROWS) {
         const long n = std::min(LAUNCH_ROWS, rows - r);

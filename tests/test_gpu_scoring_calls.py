@@ -1,0 +1,83 @@
+"""Scoring under a partition's vocabulary head: its refusals on an idle partition, each
+by its status, and that none of them leaves a trace; calls on a stream of the caller's."""
+import pytest
+
+import synth
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_partition_adamw import DEC_F32  # noqa: E402
+
+
+def call(part, x_, mem_, tok_, **kw):
+    """gp_score_sequences with buffers of its own size, an argument or more replaced."""
+    from paper_1811_06965_amd import gp
+    rows = tok_.numel()
+    f = torch.zeros(4, rows, device="cuda")[:3]
+    ids, lp = torch.zeros(rows, 64, dtype=torch.int32, device="cuda"), torch.zeros(rows, 64, device="cuda")
+    a = dict(x=x_.data_ptr(), mem=mem_.data_ptr(), tokens=tok_.data_ptr(), scale=1.0, logp=f[0].data_ptr(),
+             lse=f[1].data_ptr(), entropy=f[2].data_ptr(), top=4, top_ids=ids.data_ptr(), top_logp=lp.data_ptr(),
+             stream=torch.cuda.current_stream().cuda_stream)
+    own = dict(f=f, lp=lp)
+    a.update({k: v(own) if callable(v) else v for k, v in kw.items()})
+    gp.gp_score_sequences(part.h, *a.values())
+    return f
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=None), dict(mem=None), dict(tokens=None), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+    dict(scale=float("inf")), dict(top=-1), dict(top=33), dict(top=41), dict(top_ids=None), dict(top_logp=None),
+    dict(logp=lambda o: o["f"].data_ptr() + 2), dict(lse=lambda o: o["f"].data_ptr() + 1),
+    dict(entropy=lambda o: o["f"].data_ptr() + 3), dict(top_logp=lambda o: o["lp"].data_ptr() + 2)],
+    ids=lambda kw: "-".join(kw))
+def test_refusals_on_an_idle_partition(kw):
+    from paper_1811_06965_amd import gp
+    from paper_1811_06965_amd.runtime import Partition
+    case = synth.make_case(DEC_F32, 44)
+    with Partition(DEC_F32) as part:
+        part.load_params(case["layers"], case["head"])
+        inp = part.device_inputs(case)
+        n = DEC_F32.batch // DEC_F32.micro
+        x, tok, mem = (inp[k][:n].contiguous() for k in ("x", "dy", "mem"))
+        want = call(part, x, mem, tok).clone()
+        with pytest.raises(gp.GpError) as err:
+            call(part, x, mem, tok, **kw)
+        assert err.value.status == gp.GP_ERR_INVALID_ARG
+        assert torch.equal(call(part, x, mem, tok), want)
+        part.step(inp["x"], inp["mem"], inp["dy"], lr=1e-3)
+
+
+def test_more_alternatives_than_tokens():
+    """A vocabulary of 24: 25 alternatives are refused, 24 are not."""
+    from paper_1811_06965_amd import gp
+    from paper_1811_06965_amd.runtime import Partition
+    cfg = DEC_F32.with_(vocab=24)
+    case = synth.make_case(cfg, 44)
+    with Partition(cfg) as part:
+        part.load_params(case["layers"], case["head"])
+        inp = part.device_inputs(case)
+        n = cfg.batch // cfg.micro
+        x, tok, mem = (inp[k][:n].contiguous() for k in ("x", "dy", "mem"))
+        with pytest.raises(gp.GpError) as err:
+            call(part, x, mem, tok, top=25)
+        assert err.value.status == gp.GP_ERR_INVALID_ARG
+        r = part.score(x, tok, mem, top=24)
+        assert all(sorted(i) == list(range(24)) for i in r.top_ids.tolist())
+
+
+def test_no_memory_input_for_an_encoder():
+    from paper_1811_06965_amd import gp
+    from paper_1811_06965_amd.runtime import Partition
+    cfg = synth.CONFIGS["tiny"].with_(loss="xent_ls", vocab=40)
+    case = synth.make_case(cfg, 45)
+    with Partition(cfg) as part:
+        part.load_params(case["layers"], case["head"])
+        inp = part.device_inputs(case)
+        n = cfg.batch // cfg.micro
+        x, tok = (inp[k][:n].contiguous() for k in ("x", "dy"))
+        with pytest.raises(gp.GpError) as err:
+            call(part, x, x, tok)
+        assert err.value.status == gp.GP_ERR_INVALID_ARG
+        assert bool(part.score(x, tok).logp.isfinite().all())

@@ -78,6 +78,7 @@ class Partition:
         except Exception:
             gp.gp_partition_destroy(self.h)
             raise
+        self.device = torch.device("cuda", torch.cuda.current_device())
 
     def close(self):
         if self.h is not None:
@@ -199,9 +200,11 @@ class Partition:
         dys = dy.chunk(M)
         weights = None
         if dlogp is not None or dentropy is not None:
-            for w in (dlogp, dentropy):
-                if w is not None and (w.dtype != torch.float32 or w.shape != dy.shape or not w.is_contiguous()):
-                    raise ValueError("dlogp and dentropy must be contiguous float32 of the tokens' shape")
+            for name, t, kind in (("dy", dy, torch.int32), ("dlogp", dlogp, torch.float32),
+                                  ("dentropy", dentropy, torch.float32)):
+                if t is not None and (t.dtype != kind or t.shape != dy.shape or not t.is_contiguous()
+                                      or t.device != self.device):
+                    raise ValueError(f"{name} must be contiguous {kind} of the tokens' shape on {self.device}")
             weights = [[None] * M if w is None else w.chunk(M) for w in (dlogp, dentropy)]
         dxs = dx.chunk(M) if dx is not None else [None] * M
         dms = dmem.chunk(M) if dmem is not None else [None] * M
@@ -254,19 +257,21 @@ class Partition:
         """Log probabilities, entropies and alternatives under the vocabulary
         head (gp_score_sequences) for n S tokens: x [n, S, D] and mem in the
         partition dtype, tokens int32 [n, S].  An ops.TokenLogprobs of rows n S."""
-        rows, dev = self.cfg.batch // self.M * self.cfg.seq, x.device
-        if tokens is not None and (tokens.dtype != torch.int32 or tokens.numel() != rows or not tokens.is_contiguous()):
-            raise ValueError("tokens must be contiguous int32, one per position")
-        want = {"x": (x, rows * self.cfg.d_model)}
+        rows = self.cfg.batch // self.M * self.cfg.seq
+        if not 0 <= top <= min(gp.GP_TOP_MAX, self.cfg.vocab):
+            raise ValueError(f"top must be in [0, min({gp.GP_TOP_MAX}, vocab)]")
+        want = {"x": (x, self.tdtype, rows * self.cfg.d_model)}
+        if tokens is not None:
+            want["tokens"] = (tokens, torch.int32, rows)
         if mem is not None:
-            want["mem"] = (mem, self.cfg.batch // self.M * self.cfg.mem_seq * self.cfg.d_model)
-        for name, (t, count) in want.items():
-            if t.dtype != self.tdtype or t.numel() != count or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous {self.tdtype} of {count} elements")
+            want["mem"] = (mem, self.tdtype, self.cfg.batch // self.M * self.cfg.mem_seq * self.cfg.d_model)
+        for name, (t, kind, count) in want.items():
+            if t.dtype != kind or t.numel() != count or not t.is_contiguous() or t.device != self.device:
+                raise ValueError(f"{name} must be contiguous {kind} of {count} elements on {self.device}")
         st = torch.cuda.current_stream().cuda_stream if stream is None else stream
-        logp, lse, entropy = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind(0)
-        top_ids = torch.empty((rows, top), dtype=torch.int32, device=dev) if top else None
-        top_logp = torch.empty((rows, top), dtype=torch.float32, device=dev) if top else None
+        logp, lse, entropy = torch.empty((3, rows), dtype=torch.float32, device=self.device).unbind(0)
+        top_ids = torch.empty((rows, top), dtype=torch.int32, device=self.device) if top else None
+        top_logp = torch.empty((rows, top), dtype=torch.float32, device=self.device) if top else None
         ptr = lambda t: None if t is None else t.data_ptr()
         gp.gp_score_sequences(self.h, x.data_ptr(), ptr(mem), ptr(tokens), scale,
                               logp.data_ptr() if tokens is not None else None, lse.data_ptr(), entropy.data_ptr(), top,

@@ -149,6 +149,13 @@ class Partition:
         return gp.gp_param_count(self.h)
 
     # ------------------------------------------------------------ schedule
+    def _stream(self, handle):
+        """The stream of a raw handle (None: the current one), and a context in which tensors are allocated for it."""
+        if handle is None:
+            return torch.cuda.current_stream(self.device), torch.cuda.stream(None)
+        stream = torch.cuda.ExternalStream(handle, device=self.device)
+        return stream, torch.cuda.stream(stream)
+
     def device_inputs(self, case, device="cuda"):
         """Move a synthetic case's boundary tensors to the device."""
         t = lambda a: torch.tensor(a, dtype=torch.float32).to(device=device, dtype=self.tdtype).contiguous()
@@ -180,7 +187,7 @@ class Partition:
         dy holds tokens, and the backwards go through
         gp_backward_microbatch_weighted with these weights."""
         M = self.M
-        main = torch.cuda.current_stream() if stream is None else torch.cuda.ExternalStream(stream)
+        main, allocated_for_it = self._stream(stream)
         st = main.cuda_stream
         lanes = [st]
         if (fwd_streams > 1 or bwd_streams > 1) and M > 1 and self._lane is None:
@@ -188,12 +195,14 @@ class Partition:
         if fwd_streams > 1 and M > 1:
             self._lane.wait_stream(main)
             lanes.append(self._lane.cuda_stream)
-        if want_y and y is None:
-            y = torch.empty_like(x)
-        if want_dx and dx is None:
-            dx = torch.empty_like(x)
-        if mem is not None and want_dmem and dmem is None:
-            dmem = torch.empty_like(mem)
+        with allocated_for_it:
+            if want_y and y is None:
+                y = torch.empty_like(x)
+            if want_dx and dx is None:
+                dx = torch.empty_like(x)
+            if mem is not None and want_dmem and dmem is None:
+                dmem = torch.empty_like(mem)
+            y_remat = torch.empty_like(x) if want_recomputed else None
         xs = x.chunk(M)
         ms = mem.chunk(M) if mem is not None else [None] * M
         ys = y.chunk(M) if y is not None else [None] * M
@@ -214,7 +223,6 @@ class Partition:
             fwd(self.h, m, ptr(xs[m]), ptr(ms[m]), ptr(ys[m]), lanes[m % len(lanes)])
         if len(lanes) > 1:
             main.wait_stream(self._lane)
-        y_remat = torch.empty_like(x) if want_recomputed else None
         yr = y_remat.chunk(M) if want_recomputed else None
         blanes = [st]
         if bwd_streams > 1 and M > 1:
@@ -256,7 +264,8 @@ class Partition:
     def score(self, x, tokens=None, mem=None, scale=1.0, top=0, stream=None):
         """Log probabilities, entropies and alternatives under the vocabulary
         head (gp_score_sequences) for n S tokens: x [n, S, D] and mem in the
-        partition dtype, tokens int32 [n, S].  An ops.TokenLogprobs of rows n S."""
+        partition dtype, tokens int32 [n, S].  An ops.TokenLogprobs of rows n S,
+        its tensors allocated for `stream` (the current one unless given)."""
         rows = self.cfg.batch // self.M * self.cfg.seq
         if not 0 <= top <= min(gp.GP_TOP_MAX, self.cfg.vocab):
             raise ValueError(f"top must be in [0, min({gp.GP_TOP_MAX}, vocab)]")
@@ -268,14 +277,15 @@ class Partition:
         for name, (t, kind, count) in want.items():
             if t.dtype != kind or t.numel() != count or not t.is_contiguous() or t.device != self.device:
                 raise ValueError(f"{name} must be contiguous {kind} of {count} elements on {self.device}")
-        st = torch.cuda.current_stream().cuda_stream if stream is None else stream
-        logp, lse, entropy = torch.empty((3, rows), dtype=torch.float32, device=self.device).unbind(0)
-        top_ids = torch.empty((rows, top), dtype=torch.int32, device=self.device) if top else None
-        top_logp = torch.empty((rows, top), dtype=torch.float32, device=self.device) if top else None
+        st, allocated_for_it = self._stream(stream)
+        with allocated_for_it:
+            logp, lse, entropy = torch.empty((3, rows), dtype=torch.float32, device=self.device).unbind(0)
+            top_ids = torch.empty((rows, top), dtype=torch.int32, device=self.device) if top else None
+            top_logp = torch.empty((rows, top), dtype=torch.float32, device=self.device) if top else None
         ptr = lambda t: None if t is None else t.data_ptr()
         gp.gp_score_sequences(self.h, x.data_ptr(), ptr(mem), ptr(tokens), scale,
                               logp.data_ptr() if tokens is not None else None, lse.data_ptr(), entropy.data_ptr(), top,
-                              ptr(top_ids), ptr(top_logp), st)
+                              ptr(top_ids), ptr(top_logp), st.cuda_stream)
         return TokenLogprobs(logp if tokens is not None else None, lse, entropy, top_ids, top_logp)
 
     def grad_norm(self):

@@ -8,7 +8,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_partition_adamw import DEC_F32  # noqa: E402
+from test_gpu_partition_adamw import DEC_BF16, DEC_F32  # noqa: E402
 
 
 def call(part, x_, mem_, tok_, **kw):
@@ -81,3 +81,50 @@ def test_no_memory_input_for_an_encoder():
             call(part, x, x, tok)
         assert err.value.status == gp.GP_ERR_INVALID_ARG
         assert bool(part.score(x, tok).logp.isfinite().all())
+
+
+def held_back(count, value, dtype=torch.float32):
+    """A block of the current stream's allocator, freed, that queued work on the stream has still to write."""
+    a = torch.randn(4096, 4096, device="cuda")
+    t = torch.empty(count, dtype=dtype, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(20):  # some 20 ms
+        a = torch.mm(a, a).mul_(1e-3)
+    t.fill_(value)
+
+
+@pytest.mark.parametrize("top", [0, 4])
+def test_scores_on_a_stream_of_the_callers(top):
+    """Outputs are memory of the stream that writes them: not a block that the current stream's queued work, which the
+    given stream does not wait for, is still to write."""
+    from paper_1811_06965_amd.runtime import Partition
+    case = synth.make_case(DEC_BF16, 46, perturb=True)
+    with Partition(DEC_BF16) as part:
+        part.load_params(case["layers"], case["head"])
+        inp = part.device_inputs(case)
+        n = DEC_BF16.batch // DEC_BF16.micro
+        x, tok, mem = (inp[k][:n].contiguous() for k in ("x", "dy", "mem"))
+        want = part.score(x, tok, mem, top=top)
+        side, rows = torch.cuda.Stream(), tok.numel()
+        torch.cuda.synchronize()
+        for count in {3 * rows, max(1, top) * rows}:
+            held_back(count, 7.0)
+            got = part.score(x, tok, mem, top=top, stream=side.cuda_stream)
+            torch.cuda.synchronize()
+            assert all((a is None and b is None) or torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_step_on_a_stream_of_the_callers():
+    from paper_1811_06965_amd.runtime import Partition
+    case = synth.make_case(DEC_BF16, 47, perturb=True)
+    with Partition(DEC_BF16) as part:
+        part.load_params(case["layers"], case["head"])
+        inp = part.device_inputs(case)
+        want = part.step(inp["x"], inp["mem"], inp["dy"], want_recomputed=True)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        held_back(inp["x"].numel(), 7.0, torch.bfloat16)
+        got = part.step(inp["x"], inp["mem"], inp["dy"], want_recomputed=True, want_loss=False, stream=side.cuda_stream)
+        torch.cuda.synchronize()
+        for k in ("y", "dx", "dmem", "y_remat"):
+            assert torch.equal(got[k], want[k]), k

@@ -132,27 +132,40 @@ def _records(struct, n, **columns):
 
 
 def _addresses(tensors):
-    return [t.data_ptr() for t in tensors]
+    return list(map(torch.Tensor.data_ptr, tensors))
 
 
 class TensorList:
-    """Gradients whose addresses a program passes again and again: checked and
-    listed once.  Holds the tensors."""
+    """Gradients that a program passes again and again: checked and listed once,
+    and again where one has been given other storage (``.data``, ``set_``).  Holds
+    the tensors."""
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
-        self.tensors = _same("gradients", tensors)
+        self.tensors = list(tensors)
+        self.scratch = gp.gp_grad_norm_workspace(len(self.tensors))  # bytes that grad_norm takes
+        self._list(_addresses(self.tensors))
+
+    def _list(self, addresses):
+        _same("gradients", self.tensors)
         if not self.tensors or self.tensors[0].dtype not in DTYPE:
             raise ValueError("a TensorList needs float32 or bfloat16 tensors")
         self.dtype = DTYPE[self.tensors[0].dtype]
-        self.scratch = gp.gp_grad_norm_workspace(len(self.tensors))  # bytes that grad_norm takes
-        self._rows, self.array = _records(gp.gp_grad_tensor, len(self.tensors), grad=_addresses(self.tensors),
+        self._rows, self.array = _records(gp.gp_grad_tensor, len(self.tensors), grad=addresses,
                                           count=[t.numel() for t in self.tensors])
+        self._at = addresses
+
+    def follow(self):
+        """Lists the tensors anew if one has moved."""
+        now = _addresses(self.tensors)
+        if now != self._at:
+            self._list(now)
+        return self
 
 
 def grad_norm(grads: Union[TensorList, Sequence[torch.Tensor]], max_norm=float("inf")):
     """fp32 [2] on the device: the 2-norm over all the tensors, and the factor
     min(1, max_norm / norm) that clips them (NaN where the norm is not finite)."""
-    g = grads if isinstance(grads, TensorList) else TensorList(grads)
+    g = grads.follow() if isinstance(grads, TensorList) else TensorList(grads)
     dev, need = g.tensors[0].device, g.scratch
     out = torch.empty(2, dtype=torch.float32, device=dev)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
@@ -171,7 +184,12 @@ class AdamW:
     types that ``m`` and ``v`` of another AdamW have.  copies: bf16 tensors that
     receive the updated fp32 parameters.  weight_decay: a number or one per
     parameter.  steps: updates done before.  capturable: the step counter lives
-    on the device (``step_dev``), as a step recorded into a graph needs."""
+    on the device (``step_dev``), as a step recorded into a graph needs.
+
+    Parameters, gradients and copies that are given other storage (``.data``,
+    ``set_``, a module's ``to``) are followed at the next step, and refused if they
+    no longer match.  The states stay in the storage that they had here: change them in
+    place (``copy_``)."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m=None, v=None, m_scale=None,
                  v_scale=None, copies=None, state_bits: Optional[int] = None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8,
@@ -206,35 +224,53 @@ class AdamW:
                     raise ValueError("m_scale and v_scale must hold one float32 per 256 elements of their parameter")
         elif m_scale is not None or v_scale is not None:
             raise ValueError("scales belong to 8-bit states")
-        self.copies = None if copies is None else _same("copies", copies, self.params)
-        if self.copies and any(t.dtype != torch.bfloat16 or t.device != dev for t in self.copies):
-            raise ValueError(f"copies must be bfloat16 on {dev}")
+        self.copies = None if copies is None else list(copies)
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         if len(decay) != n:
             raise ValueError("weight_decay must be a number or one per parameter")
-        columns = dict(param=_addresses(self.params), count=[p.numel() for p in self.params], weight_decay=decay,
-                       m=_addresses(self.m), v=_addresses(self.v))
+        columns = dict(count=[p.numel() for p in self.params], weight_decay=decay, m=_addresses(self.m),
+                       v=_addresses(self.v))
         if state_bits == 8:
             columns.update(m_scale=_addresses(self.m_scale), v_scale=_addresses(self.v_scale))
-        if self.copies:
-            columns["copy"] = _addresses(self.copies)
-        live = [a for k in ("param", "m", "v") for a, c in zip(columns[k], columns["count"]) if c]
-        if len(set(live)) < len(live):
-            raise ValueError("a parameter or a state is given twice")
         self._rows, self.array = _records(gp.gp_adamw_tensor, n, **columns)
+        # the states' storage lives as long as their addresses here
+        self._states = [t.detach() for t in [*self.m, *self.v, *(self.m_scale or ()), *(self.v_scale or ())]]
         self.cfg = gp.gp_adamw_config(DTYPE[self.params[0].dtype], 0, state_bits, seed, lr, betas[0], betas[1], eps)
         self.steps = steps
         self.step_dev = torch.full((1,), steps, dtype=torch.int64, device=dev) if capturable else None
-        self.bind_grads(grads)
+        self.grads = grads
+        self._list()
+
+    def _list(self):
+        """The addresses of parameters, copies and gradients as they are now, checked against the states'."""
+        dev = self.m[0].device
+        params = _same("params", self.params, self.m)
+        copies = [] if self.copies is None else _same("copies", self.copies, self.m)
+        if params[0].dtype not in DTYPE or params[0].device != dev:
+            raise ValueError(f"params must be float32 or bfloat16 on {dev}")
+        if copies and (copies[0].dtype != torch.bfloat16 or copies[0].device != dev):
+            raise ValueError(f"copies must be bfloat16 on {dev}")
+        at, copies_at = _addresses(params), _addresses(copies)
+        states = [self._rows[k].tolist() for k in ("m", "v")]
+        live = [a for k in (at, *states) for a, c in zip(k, self._rows["count"]) if c]
+        if len(set(live)) < len(live):
+            raise ValueError("a parameter or a state is given twice")
+        self.cfg.param_dtype = DTYPE[params[0].dtype]
+        self._rows["param"] = at
+        if copies:
+            self._rows["copy"] = copies_at
+        self._written, self._written_at = params + copies, at + copies_at
+        self.bind_grads(self.grads)
 
     def bind_grads(self, grads: Sequence[torch.Tensor]):
         """The gradients that the next steps read."""
         grads = _same("grads", grads, self.params)
-        if grads[0].dtype not in DTYPE or grads[0].device != self.params[0].device:
+        if grads[0].dtype not in DTYPE or grads[0].device != self.m[0].device:
             raise ValueError("grads must be float32 or bfloat16 on the parameters' device")
         self.grads = grads
         self.cfg.grad_dtype = DTYPE[grads[0].dtype]
-        self._rows["grad"] = _addresses(grads)
+        self._grads_at = _addresses(grads)
+        self._rows["grad"] = self._grads_at
 
     def step(self, lr: Optional[float] = None, factor: Optional[torch.Tensor] = None):
         """One update.  factor: fp32 on the device, multiplied into every
@@ -242,9 +278,11 @@ class AdamW:
         The host's count ``steps`` goes up either way."""
         if lr is not None:
             self.cfg.lr = lr
-        dev = self.params[0].device
+        dev = self.m[0].device
         if factor is not None and (factor.dtype != torch.float32 or factor.numel() != 1 or factor.device != dev):
             raise ValueError("factor must be one float32 on the parameters' device")
+        if _addresses(self._written) != self._written_at or _addresses(self.grads) != self._grads_at:
+            self._list()
         host = 0 if self.step_dev is not None else self.steps + 1
         _on(dev, lambda stream: gp.gp_adamw_step(self.array, len(self.params), self.cfg, host, _ptr(self.step_dev),
                                                  _ptr(factor), stream))

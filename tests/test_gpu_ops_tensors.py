@@ -1,0 +1,130 @@
+"""The operators' lists of tensors when the tensors change under them: other storage,
+another type or size, against an optimizer made for the tensors as they are."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+SIZES = [1000, 7, 4096]
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_1811_06965_amd import ops as o
+    return o
+
+
+def make(seed, dtype=torch.float32):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.randn(n, generator=g, device="cuda").to(dtype) for n in SIZES]
+
+
+def pair(ops, bits, copies=False, **kw):
+    """Two optimizers of equal tensors, and their tensors."""
+    out = []
+    for _ in range(2):
+        p, g = make(1), make(2)
+        c = make(3, torch.bfloat16) if copies else None
+        out += [ops.AdamW(p, g, copies=c, state_bits=bits, weight_decay=0.1, seed=4, **kw), p, g, c]
+    return out
+
+
+def same(a, b):
+    return all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_other_storage_is_followed(ops, bits):
+    """Parameters, working copies and gradients that move between steps, by .data and by set_: the new storage is
+    updated and read, the old is left as it was."""
+    a, p, g, c, b, q, h, d = pair(ops, bits, copies=True)
+    old = []
+    for t in range(4):
+        if t == 1:
+            for x in p + c:
+                old.append((x.data, x.detach().clone()))
+                x.data = x.data.clone()
+        if t == 2:
+            for x in g:
+                x.data = x.data * 2
+            for x in h:
+                x.mul_(2)
+            for x, y in old:
+                assert torch.equal(x, y)
+            old = []
+        if t == 3:
+            p[1].set_(p[1].clone())
+            g[2].set_(g[2].clone())
+        a.step()
+        b.step()
+        assert same(p, q) and same(c, d) and same(a.m, b.m) and same(a.v, b.v), t
+    assert a.steps == b.steps == 4
+
+
+def test_a_module_that_moves_and_comes_back(ops):
+    """to() gives a module's parameters and gradients other storage: of another type they are refused, of the old type
+    again they are taken."""
+    m = torch.nn.Linear(40, 30, device="cuda")
+    for x in m.parameters():
+        x.grad = torch.ones_like(x)
+    opt = ops.AdamW(list(m.parameters()), [x.grad for x in m.parameters()], lr=1e-2)
+    opt.step()
+    before = [x.detach().clone() for x in m.parameters()]
+    for kw in (dict(dtype=torch.float64), dict(device="cpu")):
+        m.to(**kw)
+        with pytest.raises(ValueError):
+            opt.step()
+        assert opt.steps == 1
+        m.to(dtype=torch.float32, device="cuda")
+    opt.bind_grads([x.grad for x in m.parameters()])
+    opt.step()
+    for x, y in zip(m.parameters(), before):
+        assert bool(((y - x - 1e-2).abs() < 1e-6).all())  # lr against a constant gradient
+
+
+@pytest.mark.parametrize("which", ["params", "grads", "copies"])
+def test_another_size_is_refused(ops, which):
+    a, p, g, c, *_ = pair(ops, 32, copies=True)
+    before = [x.clone() for x in p + c + a.m + a.v]
+    x = dict(params=p, grads=g, copies=c)[which][0]
+    keep = x.data
+    for bad in (x.data[:999].clone(), torch.zeros(1001, dtype=x.dtype, device="cuda"), x.data.double(), x.data.cpu(),
+                torch.zeros(2000, dtype=x.dtype, device="cuda")[::2]):
+        x.data = bad
+        for _ in range(2):
+            with pytest.raises(ValueError):
+                a.step()
+    x.data = keep
+    assert a.steps == 0 and same(p + c + a.m + a.v, before)
+    a.step()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_states_stay_in_their_storage(ops, bits):
+    """A state that is given other storage: the optimizer goes on with what it had, which is not freed meanwhile."""
+    a, p, g, _, b, q, h, _ = pair(ops, bits)
+    held = a.m + a.v + (a.m_scale + a.v_scale if bits == 8 else [])
+    for t in range(3):
+        if t == 1:
+            for x in held:
+                x.data = torch.zeros(1, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).to(x.dtype)
+            junk = [torch.full((n,), 77.0, device="cuda") for n in SIZES for _ in range(20)]  # noqa: F841
+        a.step()
+        b.step()
+        assert same(p, q), t
+
+
+def test_a_list_follows_its_tensors(ops):
+    g = make(5)
+    lst = ops.TensorList(g)
+    for _ in range(2):
+        assert torch.equal(ops.grad_norm(lst), ops.grad_norm([x.clone() for x in g]))
+        for x in g:
+            x.data = torch.cat([x.data, x.data])  # other storage, twice the size
+    g[1].data = g[1].data.double()
+    with pytest.raises(ValueError):
+        ops.grad_norm(lst)
+    for x in g:
+        x.data = x.data.to(torch.bfloat16)
+    assert torch.equal(ops.grad_norm(lst), ops.grad_norm([x.clone() for x in g]))

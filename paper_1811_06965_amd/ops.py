@@ -61,6 +61,15 @@ def _rows(name, t):
     return rows, vocab, ld
 
 
+def _no_graph(*tensors):
+    """The operators build no autograd graph: an input whose gradient would be lost is refused."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("no autograd graph is built here: detach the inputs, or call under torch.no_grad(), and "
+                                 "take the gradient from token_logprobs_backward")
+
+
 def _vector(name, t, rows, dtype, device):
     if t is not None and (t.dtype != dtype or t.dim() != 1 or t.numel() != rows or t.device != device
                           or not t.is_contiguous()):
@@ -70,7 +79,10 @@ def _vector(name, t, rows, dtype, device):
 def token_logprobs(logits, tokens=None, scale=1.0, clip=0.0, top=0) -> TokenLogprobs:
     """gp_token_logprobs of rows of logits [rows, vocab] (a row stride is fine)
     and int32 tokens [rows] (gp.GP_NO_TOKEN where there is none; None: no
-    logp).  scale: 1 / temperature; clip: the head's logit clip, 0 = off."""
+    logp).  scale: 1 / temperature; clip: the head's logit clip, 0 = off.  Not
+    differentiable by itself: logits that require a gradient are refused unless
+    autograd is off."""
+    _no_graph(logits)
     rows, vocab, ld = _rows("logits", logits)
     dev, dt = _gpu(logits), DTYPE[logits.dtype]
     _vector("tokens", tokens, rows, torch.int32, dev)
@@ -92,6 +104,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentr
     """gp_token_logprobs_backward: the gradient of sum dlogp logp + dentropy
     entropy with respect to the logits.  out: where it goes (may be logits
     itself); allocated otherwise."""
+    _no_graph(logits, lse, entropy, dlogp, dentropy, out)
     rows, vocab, ld = _rows("logits", logits)
     dev = _gpu(logits)
     _vector("tokens", tokens, rows, torch.int32, dev)

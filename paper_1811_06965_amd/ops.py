@@ -14,6 +14,7 @@ from typing import NamedTuple, Optional, Sequence, Union
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from . import gp
 
@@ -121,6 +122,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentr
     _on(dev, lambda stream: gp.gp_token_logprobs_backward(
         DTYPE[logits.dtype], logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip, _ptr(lse), _ptr(entropy),
         _ptr(dlogp), _ptr(dentropy), out.data_ptr(), ldd, stream))
+    increment_version(out)  # a graph that saved it must not be walked back with what it holds now
     return out
 
 
@@ -299,4 +301,5 @@ class AdamW:
         host = 0 if self.step_dev is not None else self.steps + 1
         _on(dev, lambda stream: gp.gp_adamw_step(self.array, len(self.params), self.cfg, host, _ptr(self.step_dev),
                                                  _ptr(factor), stream))
+        increment_version(self._written)  # parameters that a graph saved are not those it would walk back with
         self.steps += 1

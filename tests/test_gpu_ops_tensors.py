@@ -128,3 +128,27 @@ def test_a_list_follows_its_tensors(ops):
     for x in g:
         x.data = x.data.to(torch.bfloat16)
     assert torch.equal(ops.grad_norm(lst), ops.grad_norm([x.clone() for x in g]))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_graph_of_what_was_overwritten(ops, dtype):
+    """A graph that saved a parameter, a working copy or logits is not walked back after they were updated or
+    overwritten."""
+    w = torch.randn(8, 16, device="cuda").to(dtype).requires_grad_()
+    c = torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda") if dtype == torch.float32 else None
+    opt = ops.AdamW([w], [torch.ones_like(w)], copies=None if c is None else [c])
+    x = torch.randn(4, 8, device="cuda").to(dtype).requires_grad_()
+    losses = [(x @ w).sum()]
+    if c is not None:
+        losses.append((x.to(torch.bfloat16) @ c).sum())
+    opt.step()
+    z = torch.randn(4, 16, device="cuda").to(dtype)
+    scale = torch.ones((), device="cuda", dtype=dtype, requires_grad=True)
+    losses.append((z * scale).sum())
+    tok = torch.zeros(4, dtype=torch.int32, device="cuda")
+    r = ops.token_logprobs(z, tok)
+    ops.token_logprobs_backward(z, tok, r.lse, dlogp=torch.ones(4, device="cuda"), out=z)
+    for loss in losses:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    (x @ w).sum().backward()  # a graph of the updated parameter

@@ -126,14 +126,22 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentr
     return out
 
 
+def _fits(t, like):
+    """Of the same shape, up to dimensions of 1, or one of them flat: a transposed tensor has as many elements too."""
+    if t.shape == like.shape:
+        return True
+    a, b = ([n for n in x.shape if n != 1] for x in (t, like))
+    return t.numel() == like.numel() and (a == b or len(a) == 1 or len(b) == 1 or t.numel() == 0)
+
+
 def _same(name, tensors, like=None):
-    """Tensors of one type on one GPU, each contiguous (and of the sizes of `like`)."""
+    """Tensors of one type on one GPU, each contiguous (and of the shapes of `like`)."""
     tensors = list(tensors)
     if tensors:
         kind, dev = tensors[0].dtype, tensors[0].get_device()
         if dev < 0 or any(t.dtype != kind or t.get_device() != dev or not t.is_contiguous() for t in tensors):
             raise ValueError(f"{name} must be contiguous tensors of one type on one GPU")
-    if like is not None and [t.numel() for t in tensors] != [t.numel() for t in like]:
+    if like is not None and (len(tensors) != len(like) or not all(map(_fits, tensors, like))):
         raise ValueError(f"{name} must match the parameters one by one")
     return tensors
 
@@ -193,7 +201,8 @@ class AdamW:
     """AdamW over a list of parameters, one gp_adamw_step per ``step``.
 
     params: contiguous fp32 or bf16 tensors.  grads: one per parameter, read at
-    every step (``bind_grads`` names others).  state_bits: 32, or 8 (e4m3 values
+    every step (``bind_grads`` names others); they, the states and the copies have
+    their parameter's shape or are flat.  state_bits: 32, or 8 (e4m3 values
     with an fp32 scale per 256 elements, v held as its square root); the states
     start at zero, or m, v (and m_scale, v_scale) are taken as they are, of the
     types that ``m`` and ``v`` of another AdamW have.  copies: bf16 tensors that

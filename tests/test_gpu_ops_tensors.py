@@ -152,3 +152,29 @@ def test_a_graph_of_what_was_overwritten(ops, dtype):
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             loss.backward()
     (x @ w).sum().backward()  # a graph of the updated parameter
+
+
+@pytest.mark.parametrize("which", ["grads", "m", "v", "copies"])
+def test_transposed_tensors_are_refused(ops, which):
+    def build(shape):
+        p = [torch.ones(6, 10, device="cuda"), torch.ones(5, device="cuda")]
+        kw = {k: [torch.zeros(s, device="cuda") for s in ((6, 10), (5,))] for k in ("grads", "m", "v")}
+        kw["copies"] = [torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((6, 10), (5,))]
+        kw[which][0] = kw[which][0].view(-1).view(shape)
+        return ops.AdamW(p, kw.pop("grads"), **kw)
+
+    for shape in ((10, 6), (2, 30), (3, 4, 5)):
+        with pytest.raises(ValueError, match="match the parameters"):
+            build(shape)
+    for shape in ((6, 10), (60,), (6, 1, 10), (1, 60)):
+        build(shape).step()
+    opt = build((6, 10))
+    with pytest.raises(ValueError, match="match the parameters"):
+        opt.bind_grads([torch.zeros(10, 6, device="cuda"), torch.zeros(5, device="cuda")])
+    opt.bind_grads([torch.zeros(60, device="cuda"), torch.zeros(5, 1, device="cuda")])
+    opt.step()
+
+
+def test_empty_tensors_of_any_shape(ops):
+    p = [torch.ones(0, 3, device="cuda"), torch.ones(4, device="cuda")]
+    ops.AdamW(p, [torch.ones(0, device="cuda"), torch.ones(4, device="cuda")]).step()

@@ -158,6 +158,14 @@ def _addresses(tensors):
     return list(map(torch.Tensor.data_ptr, tensors))
 
 
+def _spans(rows, **bytes_each):
+    """Starts and ends, by start, of what each column's addresses and the bytes of each tensor make; empty ones left out."""
+    start = np.concatenate([rows[k] for k in bytes_each]).astype(np.int64)
+    size = np.concatenate([np.broadcast_to(b, rows.shape) for b in bytes_each.values()])
+    order = np.argsort(np.where(size > 0, start, -1), kind="stable")[np.count_nonzero(size == 0):]
+    return start[order], (start + size)[order]
+
+
 class TensorList:
     """Gradients that a program passes again and again: checked and listed once,
     and again where one has been given other storage (``.data``, ``set_``).  Holds
@@ -260,41 +268,59 @@ class AdamW:
         # the states' storage lives as long as their addresses here
         self._states = [t.detach() for t in [*self.m, *self.v, *(self.m_scale or ()), *(self.v_scale or ())]]
         self.cfg = gp.gp_adamw_config(DTYPE[self.params[0].dtype], 0, state_bits, seed, lr, betas[0], betas[1], eps)
-        self.steps = steps
+        self.device, self.steps = dev, steps
         self.step_dev = torch.full((1,), steps, dtype=torch.int64, device=dev) if capturable else None
-        self.grads = grads
-        self._list()
+        self._list(grads)
 
-    def _list(self):
+    def _list(self, grads):
         """The addresses of parameters, copies and gradients as they are now, checked against the states'."""
-        dev = self.m[0].device
-        params = _same("params", self.params, self.m)
-        copies = [] if self.copies is None else _same("copies", self.copies, self.m)
+        dev, states = self.device, self._states[:len(self.params)]
+        params = _same("params", self.params, states)
+        copies = [] if self.copies is None else _same("copies", self.copies, states)
         if params[0].dtype not in DTYPE or params[0].device != dev:
             raise ValueError(f"params must be float32 or bfloat16 on {dev}")
         if copies and (copies[0].dtype != torch.bfloat16 or copies[0].device != dev):
             raise ValueError(f"copies must be bfloat16 on {dev}")
         at, copies_at = _addresses(params), _addresses(copies)
-        states = [self._rows[k].tolist() for k in ("m", "v")]
-        live = [a for k in (at, *states) for a, c in zip(k, self._rows["count"]) if c]
-        if len(set(live)) < len(live):
-            raise ValueError("a parameter or a state is given twice")
         self.cfg.param_dtype = DTYPE[params[0].dtype]
         self._rows["param"] = at
         if copies:
             self._rows["copy"] = copies_at
+        n = self._rows["count"]
+        state = n * states[0].element_size()
+        columns = dict(param=n * params[0].element_size(), m=state, v=state)
+        if self.m_scale is not None:
+            columns["m_scale"] = columns["v_scale"] = -(-n // gp.GP_STATE_BLOCK) * 4
+        if copies:
+            columns["copy"] = n * 2
+        self._starts, self._ends = _spans(self._rows, **columns)
+        if (self._starts[1:] < self._ends[:-1]).any():
+            raise ValueError("parameters, states, scales and copies must not share memory")
+        self._list_grads(grads)
         self._written, self._written_at = params + copies, at + copies_at
-        self.bind_grads(self.grads)
 
     def bind_grads(self, grads: Sequence[torch.Tensor]):
         """The gradients that the next steps read."""
+        if _addresses(self._written) != self._written_at:
+            self._list(grads)
+        else:
+            self._list_grads(grads)
+
+    def _list_grads(self, grads):
         grads = _same("grads", grads, self.params)
-        if grads[0].dtype not in DTYPE or grads[0].device != self.m[0].device:
+        if grads[0].dtype not in DTYPE or grads[0].device != self.device:
             raise ValueError("grads must be float32 or bfloat16 on the parameters' device")
+        at = _addresses(grads)
+        n = self._rows["count"] * grads[0].element_size()
+        start = np.array(at, dtype=np.int64)
+        # the first output that ends behind a gradient's start begins behind its end
+        behind = np.searchsorted(self._ends, start, side="right")
+        if ((start + n > np.append(self._starts, np.iinfo(np.int64).max)[behind]) & (n > 0)).any():
+            raise ValueError("gradients must not share memory with what a step writes")
         self.grads = grads
         self.cfg.grad_dtype = DTYPE[grads[0].dtype]
-        self._grads_at = _addresses(grads)
-        self._rows["grad"] = self._grads_at
+        self._grads_at = at
+        self._rows["grad"] = at
 
     def step(self, lr: Optional[float] = None, factor: Optional[torch.Tensor] = None):
         """One update.  factor: fp32 on the device, multiplied into every
@@ -302,11 +328,11 @@ class AdamW:
         The host's count ``steps`` goes up either way."""
         if lr is not None:
             self.cfg.lr = lr
-        dev = self.m[0].device
+        dev = self.device
         if factor is not None and (factor.dtype != torch.float32 or factor.numel() != 1 or factor.device != dev):
             raise ValueError("factor must be one float32 on the parameters' device")
         if _addresses(self._written) != self._written_at or _addresses(self.grads) != self._grads_at:
-            self._list()
+            self._list(self.grads)
         host = 0 if self.step_dev is not None else self.steps + 1
         _on(dev, lambda stream: gp.gp_adamw_step(self.array, len(self.params), self.cfg, host, _ptr(self.step_dev),
                                                  _ptr(factor), stream))

@@ -178,3 +178,58 @@ def test_transposed_tensors_are_refused(ops, which):
 def test_empty_tensors_of_any_shape(ops):
     p = [torch.ones(0, 3, device="cuda"), torch.ones(4, device="cuda")]
     ops.AdamW(p, [torch.ones(0, device="cuda"), torch.ones(4, device="cuda")]).step()
+
+
+def test_shared_memory_is_refused(ops):
+    """Anything a step writes that shares memory with something else of the step, by its start or in part."""
+    def build(**kw):
+        z = lambda n, k=torch.float32: torch.zeros(n, dtype=k, device="cuda")  # noqa: E731
+        a = dict(params=[z(512), z(300)], grads=[z(512), z(300)], m=[z(512), z(300)], v=[z(512), z(300)],
+                 copies=[z(512, torch.bfloat16), z(300, torch.bfloat16)])
+        buf = torch.zeros(2000, device="cuda")
+        for k, (i, cut) in kw.items():
+            a[k][i] = cut(buf)
+        opt = ops.AdamW(a.pop("params"), a.pop("grads"), **a)
+        opt.step()
+        return opt
+
+    def cut(a, n):
+        return lambda b: b[a:a + n]
+
+    def half(a, n):  # bf16 elements of the same buffer
+        return lambda b: b.view(torch.bfloat16)[a:a + n]
+
+    for kw in (dict(params=(0, cut(0, 512)), m=(1, cut(511, 300))), dict(params=(0, cut(0, 512)), v=(0, cut(0, 512))),
+               dict(m=(0, cut(100, 512)), v=(0, cut(0, 512))), dict(params=(1, cut(300, 300)), copies=(0, half(90, 512))),
+               dict(copies=(0, half(0, 512)), v=(1, cut(255, 300)))):
+        with pytest.raises(ValueError, match="must not share memory"):
+            build(**kw)
+    for kw in (dict(params=(0, cut(0, 512)), grads=(1, cut(511, 300))), dict(params=(1, cut(0, 300)), grads=(1, cut(0, 300))),
+               dict(v=(1, cut(200, 300)), grads=(0, cut(0, 512)))):
+        with pytest.raises(ValueError, match="gradients must not share"):
+            build(**kw)
+    # side by side in one buffer, and one gradient for two parameters, are fine
+    build(params=(0, cut(0, 512)), m=(1, cut(512, 300)), copies=(0, half(1624, 512)), grads=(1, cut(1068, 300)))
+    p, g = [torch.ones(9, device="cuda") for _ in range(2)], torch.ones(9, device="cuda")
+    opt = ops.AdamW(p, [g, g], lr=0.5)
+    opt.step()
+    assert torch.equal(*p)
+    with pytest.raises(ValueError, match="gradients must not share"):
+        opt.bind_grads([g, opt.v[0]])
+    opt.step()
+    scales = [torch.zeros(3, device="cuda")] * 2
+    kw = {k: [torch.zeros(700, device="cuda").to(torch.float8_e4m3fn)] for k in "mv"}
+    with pytest.raises(ValueError, match="must not share memory"):
+        ops.AdamW([torch.zeros(700, device="cuda")], [torch.zeros(700, device="cuda")], m_scale=scales[:1],
+                  v_scale=scales[:1], **kw)
+
+
+def test_a_parameter_that_moves_onto_another_tensor_is_refused(ops):
+    a, p, g, *_ = pair(ops, 32)
+    for x in (a.m[0], g[0]):
+        p[0].data = x.data
+        for _ in range(2):
+            with pytest.raises(ValueError, match="must not share memory"):
+                a.step()
+    p[0].data = torch.zeros(1000, device="cuda")
+    a.step()

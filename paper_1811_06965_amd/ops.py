@@ -233,6 +233,8 @@ class AdamW:
             state_bits = 8 if m and m[0].dtype == torch.float8_e4m3fn else 32
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 32 or 8")
+        if steps < 0:
+            raise ValueError("steps must not be negative")
         dev, n = self.params[0].device, len(self.params)
         kind = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         if (m is None) != (v is None):

@@ -233,3 +233,10 @@ def test_a_parameter_that_moves_onto_another_tensor_is_refused(ops):
                 a.step()
     p[0].data = torch.zeros(1000, device="cuda")
     a.step()
+
+
+@pytest.mark.parametrize("capturable", [True, False])
+def test_negative_steps_are_refused(ops, capturable):
+    """A counter on the device that starts at -1 would make the first bias correction 0 and the parameters NaN."""
+    with pytest.raises(ValueError, match="steps"):
+        ops.AdamW(make(1), make(2), steps=-1, capturable=capturable)

@@ -352,8 +352,8 @@ gp_status gp_stream_destroy(gp_stream stream);
  * With check_finite set the call synchronises, and if any gradient is
  * non-finite the update is skipped and GP_ERR_NONFINITE returned.
  * GP_OPT_ADAMW counts its updates on the device, so that a captured step may be
- * replayed.  With max_grad_norm a norm that is not finite skips the update on the
- * device; a call with loss_out then returns GP_ERR_NONFINITE.
+ * replayed (with the lr it was captured with).  With max_grad_norm a norm that is not
+ * finite skips the update on the device; a call with loss_out then returns GP_ERR_NONFINITE.
  * GP_LOSS_XENT_LS: a label outside [0, V) is read as class 0 on the device
  * and flagged; the next call that synchronises (loss_out non-NULL or
  * check_finite) then skips the update and returns GP_ERR_INVALID_ARG.
@@ -379,7 +379,8 @@ gp_status gp_get_grad_norm(gp_partition* p, float* norm);
  *   tokens, scale, logp, lse, entropy, top, top_ids, top_logp : as gp_token_logprobs,
  *            with rows = n seq_len in token order.
  * Ordered after the last update and before the next mini-batch's work by the
- * library, whatever streams they are issued on.
+ * library, whatever streams they are issued on; the replays of a captured mini-batch, which
+ * the library does not see, are the caller's to order.
  * GP_ERR_STATE: not configured, or inside a mini-batch.
  * GP_ERR_UNSUPPORTED: the partition has no vocabulary head.
  * GP_ERR_INVALID_ARG: as gp_forward_microbatch and gp_token_logprobs.
@@ -496,7 +497,9 @@ gp_status gp_mfma_peak(void* stream, double* tflops);
  *             in another order.
  * A logit x of -1e30 or less (-inf, or a type's lowest value, as masks leave it) is a
  * token that cannot occur: p = 0, logp -inf, among the alternatives last and in
- * order of index.  A row of nothing else has lse and logp -inf and entropy 0.
+ * order of index.  A row of nothing else has lse and logp -inf and entropy 0.  That holds for
+ * x, so with clip > 0 a masked logit is clipped to -clip like any other and its token can occur:
+ * a caller with both clips its logits first, masks them, and gives clip 0.
  * A row with NaN or +inf gives NaN; NaN counts as the largest logit.  Sums are
  * fp32, in an order that only the sizes and the alignment decide.
  * GP_ERR_INVALID_ARG: NULL logits, negative sizes, vocab < 1 or > 2^30, ld < vocab,
@@ -577,19 +580,22 @@ typedef struct {
  *   g = factor grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2
  *   param <- (1 - lr weight_decay) param
  *            - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, the parameter rounded once (round to nearest even).  A v that passes the
- * largest float is infinite and the step 0; with 8-bit states its block's scale is infinite
- * too, and the block's v is lost.  t is `step` (>= 1),
- * or, with step_dev given (device int64; step is then 0), step_dev[0] + 1, and the call
- * stores it back: what a captured step needs, since a replay repeats `step`.
+ * in fp32, the parameter rounded once (round to nearest even).  With 8-bit states the
+ * parameter's division is a product with a reciprocal off by up to 2^-23 of it, and its sums are
+ * fused.  A v that passes the largest float is infinite and the step 0; with 8-bit states its
+ * block's scale is infinite too, and the block's v is lost.  t is `step` (>= 1), or, with
+ * step_dev given (device int64; step is then 0), step_dev[0] + 1, and the call stores it back:
+ * what a captured step needs, since a replay repeats `step`.  A replay also repeats lr and the
+ * rest of cfg and of the tensors' records; another lr is another capture.
  *   factor  : device fp32 [1] that every gradient is multiplied with (gp_grad_norm's
- *             second value); NULL: 1.  If it is NaN nothing is changed, step_dev included.
+ *             second value); NULL: 1.  If it is NaN nothing is changed, step_dev included
+ *             (whether such an update counts in the next `step` is the caller's to say).
  * States in 8 bits: GP_STATE_BLOCK consecutive elements share the scale
  * max|x| / 448, and x / scale is rounded to e4m3 up or down at random, so that the
  * small changes of a moment are kept on average where rounding to nearest would lose
  * them (with beta2 = 0.999 nearly all).  What is not zero in v does not become zero.  The 16
- * random bits are a fixed function of seed, t and the element's index i in its
- * tensor, so a step gives the same bits each time:
+ * random bits are a fixed function of seed, t and the element's index i in its tensor
+ * (the same for element i of every tensor), so a step gives the same bits each time:
  *   h = floor(i / 4) + 0x3C6EF372 seed + 0x1E3779B1 t;  h ^= h >> 16;  h *= 0x6A3F9B15;
  *   h ^= h >> 15;  h *= 0x5D47C1E3;  h ^= h >> 16;  h *= K[i mod 4],
  *   K = 0x4F1BBCDD, 0x7A6D2C8B, 0x35E9A1F7, 0x1D872B41   (mod 2^32);

@@ -249,9 +249,9 @@ __device__ __forceinline__ void find_top(TopShared<NT>& sh, const T* zr, int V, 
 // A workgroup of NT threads per row, or `splits` of them, each over `per` chunks of it;
 // thread t takes the chunks t, t + NT, .., four loads ahead of their use (eight made
 // long rows 3% slower).  Bound by HBM where rows are many: 1024 rows of 32000 bf16
-// 14.0 us (4.7 TB/s, the launch included), 4096 of 128000 with 8 alternatives 191 us (5.5
-// TB/s), close to what its 11 vector instructions a logit take; for few rows by the chain
-// of reductions: one row of 32000 4.4 us, with 5 alternatives 7.4.
+// 14.0 us (4.7 TB/s, the launch included), 4096 of 32000 fp32 91 us (5.8 TB/s) and 95 with 8
+// alternatives, 4096 of 128000 bf16 with 8 191 us (5.5 TB/s), close to what its 11 vector instructions a logit take; for few rows by the chain
+// of reductions: one row of 32000 4.4 us, with 5 alternatives 7.3.
 template <typename T, bool CLIP, bool TOP, int NT>
 __global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, int V, long ld,
                                                      const int* __restrict__ tokens, float scale, float clip, RowOut out,
@@ -462,7 +462,7 @@ int chunk_count(int dtype, int vocab) {
 // split / whole, bf16 with 5 alternatives: one row of 131072 9.1 / 14.8, 32 rows 10.8 / 15.3,
 // 64 rows 12.2 / 15.0 (7.4 / 11.6 with none, 16.6 / 16.2 with 20), 96 rows 13.3 / 15.2; but 128
 // rows 15.7 / 15.8, one row of 32000 8.4 / 7.4, 64 of 65536 10.6 / 10.3, and 93 of 50021 fp32
-// with 20 15.8 / 10.5.
+// with 20 17.5 / 11.1 (19.2 / 12.9 with one row of masks alone, whose alternatives are all ties).
 int row_splits(int dtype, long rows, int vocab) {
     const long chunks = chunk_count(dtype, vocab);
     if (rows < 1 || rows > 96 || chunks < 16384) return 1;

@@ -80,7 +80,8 @@ def _vector(name, t, rows, dtype, device):
 def token_logprobs(logits, tokens=None, scale=1.0, clip=0.0, top=0) -> TokenLogprobs:
     """gp_token_logprobs of rows of logits [rows, vocab] (a row stride is fine)
     and int32 tokens [rows] (gp.GP_NO_TOKEN where there is none; None: no
-    logp).  scale: 1 / temperature; clip: the head's logit clip, 0 = off.  Not
+    logp).  scale: 1 / temperature; clip: the head's logit clip, 0 = off (it lifts a
+    masked logit to -clip: clip before masking instead).  Not
     differentiable by itself: logits that require a gradient are refused unless
     autograd is off."""
     _no_graph(logits)
@@ -173,7 +174,6 @@ class TensorList:
 
     def __init__(self, tensors: Sequence[torch.Tensor]):
         self.tensors = list(tensors)
-        self.scratch = gp.gp_grad_norm_workspace(len(self.tensors))  # bytes that grad_norm takes
         self._list(_addresses(self.tensors))
 
     def _list(self, addresses):
@@ -181,6 +181,7 @@ class TensorList:
         if not self.tensors or self.tensors[0].dtype not in DTYPE:
             raise ValueError("a TensorList needs float32 or bfloat16 tensors")
         self.dtype = DTYPE[self.tensors[0].dtype]
+        self.scratch = gp.gp_grad_norm_workspace(len(self.tensors))  # bytes that grad_norm takes
         self._rows, self.array = _records(gp.gp_grad_tensor, len(self.tensors), grad=addresses,
                                           count=[t.numel() for t in self.tensors])
         self._at = addresses
@@ -327,7 +328,10 @@ class AdamW:
     def step(self, lr: Optional[float] = None, factor: Optional[torch.Tensor] = None):
         """One update.  factor: fp32 on the device, multiplied into every
         gradient (``grad_norm(...)[1:]``); a NaN leaves everything as it was.
-        The host's count ``steps`` goes up either way."""
+        The host's count ``steps`` goes up either way, for the factor stays on the
+        device: the bias corrections that follow count a skipped update, unless
+        capturable, where the device's counter does not.  A captured step keeps
+        the lr, seed and addresses it was captured with."""
         if lr is not None:
             self.cfg.lr = lr
         dev = self.device

@@ -248,7 +248,7 @@ class Partition:
     def capture_step(self, x, mem, dy, lr=0.0, dx=None, dmem=None, want_y=False, y=None, dlogp=None, dentropy=None):
         """Capture one whole mini-batch step (M forwards, M backwards, the
         update) into a HIP graph on a capture stream and return it; replay()
-        runs the step again on the same buffers.  The capture itself runs no
+        runs the step again on the same buffers, with the same lr.  The capture itself runs no
         work.  The loss is not read (that would synchronise), and the
         partition must not check gradients for finiteness (same reason).
         The step is captured on the capture stream alone (one stream for the

@@ -250,8 +250,9 @@ __device__ __forceinline__ void find_top(TopShared<NT>& sh, const T* zr, int V, 
 // thread t takes the chunks t, t + NT, .., four loads ahead of their use (eight made
 // long rows 3% slower).  Bound by HBM where rows are many: 1024 rows of 32000 bf16
 // 14.0 us (4.7 TB/s, the launch included), 4096 of 32000 fp32 91 us (5.8 TB/s) and 95 with 8
-// alternatives, 4096 of 128000 bf16 with 8 191 us (5.5 TB/s), close to what its 11 vector instructions a logit take; for few rows by the chain
-// of reductions: one row of 32000 4.4 us, with 5 alternatives 7.3.
+// alternatives, 4096 of 128000 bf16 with 8 191 us (5.5 TB/s), close to what its 11 vector
+// instructions a logit take; for few rows by the chain of reductions: one row of 32000 4.4 us, with
+// 5 alternatives 7.3.
 template <typename T, bool CLIP, bool TOP, int NT>
 __global__ void __launch_bounds__(NT) logprob_kernel(const T* __restrict__ z, int V, long ld,
                                                      const int* __restrict__ tokens, float scale, float clip, RowOut out,

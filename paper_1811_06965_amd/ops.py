@@ -277,6 +277,7 @@ class AdamW:
 
     def _list(self, grads):
         """The addresses of parameters, copies and gradients as they are now, checked against the states'."""
+        self._written_at = None  # whatever is refused below is looked at again
         dev, states = self.device, self._states[:len(self.params)]
         params = _same("params", self.params, states)
         copies = [] if self.copies is None else _same("copies", self.copies, states)

@@ -240,3 +240,17 @@ def test_negative_steps_are_refused(ops, capturable):
     """A counter on the device that starts at -1 would make the first bias correction 0 and the parameters NaN."""
     with pytest.raises(ValueError, match="steps"):
         ops.AdamW(make(1), make(2), steps=-1, capturable=capturable)
+
+
+def test_a_parameter_that_comes_back_after_a_refusal(ops):
+    """Refused for sharing memory and given its own storage again: that is what the next step writes."""
+    a, p, g, _, b, q, *_ = pair(ops, 32)
+    for x in (a.m[0], g[0]):
+        own = p[0].data
+        p[0].data = x.data
+        with pytest.raises(ValueError, match="must not share memory"):
+            a.step()
+        p[0].data = own
+        a.step()
+        b.step()
+        assert same(p, q) and same(a.m, b.m) and same(a.v, b.v) and p[0].data_ptr() == own.data_ptr()

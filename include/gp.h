@@ -583,7 +583,8 @@ typedef struct {
  * in fp32, the parameter rounded once (round to nearest even).  With 8-bit states the
  * parameter's division is a product with a reciprocal off by up to 2^-23 of it, and its sums are
  * fused.  A v that passes the largest float is infinite and the step 0; with 8-bit states its
- * block's scale is infinite too, and the block's v is lost.  t is `step` (>= 1), or, with
+ * block's scale is infinite too, every v of the block with it.  An infinite or NaN gradient makes its
+ * parameter NaN, and with 8-bit states its block's at the next update.  t is `step` (>= 1), or, with
  * step_dev given (device int64; step is then 0), step_dev[0] + 1, and the call stores it back:
  * what a captured step needs, since a replay repeats `step`.  A replay also repeats lr and the
  * rest of cfg and of the tensors' records; another lr is another capture.

@@ -210,7 +210,8 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
         unsigned qm = 0, qr = 0;
         // What is not zero in v does not become zero: at least code 1 (told from the root itself, whose
         // scaled bits are 0 from 2^-38 of the block's largest down); 0 in a block stored as zeros.
-        const unsigned least = sr != 0.f ? 1u : 0u;
+        // In a block with an infinite v every one becomes infinite (a zero times the scale would be a NaN).
+        const unsigned least = sr != 0.f ? 1u : 0u, lost = sr == INFINITY ? 1u : 0u;
         auto codes = [&](auto folded, float am, float ar) {
             constexpr bool F = decltype(folded)::value;
 #pragma unroll
@@ -218,7 +219,8 @@ __device__ __forceinline__ void update4(const AdamwTensor& T, const AdamwScalars
                 const unsigned u = h * K[e], bm = code_bits<F>(mv[e], am), br = code_bits<F>(root[e], ar);
                 const unsigned sign = __float_as_uint(mv[e]) >> 24 & 0x80u;
                 qm |= (e4m3_code(bm, u & 0xFFFFu) | sign) << (8 * e);
-                qr |= max(e4m3_code(br, u >> 16), min(__float_as_uint(root[e]), least)) << (8 * e);
+                const unsigned some = __float_as_uint(root[e]) | (F ? 0u : lost);
+                qr |= max(e4m3_code(br, u >> 16), min(some, least)) << (8 * e);
             }
         };
         if (tm < 0x1p13f && tr < 0x1p13f)

@@ -84,3 +84,27 @@ def test_a_norm_past_the_largest_float(ops, count):
     assert float(r[0]) == math.inf and math.isnan(float(r[1]))
     r = ops.grad_norm([big[:1]], max_norm=1.0)
     assert abs(float(r[0]) / 3e38 - 1) < 1e-6 and abs(float(r[1]) * 3e38 - 1) < 1e-6
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_after_a_gradient_whose_square_is_infinite(ops, bits):
+    """A v that passed the largest float stays infinite: its parameter's steps are 0 from there on, in 8 bits its
+    block's too, whether they had a gradient before or not; the other blocks go on, and nothing becomes a NaN."""
+    n = 1024
+    p, g = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    g[1::2] = 0
+    p[:] = 1
+    opt = ops.AdamW([p], [g], state_bits=bits, lr=1e-3, seed=2)
+    opt.step()
+    g[300] = 2e19
+    opt.step()
+    held = p.clone()
+    g[300] = 1
+    for _ in range(3):
+        opt.step()
+    moved = p != held
+    want = g != 0
+    if bits == 8:
+        want[256:512] = False
+    want[300] = False
+    assert bool(p.isfinite().all()) and torch.equal(moved, want)

@@ -612,6 +612,95 @@ typedef struct {
 gp_status gp_adamw_step(const gp_adamw_tensor* tensors, int n, const gp_adamw_config* cfg, long long step,
                         long long* step_dev, const float* factor, gp_stream stream);
 
+/*
+ * Rows of a tensor [batch, len, heads, head_dim] anywhere in device memory: the
+ * features of a head adjacent, the rest at strides in elements (0 to 2^41).  The address
+ * and every stride in use are multiples of 16 bytes; rows lie at least head_dim
+ * elements and at most 2^24 bytes apart.  So the heads of one projection, the halves of a packed
+ * [.., 2, heads, head_dim] or a [batch, heads, len, head_dim] tensor are taken as they lie.
+ */
+typedef struct {
+    void* data;
+    long seq_stride, row_stride, head_stride;
+} gp_head_rows;
+
+/* The most buckets of a relative position bias, and the furthest distance that has its own. */
+#define GP_BUCKETS_MAX 1024
+#define GP_DISTANCE_MAX 1024
+
+/* Attention of queries to keys of another length.  Query row i of sequence b stands at position
+ * i + q_starts[b] among the keys. */
+typedef struct {
+    int dtype;                     /* gp_dtype of every tensor of rows */
+    int batch, heads, kv_heads;    /* heads / kv_heads neighbouring query heads share a key and value head */
+    int q_len, k_len, head_dim;    /* head_dim: whole 16 bytes, at most 128 */
+    int causal;                    /* nonzero: keys up to the query's position alone */
+    float scale;                   /* > 0; 1 / sqrt(head_dim) as a rule */
+    const int* q_lens;             /* device int32 [batch]: rows in use of each sequence, cut to [0, q_len]; NULL: q_len */
+    const int* k_lens;             /* the same of the keys; NULL: k_len */
+    const int* q_starts;           /* device int32 [batch]; NULL: 0 */
+    const float* bias;             /* device fp32 [heads, buckets], or NULL */
+    const int* bucket_of;          /* device int32 [2 max_distance + 1]: bucket of the distance key - position from
+                                      -max_distance on; further ones take the outermost; cut to [0, buckets) */
+    int buckets, max_distance;     /* at most GP_BUCKETS_MAX and GP_DISTANCE_MAX; 0 without a bias */
+} gp_attention_config;
+
+/*
+ * out_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i),  lse_i = log sum_j exp(s_ij),
+ * s_ij = scale q_i . k_j + bias[h, bucket(j - position of i)]
+ * over the keys j < k_lens[b] and, with causal, j <= position of i (cross-attention to an
+ * encoder's states; a decoder's self-attention; with q_len 1 one token's step).
+ *   q, out : [batch, q_len, heads, head_dim];  k, v : [batch, k_len, kv_heads, head_dim].
+ *   lse    : device fp32 [batch, heads, q_len], what the backward pass needs; may be NULL.
+ *   ws     : device scratch, 16-byte aligned, of at least the bytes that
+ *            gp_attention_workspace(cfg, 0, &bytes) names (0 where keys are not split).
+ * Rows that see no key, and rows from q_lens[b] on, have out 0 and lse -inf.  A bias of -1e30
+ * or less is a mask.  What masked keys and values hold, infinities and NaN included, changes
+ * nothing; neither do rows of q from q_lens[b] on.  Products are made in dtype with fp32 sums (with
+ * bf16 the weights p are rounded to bf16 before they meet v), the softmax in fp32.  out
+ * must not overlap the inputs (tensors beside each other in every period of a stride that both have are fine).
+ * GP_ERR_INVALID_ARG: NULL tensors, sizes out of range (lengths up to 2^28, 65535 heads, batch x heads x
+ *   (length / 128 + 1) below 2^24), heads not a multiple of kv_heads, an output that overlaps an input, a
+ *   misaligned address or stride, scale not > 0, a bias without its buckets, a workspace that is NULL or too small.  GP_ERR_UNSUPPORTED: head_dim > 128, more buckets or a further
+ *   distance than above.
+ */
+gp_status gp_attention(const gp_attention_config* cfg, const gp_head_rows* q, const gp_head_rows* k,
+                       const gp_head_rows* v, const gp_head_rows* out, float* lse, void* ws, size_t ws_bytes,
+                       gp_stream stream);
+gp_status gp_attention_workspace(const gp_attention_config* cfg, int backward, size_t* bytes);
+
+/*
+ * The gradient of sum dout . out, from the out and lse that gp_attention gave:
+ *   delta_i = dout_i . out_i,  ds_ij = p_ij (dout_i . v_j - delta_i)
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
+ *   dbias[h, b] = sum of ds over the pairs of bucket b
+ * dk and dv summed over the heads that share them; zero for keys from k_lens[b] on and for queries that see no
+ * key or lie at q_lens[b] or beyond.
+ *   out    : NULL: delta is formed as sum_j p_ij (dout_i . v_j), without the rounding of out
+ *            (slower by two products; a bf16 call with a bias does so in any case, since that rounding is
+ *            common to all pairs of a row and adds up in dbias).
+ *   dbias  : device fp32 [heads, buckets], overwritten; may be NULL.
+ *   ws     : gp_attention_workspace(cfg, 1, &bytes).
+ * No atomics: the same call gives the same bits.  The gradients must not overlap each other or any input.
+ * GP_ERR_INVALID_ARG, GP_ERR_UNSUPPORTED: as gp_attention; lse NULL; dbias without a bias.
+ */
+gp_status gp_attention_backward(const gp_attention_config* cfg, const gp_head_rows* q, const gp_head_rows* k,
+                                const gp_head_rows* v, const gp_head_rows* out, const float* lse,
+                                const gp_head_rows* dout, const gp_head_rows* dq, const gp_head_rows* dk,
+                                const gp_head_rows* dv, float* dbias, void* ws, size_t ws_bytes, gp_stream stream);
+
+/*
+ * The usual map of distances to buckets, into host memory [2 max_distance + 1] (to be copied to the device
+ * for gp_attention_config.bucket_of): of one side's n buckets (buckets / 2 where bidirectional, all otherwise) the first
+ * n / 2 hold one distance each, the others are spaced evenly in the logarithm up to max_distance:
+ *   d < n/2: d;  else min(n - 1, n/2 + floor(log(d / (n/2)) / log(max_distance / (n/2)) (n - n/2))),
+ * the floor taken exactly.  Keys before the query, and at its place, come first; keys behind it have n more
+ * (bidirectional), or bucket 0.
+ * GP_ERR_INVALID_ARG: bucket_of NULL, fewer than 2 buckets a side, an odd number for two sides,
+ *   max_distance not in (n/2, GP_DISTANCE_MAX], buckets > GP_BUCKETS_MAX.
+ */
+gp_status gp_relative_buckets(int buckets, int max_distance, int bidirectional, int* bucket_of);
+
 /* Message of the calling thread's last failure (library-owned, valid until the
  * thread's next failing call); "" if none. */
 const char* gp_last_error(void);

@@ -43,9 +43,10 @@ EXPORTS = ["gp_partition_create", "gp_partition_configure", "gp_partition_destro
            "gp_token_logprobs", "gp_token_logprobs_workspace", "gp_token_logprobs_backward", "gp_grad_norm",
            "gp_grad_norm_workspace", "gp_adamw_step", "gp_get_grad_norm", "gp_score_sequences",
            "gp_backward_microbatch_weighted", "gp_get_moment", "gp_set_moment", "gp_get_updates", "gp_set_updates",
-           "gp_last_error"]
+           "gp_attention", "gp_attention_workspace", "gp_attention_backward", "gp_relative_buckets", "gp_last_error"]
 
 GP_TOP_MAX, GP_NO_TOKEN, GP_STATE_BLOCK = 32, -1, 256
+GP_BUCKETS_MAX, GP_DISTANCE_MAX = 1024, 1024
 
 
 class gp_config(ctypes.Structure):
@@ -73,6 +74,19 @@ class gp_adamw_config(ctypes.Structure):
     _fields_ = [("param_dtype", ctypes.c_int), ("grad_dtype", ctypes.c_int), ("state_bits", ctypes.c_int),
                 ("seed", ctypes.c_uint), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
                 ("beta2", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class gp_head_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_long), ("row_stride", ctypes.c_long),
+                ("head_stride", ctypes.c_long)]
+
+
+class gp_attention_config(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("batch", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("q_len", ctypes.c_int), ("k_len", ctypes.c_int), ("head_dim", ctypes.c_int), ("causal", ctypes.c_int),
+                ("scale", ctypes.c_float), ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p),
+                ("q_starts", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("bucket_of", ctypes.c_void_p),
+                ("buckets", ctypes.c_int), ("max_distance", ctypes.c_int)]
 
 
 class GpError(RuntimeError):
@@ -132,6 +146,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.gp_backward_microbatch_weighted.argtypes = [P, I, VP, VP, VP, VP, VP, VP]
     lib.gp_get_grad_norm.argtypes = [P, ctypes.POINTER(F)]
     lib.gp_score_sequences.argtypes = [P, VP, VP, VP, F, VP, VP, VP, I, VP, VP, VP]
+    C, R = ctypes.POINTER(gp_attention_config), ctypes.POINTER(gp_head_rows)
+    lib.gp_attention.argtypes = [C, R, R, R, R, VP, VP, SZ, VP]
+    lib.gp_attention_workspace.argtypes = [C, I, ctypes.POINTER(SZ)]
+    lib.gp_attention_backward.argtypes = [C, R, R, R, R, VP, R, R, R, R, VP, VP, SZ, VP]
+    lib.gp_relative_buckets.argtypes = [I, I, I, ctypes.POINTER(ctypes.c_int)]
     lib.gp_last_error.argtypes = []
     lib.gp_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -336,6 +355,29 @@ def gp_grad_norm_workspace(n):
 def gp_adamw_step(tensors, n, cfg: gp_adamw_config, step, step_dev, factor, stream):
     """tensors: an array of gp_adamw_tensor."""
     _check(load().gp_adamw_step(tensors, n, ctypes.byref(cfg), step, step_dev, factor, stream))
+
+
+def gp_attention(cfg: gp_attention_config, q, k, v, out, lse, ws, ws_bytes, stream):
+    """q, k, v, out: gp_head_rows."""
+    _check(load().gp_attention(cfg, q, k, v, out, lse, ws, ws_bytes, stream))
+
+
+def gp_attention_workspace(cfg: gp_attention_config, backward):
+    v = ctypes.c_size_t()
+    _check(load().gp_attention_workspace(cfg, backward, ctypes.byref(v)))
+    return v.value
+
+
+def gp_attention_backward(cfg: gp_attention_config, q, k, v, out, lse, dout, dq, dk, dv, dbias, ws, ws_bytes, stream):
+    """q, k, v, out (or None), dout, dq, dk, dv: gp_head_rows."""
+    _check(load().gp_attention_backward(cfg, q, k, v, out, lse, dout, dq, dk, dv, dbias, ws, ws_bytes, stream))
+
+
+def gp_relative_buckets(buckets, max_distance, bidirectional):
+    """Bucket of each distance from -max_distance to max_distance (a list)."""
+    v = (ctypes.c_int * (2 * max(0, min(max_distance, GP_DISTANCE_MAX)) + 1))()
+    _check(load().gp_relative_buckets(buckets, max_distance, bidirectional, v))
+    return list(v)
 
 
 def gp_mfma_peak(stream=None):

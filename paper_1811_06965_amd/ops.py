@@ -2,14 +2,17 @@
 
 Beside the partition's own head and update: log probabilities of given tokens
 with entropy and alternatives (``token_logprobs``) and their gradient
-(``token_logprobs_backward``), the norm over many gradients (``grad_norm``) and
-AdamW over many tensors with states in 32 or 8 bits (``AdamW``).  Every step of
+(``token_logprobs_backward``), the norm over many gradients (``grad_norm``),
+AdamW over many tensors with states in 32 or 8 bits (``AdamW``), attention to keys of
+another length with a learned relative position bias (``attention``, ``RelativeBias``)
+and its gradients (``attention_backward``).  Every step of
 the work runs in libgp.so, on the current stream of the tensors' device;
 results and scratch memory come from torch's allocator.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional, Sequence, Union
 
 import numpy as np
@@ -62,13 +65,13 @@ def _rows(name, t):
     return rows, vocab, ld
 
 
-def _no_graph(*tensors):
+def _no_graph(*tensors, gradient="token_logprobs_backward"):
     """The operators build no autograd graph: an input whose gradient would be lost is refused."""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
                 raise ValueError("no autograd graph is built here: detach the inputs, or call under torch.no_grad(), and "
-                                 "take the gradient from token_logprobs_backward")
+                                 f"take the gradient from {gradient}")
 
 
 def _vector(name, t, rows, dtype, device):
@@ -345,3 +348,122 @@ class AdamW:
                                                  _ptr(factor), stream))
         increment_version(self._written)  # parameters that a graph saved are not those it would walk back with
         self.steps += 1
+
+
+class RelativeBias:
+    """A learned bias by relative position: table[h, bucket(key - query)] is
+    added to the scores of head h.  table: contiguous fp32 [heads, buckets], read at every
+    call (an optimiser updates it in place).  The buckets are gp_relative_buckets': half of
+    one side's hold one distance each, the others grow with the logarithm up to max_distance,
+    beyond which all share the last; bidirectional: one half for keys behind the query."""
+
+    def __init__(self, table: torch.Tensor, max_distance=128, bidirectional=True):
+        if table.dim() != 2 or table.dtype != torch.float32:
+            raise ValueError("table must be float32 [heads, buckets]")
+        dev = _gpu(table)
+        self.table, self.max_distance, self.bidirectional = table, max_distance, bidirectional
+        of = gp.gp_relative_buckets(table.shape[1], max_distance, bidirectional)
+        self.bucket_of = torch.tensor(of, dtype=torch.int32).to(dev)
+
+
+class Attention(NamedTuple):
+    out: torch.Tensor  # [batch, q_len, heads, head_dim], of the type of q
+    lse: torch.Tensor  # fp32 [batch, heads, q_len]
+
+
+class AttentionGrads(NamedTuple):
+    dq: torch.Tensor
+    dk: torch.Tensor
+    dv: torch.Tensor
+    dbias: Optional[torch.Tensor]  # fp32 [heads, buckets]; None without a bias
+
+
+def _head_rows(name, t, like, shape):
+    """gp_head_rows of a tensor [batch, len, heads, head_dim] of the type and device of `like`."""
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must be {list(shape)} in {like.dtype} on {like.device}")
+    s = t.stride()
+    if s[3] != 1 and shape[3] > 1:
+        raise ValueError(f"{name}: the features of a head must be adjacent")
+    return gp.gp_head_rows(t.data_ptr(), s[0], s[1], s[2])
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_bytes(backward, *sizes):
+    """Bytes of scratch: they depend on the sizes alone."""
+    cfg = gp.gp_attention_config(*sizes[:7], 0, 1.0)
+    if sizes[7]:
+        cfg.bias = cfg.bucket_of = 16
+        cfg.buckets, cfg.max_distance = sizes[7:]
+    return gp.gp_attention_workspace(cfg, backward)
+
+
+def _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, backward):
+    """(config, gp_head_rows of q, k and v, bytes of scratch)."""
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t.dim() != 4 or t.dtype not in DTYPE:
+            raise ValueError(f"{name} must be [batch, len, heads, head_dim] in float32 or bfloat16")
+    B, Sq, H, dh = q.shape
+    Sk, K = k.shape[1], k.shape[2]
+    dev = _gpu(q)
+    for name, t in (("q_lens", q_lens), ("k_lens", k_lens), ("q_starts", q_starts)):
+        _vector(name, t, B, torch.int32, dev)
+    cfg = gp.gp_attention_config(DTYPE[q.dtype], B, H, K, Sq, Sk, dh, causal, dh ** -0.5 if scale is None else scale,
+                                 _ptr(q_lens), _ptr(k_lens), _ptr(q_starts))
+    buckets = distance = 0
+    if bias is not None:
+        table = bias.table
+        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[0] != H or table.device != dev or not table.is_contiguous():
+            raise ValueError(f"the bias must have a contiguous float32 table of {H} heads on {dev}")
+        if bias.bucket_of.device != dev:
+            raise ValueError(f"the bias was made on {bias.bucket_of.device}")
+        buckets, distance = table.shape[1], bias.max_distance
+        cfg.bias, cfg.bucket_of, cfg.buckets, cfg.max_distance = table.data_ptr(), bias.bucket_of.data_ptr(), buckets, distance
+    like = (B, Sk, K, dh)
+    rows = (_head_rows("q", q, q, q.shape), _head_rows("k", k, q, like), _head_rows("v", v, q, like))
+    need = _attention_bytes(backward, cfg.dtype, B, H, K, Sq, Sk, dh, buckets, distance)
+    return cfg, rows, need
+
+
+def attention(q, k, v, q_lens=None, k_lens=None, q_starts=None, causal=False, scale=None,
+              bias: Optional[RelativeBias] = None) -> Attention:
+    """gp_attention: softmax(scale q k^T + bias) v of queries [batch, q_len,
+    heads, head_dim] over keys and values [batch, k_len, kv_heads, head_dim] of any strides
+    (features adjacent), kv_heads dividing heads.  q_lens, k_lens: int32 [batch], rows in
+    use of each sequence; q_starts: int32 [batch], position of the first query among the keys
+    (0), for causal and the bias.  scale: 1 / sqrt(head_dim) unless given.  Not differentiable
+    by itself: attention_backward gives the gradients."""
+    _no_graph(q, k, v, None if bias is None else bias.table, gradient="attention_backward")
+    cfg, rows, need = _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, 0)
+    dev = q.device
+    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    lse = torch.empty((cfg.batch, cfg.heads, cfg.q_len), dtype=torch.float32, device=dev)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    o = _head_rows("out", out, q, q.shape)
+    _on(dev, lambda stream: gp.gp_attention(cfg, *rows, o, lse.data_ptr(), _ptr(ws), need, stream))
+    return Attention(out, lse)
+
+
+def attention_backward(q, k, v, out, lse, dout, q_lens=None, k_lens=None, q_starts=None, causal=False, scale=None,
+                       bias: Optional[RelativeBias] = None, grads=None) -> AttentionGrads:
+    """gp_attention_backward: the gradients of sum dout out with respect to q, k,
+    v and the bias's table, from the out and lse that ``attention`` gave for the same
+    arguments.  out=None: without the rounding of out, slower.  grads: (dq, dk, dv), tensors of
+    the shapes of q, k and v that receive them; allocated otherwise."""
+    _no_graph(q, k, v, out, lse, dout, None if bias is None else bias.table, *(grads or ()), gradient="this call's results")
+    cfg, rows, need = _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, 1)
+    dev = q.device
+    if lse.shape != (cfg.batch, cfg.heads, cfg.q_len) or lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32 [batch, heads, q_len], as attention gives it")
+    o = None if out is None else _head_rows("out", out, q, q.shape)
+    g = _head_rows("dout", dout, q, q.shape)
+    if grads is None:
+        grads = [torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v)]
+    dq, dk, dv = grads
+    to = (_head_rows("dq", dq, q, q.shape), _head_rows("dk", dk, q, k.shape), _head_rows("dv", dv, q, k.shape))
+    dbias = None if bias is None else torch.empty_like(bias.table)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _on(dev, lambda stream: gp.gp_attention_backward(cfg, *rows, o, lse.data_ptr(), g, *to, _ptr(dbias), _ptr(ws), need,
+                                                     stream))
+    increment_version([dq, dk, dv])
+    return AttentionGrads(dq, dk, dv, dbias)

@@ -530,6 +530,45 @@ gp_status gp_token_logprobs_backward(int dtype, const void* logits, long rows, i
                                      const float* dlogp, const float* dentropy, void* dlogits, long ldd,
                                      gp_stream stream);
 
+/* The most tokens of a teacher that gp_distill takes of a row. */
+#define GP_DISTILL_MAX 256
+
+/*
+ * The divergence of rows of logits from a teacher that is known by its most likely tokens
+ * (top_ids and top_logp of gp_token_logprobs under the teacher's logits, for instance):
+ *   logits, scale, clip, ld : as gp_token_logprobs; p = exp(s - lse).
+ *   ids     : device int32 [rows, top], tokens in any order; GP_NO_TOKEN where a row names fewer;
+ *             any other value outside [0, vocab) makes the row's loss NaN.  top: 1 .. GP_DISTILL_MAX.
+ *   teacher : device fp32 [rows, top], their log probabilities.  What stands beside GP_NO_TOKEN is not used.
+ *   rest = 0: q = softmax of the row's named teacher values;  loss = sum q (log q - log p)
+ *   rest = 1: q = exp(teacher), Q = 1 - sum q, R = the sum of p over the tokens not named;
+ *             loss = sum q (log q - log p) + Q (log Q - log R), the last term where Q > 0 and R > 0
+ *   loss, lse, rest_lse : device fp32 [rows]; rest_lse = log sum of exp(s_v) over the tokens not named (-inf
+ *             where there is none that can occur); it may be NULL without rest.
+ *   ws      : device scratch of ws_bytes bytes, 16-byte aligned; gp_distill_workspace says how many make the call
+ *             fastest.  Fewer (0 and NULL included) change the order of the sums.
+ * A term whose q is 0 counts as 0, one whose p is 0 as +inf.  A row that names no token has loss 0.  A token that is named twice
+ * has both its weights.  A logit of -1e30 or less cannot occur, as in gp_token_logprobs; NaN and +inf give NaN.
+ * GP_ERR_INVALID_ARG: as gp_token_logprobs; top out of range, a NULL ids, teacher or output.
+ */
+gp_status gp_distill(int dtype, const void* logits, long rows, int vocab, long ld, const int* ids, const float* teacher,
+                     int top, float scale, float clip, int rest, float* loss, float* lse, float* rest_lse, void* ws,
+                     size_t ws_bytes, gp_stream stream);
+gp_status gp_distill_workspace(int dtype, long rows, int vocab, size_t* bytes);
+
+/*
+ * The gradient of sum_r dloss_r loss_r with respect to the logits, from the lse and rest_lse that gp_distill gave:
+ *   dz_v = [|z_v| <= clip] dloss scale (W p_v - q_v) for a named token,
+ *   dz_v = [|z_v| <= clip] dloss scale (W - Q / R) p_v for the others (without rest, and where its term is left out, W p_v),
+ * W the sum of the weights in the loss (the bracket only with clip > 0).  Rows that name no token, and rows with
+ * lse = -inf, have a zero gradient, a wrong id a row of NaN.
+ *   dlogits : as gp_token_logprobs_backward: [rows, vocab] in dtype, rows ldd apart, may be logits itself.
+ * GP_ERR_INVALID_ARG: as gp_distill; NULL lse, dloss, dlogits, or rest_lse with rest; an overlap.
+ */
+gp_status gp_distill_backward(int dtype, const void* logits, long rows, int vocab, long ld, const int* ids,
+                              const float* teacher, int top, float scale, float clip, int rest, const float* lse,
+                              const float* rest_lse, const float* dloss, void* dlogits, long ldd, gp_stream stream);
+
 /* One gradient of gp_grad_norm: count elements at a device address. */
 typedef struct {
     const void* grad;

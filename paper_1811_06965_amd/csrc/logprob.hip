@@ -4,15 +4,11 @@
 #include <cmath>
 
 #include "common.hpp"
+#include "logits.hpp"
 
 namespace gp {
 
 namespace {
-
-constexpr float LOG2E = 1.44269504088896341f;
-constexpr float NEVER = -1e30f;  // a logit down here is a mask's, its token cannot occur
-__host__ __device__ inline float lower_bound(float clip) { return -clip > NEVER ? -clip : NEVER; }
-constexpr int SPLIT_MAX = 32;    // workgroups of one row: at most the lanes of the wave that joins them
 
 // Sums of a row's terms around a reference logit r: with d = x - r, a = sum exp(scale d)
 // and b = sum d exp(scale d).  Then lse = scale r + log a and the entropy is
@@ -28,7 +24,6 @@ struct Part {
         return {to, fa, __builtin_fmaf(fa, d, f * b)};
     }
 };
-constexpr float NO_REF = -2e30f;  // below every reference
 // The parts of 64 lanes as one.
 __device__ __forceinline__ Part wave_join(Part p, float c2) {
     const float r = wave_reduce_f(p.r, NO_REF, [](float a, float b) { return max_nan(a, b); });
@@ -58,27 +53,6 @@ __device__ __forceinline__ u64 wave_max_key(u64 k) {
     const unsigned lo = wave_max_u((unsigned)(k >> 32) == hi ? (unsigned)k : 0u);
     return ((u64)hi << 32) | lo;
 }
-
-// A row in chunks of 16 bytes, the last one short where V asks for it.  Global memory
-// takes 16-byte accesses at any element's address.
-template <typename T> struct Chunks {
-    static constexpr int N = Vec16<T>::N;
-    typedef typename Vec16<T>::type vec __attribute__((aligned(sizeof(T))));
-    static __device__ __forceinline__ vec load(const T* row, int j) {
-        return *reinterpret_cast<const vec*>(row + (long)j * N);
-    }
-    // the values of any chunk of a row of V; `none` behind its end
-    static __device__ __forceinline__ void values(const T* row, int V, int j, float none, float (&x)[N]) {
-        if (j < V / N) {
-            const vec v = load(row, j);
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = to_f32((T)v[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = j * N + e < V ? to_f32(row[(long)j * N + e]) : none;
-        }
-    }
-};
 
 struct RowOut {
     float* logp;
@@ -453,22 +427,6 @@ __global__ void __launch_bounds__(256) logprob_grad_kernel(const T* z, int V, lo
     }
 }
 
-int chunk_count(int dtype, int vocab) {
-    const int n = dtype == GP_BF16 ? 8 : 4;
-    return vocab / n + (vocab % n ? 1 : 0);
-}
-// Workgroups of a row, joined by a second launch: several for up to 96 rows of 256 KB or
-// more, each over 16 KB or more of it and 768 in all, while one workgroup per row
-// leaves most CUs without work and takes longer for its row than the joining does.  us,
-// split / whole, bf16 with 5 alternatives: one row of 131072 9.1 / 14.8, 32 rows 10.8 / 15.3,
-// 64 rows 12.2 / 15.0 (7.4 / 11.6 with none, 16.6 / 16.2 with 20), 96 rows 13.3 / 15.2; but 128
-// rows 15.7 / 15.8, one row of 32000 8.4 / 7.4, 64 of 65536 10.6 / 10.3, and 93 of 50021 fp32
-// with 20 17.5 / 11.1 (19.2 / 12.9 with one row of masks alone, whose alternatives are all ties).
-int row_splits(int dtype, long rows, int vocab) {
-    const long chunks = chunk_count(dtype, vocab);
-    if (rows < 1 || rows > 96 || chunks < 16384) return 1;
-    return (int)std::min<long>(SPLIT_MAX, std::min(768 / rows, chunks / 1024));
-}
 // Threads of a workgroup.  Short rows take one wave, whose joins and rankings wait for
 // nobody; few rows, or rows over 128 KB, the most loads in flight, from 32 KB a row on where
 // a CU has one row at most, else from 50 KB on; in between many rows
@@ -487,15 +445,6 @@ int row_threads(long rows, int chunks, int splits, int top) {
 }
 size_t split_bytes(long rows, int splits, int top) { return (size_t)rows * splits * (sizeof(Part) + 8 * (size_t)top); }
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// Rows of `row` bytes, `pitch` apart, from two starts lie between each other (the columns of one
-// buffer) without overlapping.
-bool side_by_side(uintptr_t a, uintptr_t b, size_t row, size_t pitch) {
-    const size_t off = pitch ? (a < b ? b - a : a - b) % pitch : 0;
-    return off >= row && off + row <= pitch;
-}
-
 gp_status check_rows(int dtype, const void* logits, long rows, int vocab, long ld, float scale, float clip) {
     auto bad = [](const char* m) { return set_error(GP_ERR_INVALID_ARG, m); };
     if (dtype != GP_F32 && dtype != GP_BF16) return bad("token_logprobs: unknown dtype");
@@ -508,12 +457,6 @@ gp_status check_rows(int dtype, const void* logits, long rows, int vocab, long l
     if (!aligned(logits, dtype == GP_BF16 ? 2 : 4)) return bad("token_logprobs: logits not aligned to their elements");
     return GP_OK;
 }
-
-// Rows of a launch at most: a launch holds fewer than 2^32 threads, a workgroup of a row
-// up to 1024 of them.
-constexpr long LAUNCH_ROWS = 1L << 21;
-
-template <typename P> P* past(P* p, long n) { return p ? p + n : nullptr; }
 
 template <typename T>
 gp_status launch_rows(const T* z, long rows, int V, long ld, const int* tokens, float scale, float clip,

@@ -43,10 +43,11 @@ EXPORTS = ["gp_partition_create", "gp_partition_configure", "gp_partition_destro
            "gp_token_logprobs", "gp_token_logprobs_workspace", "gp_token_logprobs_backward", "gp_grad_norm",
            "gp_grad_norm_workspace", "gp_adamw_step", "gp_get_grad_norm", "gp_score_sequences",
            "gp_backward_microbatch_weighted", "gp_get_moment", "gp_set_moment", "gp_get_updates", "gp_set_updates",
-           "gp_attention", "gp_attention_workspace", "gp_attention_backward", "gp_relative_buckets", "gp_last_error"]
+           "gp_attention", "gp_attention_workspace", "gp_attention_backward", "gp_relative_buckets", "gp_distill",
+           "gp_distill_workspace", "gp_distill_backward", "gp_last_error"]
 
 GP_TOP_MAX, GP_NO_TOKEN, GP_STATE_BLOCK = 32, -1, 256
-GP_BUCKETS_MAX, GP_DISTANCE_MAX = 1024, 1024
+GP_BUCKETS_MAX, GP_DISTANCE_MAX, GP_DISTILL_MAX = 1024, 1024, 256
 
 
 class gp_config(ctypes.Structure):
@@ -146,6 +147,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.gp_backward_microbatch_weighted.argtypes = [P, I, VP, VP, VP, VP, VP, VP]
     lib.gp_get_grad_norm.argtypes = [P, ctypes.POINTER(F)]
     lib.gp_score_sequences.argtypes = [P, VP, VP, VP, F, VP, VP, VP, I, VP, VP, VP]
+    lib.gp_distill.argtypes = [I, VP, L, I, L, VP, VP, I, F, F, I, VP, VP, VP, VP, SZ, VP]
+    lib.gp_distill_workspace.argtypes = [I, L, I, ctypes.POINTER(SZ)]
+    lib.gp_distill_backward.argtypes = [I, VP, L, I, L, VP, VP, I, F, F, I, VP, VP, VP, VP, L, VP]
     C, R = ctypes.POINTER(gp_attention_config), ctypes.POINTER(gp_head_rows)
     lib.gp_attention.argtypes = [C, R, R, R, R, VP, VP, SZ, VP]
     lib.gp_attention_workspace.argtypes = [C, I, ctypes.POINTER(SZ)]
@@ -339,6 +343,25 @@ def gp_token_logprobs_backward(dtype, logits, rows, vocab, ld, tokens, scale, cl
                                dlogits, ldd, stream):
     _check(load().gp_token_logprobs_backward(dtype, logits, rows, vocab, ld, tokens, scale, clip, lse, entropy, dlogp,
                                              dentropy, dlogits, ldd, stream))
+
+
+def gp_distill(dtype, logits, rows, vocab, ld, ids, teacher, top, scale, clip, rest, loss, lse, rest_lse, ws, ws_bytes,
+               stream):
+    _check(load().gp_distill(dtype, logits, rows, vocab, ld, ids, teacher, top, scale, clip, rest, loss, lse, rest_lse, ws,
+                             ws_bytes, stream))
+
+
+def gp_distill_workspace(dtype, rows, vocab):
+    """Bytes of scratch with which gp_distill is fastest."""
+    v = ctypes.c_size_t()
+    _check(load().gp_distill_workspace(dtype, rows, vocab, ctypes.byref(v)))
+    return v.value
+
+
+def gp_distill_backward(dtype, logits, rows, vocab, ld, ids, teacher, top, scale, clip, rest, lse, rest_lse, dloss, dlogits,
+                        ldd, stream):
+    _check(load().gp_distill_backward(dtype, logits, rows, vocab, ld, ids, teacher, top, scale, clip, rest, lse, rest_lse,
+                                      dloss, dlogits, ldd, stream))
 
 
 def gp_grad_norm(dtype, grads, n, max_norm, norm_factor, ws, ws_bytes, stream):

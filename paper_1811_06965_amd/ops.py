@@ -2,7 +2,8 @@
 
 Beside the partition's own head and update: log probabilities of given tokens
 with entropy and alternatives (``token_logprobs``) and their gradient
-(``token_logprobs_backward``), the norm over many gradients (``grad_norm``),
+(``token_logprobs_backward``), the divergence from a teacher's most likely tokens
+(``distill``) and its gradient (``distill_backward``), the norm over many gradients (``grad_norm``),
 AdamW over many tensors with states in 32 or 8 bits (``AdamW``), attention to keys of
 another length with a learned relative position bias (``attention``, ``RelativeBias``)
 and its gradients (``attention_backward``).  Every step of
@@ -104,6 +105,17 @@ def token_logprobs(logits, tokens=None, scale=1.0, clip=0.0, top=0) -> TokenLogp
     return TokenLogprobs(logp, lse, entropy, top_ids, top_logp)
 
 
+def _gradient_of(logits, vocab, ld, out):
+    """(where the logits' gradient goes, its row stride)."""
+    if out is None:
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device), vocab
+    if out is logits:
+        return out, ld
+    if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device:
+        raise ValueError("out must have the type, shape and device of the logits")
+    return out, _rows("out", out)[2]
+
+
 def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentropy=None, scale=1.0, clip=0.0,
                             out=None):
     """gp_token_logprobs_backward: the gradient of sum dlogp logp + dentropy
@@ -115,18 +127,65 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, dlogp=None, dentr
     _vector("tokens", tokens, rows, torch.int32, dev)
     for name, t in (("lse", lse), ("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
         _vector(name, t, rows, torch.float32, dev)
-    if out is None:
-        out, ldd = torch.empty((rows, vocab), dtype=logits.dtype, device=dev), vocab
-    elif out is logits:
-        ldd = ld
-    elif out.dtype != logits.dtype or out.shape != logits.shape or out.device != dev:
-        raise ValueError("out must have the type, shape and device of the logits")
-    else:
-        ldd = _rows("out", out)[2]
+    out, ldd = _gradient_of(logits, vocab, ld, out)
     _on(dev, lambda stream: gp.gp_token_logprobs_backward(
         DTYPE[logits.dtype], logits.data_ptr(), rows, vocab, ld, _ptr(tokens), scale, clip, _ptr(lse), _ptr(entropy),
         _ptr(dlogp), _ptr(dentropy), out.data_ptr(), ldd, stream))
     increment_version(out)  # a graph that saved it must not be walked back with what it holds now
+    return out
+
+
+class Distillation(NamedTuple):
+    loss: torch.Tensor                # fp32 [rows]
+    lse: torch.Tensor                 # fp32 [rows]
+    rest_lse: Optional[torch.Tensor]  # fp32 [rows]; None without rest
+
+
+def _teacher(ids, teacher, rows, device):
+    """Tokens named per row."""
+    for name, t, kind in (("ids", ids, torch.int32), ("teacher", teacher, torch.float32)):
+        if t.dim() != 2 or t.shape[0] != rows or t.shape != ids.shape or t.dtype != kind or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {kind} [rows, top] on {device}")
+    return ids.shape[1]
+
+
+def distill(logits, ids, teacher, scale=1.0, clip=0.0, rest=True) -> Distillation:
+    """gp_distill: the divergence of rows of logits [rows, vocab] (a row stride is
+    fine) from a teacher's log probabilities, fp32 [rows, top], of the tokens ids, int32 [rows, top]
+    (``token_logprobs(teacher_logits, top=n)`` gives both; gp.GP_NO_TOKEN where a row names
+    fewer).  rest: what the teacher gives to the other tokens is one more outcome; without
+    it the named tokens' probabilities are normalised.  scale, clip: as token_logprobs.  Not
+    differentiable by itself: distill_backward gives the gradient."""
+    _no_graph(logits, teacher, gradient="distill_backward")
+    rows, vocab, ld = _rows("logits", logits)
+    dev, dt = _gpu(logits), DTYPE[logits.dtype]
+    top = _teacher(ids, teacher, rows, dev)
+    need = gp.gp_distill_workspace(dt, rows, vocab)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    loss, lse, rest_lse = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind(0)
+    if not rest:
+        rest_lse = None
+    _on(dev, lambda stream: gp.gp_distill(
+        dt, logits.data_ptr(), rows, vocab, ld, ids.data_ptr(), teacher.data_ptr(), top, scale, clip, rest, loss.data_ptr(),
+        lse.data_ptr(), _ptr(rest_lse), _ptr(ws), need, stream))
+    return Distillation(loss, lse, rest_lse)
+
+
+def distill_backward(logits, ids, teacher, lse, dloss, rest_lse=None, scale=1.0, clip=0.0, rest=True, out=None):
+    """gp_distill_backward: the gradient of sum dloss loss with respect to the
+    logits, from the lse and rest_lse that ``distill`` gave for the same arguments.  out: where it
+    goes (may be logits itself); allocated otherwise."""
+    _no_graph(logits, teacher, lse, dloss, rest_lse, out, gradient="this call's result")
+    rows, vocab, ld = _rows("logits", logits)
+    dev = _gpu(logits)
+    top = _teacher(ids, teacher, rows, dev)
+    for name, t in (("lse", lse), ("dloss", dloss), ("rest_lse", rest_lse)):
+        _vector(name, t, rows, torch.float32, dev)
+    out, ldd = _gradient_of(logits, vocab, ld, out)
+    _on(dev, lambda stream: gp.gp_distill_backward(
+        DTYPE[logits.dtype], logits.data_ptr(), rows, vocab, ld, ids.data_ptr(), teacher.data_ptr(), top, scale, clip, rest,
+        _ptr(lse), _ptr(rest_lse), _ptr(dloss), out.data_ptr(), ldd, stream))
+    increment_version(out)
     return out
 
 

@@ -5,6 +5,7 @@
 #include <cfloat>
 #include <cmath>
 #include <cstdio>
+#include <type_traits>
 
 #include "attention_rows.hpp"
 #include "common.hpp"
@@ -128,61 +129,57 @@ template <typename T, int DH, int R> struct Tile {
     // where an unmasked pair holds +inf or -inf (a NaN counts as both), which is then added.
     static __device__ __forceinline__ f32x16 unmasked(const char* s, int row0, int cc, int d0, const f32x16& w, int lane,
                                                       f32x16 acc) {
-        f32x16 up = zero16(), down = zero16();
-        auto split = [](float x, float& p, float& n) {
-            p = x == INFINITY || x != x ? 1.f : 0.f;
-            n = x == -INFINITY || x != x ? 1.f : 0.f;
-            return p + n > 0.f ? 0.f : x;
-        };
+        const auto infinite = [](float x, float which) { return x == which || x != x; };
+        const auto finite = [](float x) { return x - x == 0.f ? x : 0.f; };
+        f32x16 found;
         if constexpr (sizeof(T) == 2) {
             const bf16x8 x = column(s, row0, cc, d0, lane);
-            bf16x8 f, p, n, b, seen;
+            bf16x8 f, b, seen;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float u, d;
-                f[e] = (bf16)split((float)x[e], u, d);
-                p[e] = (bf16)u;
-                n[e] = (bf16)d;
                 const bool m = w[8 * cc + e] == -INFINITY;
+                f[e] = (bf16)finite((float)x[e]);
                 b[e] = (bf16)(m ? 0.f : w[8 * cc + e]);
                 seen[e] = (bf16)(m ? 0.f : 1.f);
             }
             acc = mma(f, b, acc);
-            up = mma(p, seen, up);
-            down = mma(n, seen, down);
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const float inf = which ? -INFINITY : INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = (bf16)(infinite((float)x[e], inf) ? 1.f : 0.f);
+                found = mma(f, seen, zero16());
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] = found[e] > 0.f ? acc[e] + inf : acc[e];
+            }
         } else {
+            float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float u, d;
-                const float f = split(element(s, row0 + acc_row(8 * cc + e, lane), d0, lane), u, d);
-                const bool m = w[8 * cc + e] == -INFINITY;
-                const float seen = m ? 0.f : 1.f;
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(f, m ? 0.f : w[8 * cc + e], acc, 0, 0, 0);
-                up = __builtin_amdgcn_mfma_f32_32x32x2f32(u, seen, up, 0, 0, 0);
-                down = __builtin_amdgcn_mfma_f32_32x32x2f32(d, seen, down, 0, 0, 0);
+                x[e] = element(s, row0 + acc_row(8 * cc + e, lane), d0, lane);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(finite(x[e]), w[8 * cc + e] == -INFINITY ? 0.f : w[8 * cc + e], acc, 0, 0, 0);
             }
-        }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            acc[e] = up[e] > 0.f ? acc[e] + INFINITY : acc[e];
-            acc[e] = down[e] > 0.f ? acc[e] - INFINITY : acc[e];
+            for (int which = 0; which < 2; ++which) {
+                const float inf = which ? -INFINITY : INFINITY;
+                found = zero16();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    found = __builtin_amdgcn_mfma_f32_32x32x2f32(infinite(x[e], inf) ? 1.f : 0.f, w[8 * cc + e] == -INFINITY ? 0.f : 1.f, found, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] = found[e] > 0.f ? acc[e] + inf : acc[e];
+            }
         }
         return acc;
     }
     // acc += the tile's 32 rows from row0 on, transposed, times w.
-    template <int ND>
-    static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, int lane, bool careful, f32x16 (&acc)[ND]) {
-        if (careful) {
+    template <bool CAREFUL, int ND>
+    static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, int lane, f32x16 (&acc)[ND]) {
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc)
+        for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = unmasked(s, row0, cc, d * 32, w, lane, acc[d]);
-        } else {
-#pragma unroll
-            for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) acc[d] = transposed(s, row0, cc, d * 32, w, lane, acc[d]);
-        }
+            for (int d = 0; d < ND; ++d)
+                acc[d] = CAREFUL ? unmasked(s, row0, cc, d * 32, w, lane, acc[d]) : transposed(s, row0, cc, d * 32, w, lane, acc[d]);
     }
 };
 
@@ -211,6 +208,15 @@ __device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[ND], fl
             for (int e = 0; e < 4; ++e) t[e] = to_elt<T>(f == 0.f ? 0.f : acc[db][4 * rg + e] * f);
             if (d < dh) *reinterpret_cast<vec*>(row + d * (int)sizeof(T)) = t;
         }
+}
+
+template <int ND> __device__ __forceinline__ bool all_finite(const f32x16 (&x)[ND]) {
+    float z = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z = __builtin_fmaf(x[d][e], 0.f, z);
+    return z == 0.f;
 }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -325,7 +331,8 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
     f32x16 o[ND];
     // A product of a masked pair's weight 0 with an infinity or a NaN is a NaN: where a mask may lie inside a block and
     // something not finite came out, a second, careful pass leaves those products out.
-    for (bool careful = false;; careful = true) {
+    auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
         m = NO_REF;
         l = 0.f;
 #pragma unroll
@@ -380,24 +387,20 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
-                const bool slow = careful && (edge || masks);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float x = s[kb][e], p = exp2_hw(BIAS ? x - m : __builtin_fmaf(x, c, -m));
                     sum[e & 3] += p;
-                    s[kb][e] = slow && x == -INFINITY ? x : p;
+                    s[kb][e] = CAREFUL && x == -INFINITY ? x : p;
                 }
-                Tl::add(vs, kb * 32, s[kb], lane, slow, o);
+                Tl::template add<CAREFUL>(vs, kb * 32, s[kb], lane, o);
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
-        if (careful || !(a.causal || masks)) break;
-        float z = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z = __builtin_fmaf(o[d][e], 0.f, z);
-        if (!__syncthreads_or(z != 0.f)) break;
+    };
+    pass(std::false_type{});
+    if (a.causal || masks) {
+        if (__syncthreads_or(!all_finite(o))) pass(std::true_type{});
     }
     l = both_sum(l);
     if (!in) return;
@@ -596,7 +599,8 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         lds_barrier();
     }
     f32x16 dq[ND];
-    for (bool careful = false;; careful = true) {
+    auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
         if (BIAS && a.dist) dist.clear();
 #pragma unroll
         for (int d = 0; d < ND; ++d) dq[d] = zero16();
@@ -607,31 +611,28 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
             if (t + 1 < t1) stage(t + 1);
             if (t * KT >= kw) continue;
             const char *ks = lds + (t & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
-            const bool edge = tile_edge(t), slow = careful && (edge || masks);
-#pragma unroll
+            const bool edge = tile_edge(t);
+#pragma unroll 1
             for (int kb = 0; kb < NB; ++kb) {
                 f32x16 s, dp;
-                block(ks, vs, t * KT + kb * 32, kb, edge, slow, s, dp);
+                block(ks, vs, t * KT + kb * 32, kb, edge, CAREFUL, s, dp);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float d = s[e] * (dp[e] - delta);
-                    s[e] = !slow ? d : s[e] == -INFINITY ? s[e] : d == -INFINITY ? NAN : d;
+                    s[e] = !CAREFUL ? d : s[e] == -INFINITY ? s[e] : d == -INFINITY ? NAN : d;
                 }
-                Tl::add(ks, kb * 32, s, lane, slow, dq);
-                if (slow) {
+                Tl::template add<CAREFUL>(ks, kb * 32, s, lane, dq);
+                if (CAREFUL) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[e] = s[e] == -INFINITY ? 0.f : s[e];
                 }
                 if (BIAS && a.dist) dist.add(s, t * KT + kb * 32 - pos0 - 31);
             }
         }
-        if (careful || !(a.causal || masks)) break;
-        float z = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z = __builtin_fmaf(dq[d][e], 0.f, z);
-        if (!__syncthreads_or(z != 0.f)) break;
+    };
+    pass(std::false_type{});
+    if (a.causal || masks) {
+        if (__syncthreads_or(!all_finite(dq))) pass(std::true_type{});
     }
     if (in) store_row<T, ND>(a.dq.at(wk.b, i, wk.h), dq, live ? a.scale : 0.f, a.dh, lane);
     if (lane < 32 && i < a.stat_rows) a.stats[stat + i] = f32x2{lse2, delta};
@@ -678,7 +679,8 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
     const float c = a.scale * LOG2E;
     bool masks = false;
     f32x16 dk[ND], dv[ND];
-    for (bool careful = false;; careful = true) {
+    auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
         for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zero16();
         for (int g = 0; g < group; ++g) {
@@ -703,8 +705,8 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                 const int pos0 = t * QT + len.start;
                 if (k0 >= len.k || (a.causal && pos0 + QT - 1 < k0)) continue;
                 const char *qs = lds + (t & 1) * 2 * Tl::BYTES, *gs = qs + Tl::BYTES;
-                const bool edge = t * QT + QT > len.q || (a.causal && pos0 < k0 + 31), slow = careful && (edge || masks);
-#pragma unroll
+                const bool edge = t * QT + QT > len.q || (a.causal && pos0 < k0 + 31);
+#pragma unroll 1
                 for (int qb = 0; qb < NB; ++qb) {
                     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
@@ -724,26 +726,23 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                         const float bias = !BIAS ? 0.f : n.far ? n.value : n.at[-((e >> 2) * 8 + (e & 3))];
                         float p = exp2_hw(BIAS ? __builtin_fmaf(s[e], c, bias) - row[0] : __builtin_fmaf(s[e], c, -row[0]));
                         float d = p * (dp[e] - row[1]);
-                        if (slow && d == -INFINITY) d = NAN;
+                        if (CAREFUL && d == -INFINITY) d = NAN;
                         if ((edge && (acc_row(e, lane) < r0 || acc_row(e, lane) >= r1)) || (BIAS && masks && bias == -INFINITY)) {
-                            p = slow ? -INFINITY : 0.f;
+                            p = CAREFUL ? -INFINITY : 0.f;
                             d = p;
                         }
                         s[e] = p;
                         ds[e] = d;
                     }
-                    Tl::add(gs, qb * 32, s, lane, slow, dv);
-                    Tl::add(qs, qb * 32, ds, lane, slow, dk);
+                    Tl::template add<CAREFUL>(gs, qb * 32, s, lane, dv);
+                    Tl::template add<CAREFUL>(qs, qb * 32, ds, lane, dk);
                 }
             }
         }
-        if (careful || !(a.causal || masks)) break;
-        float z = 0.f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z = __builtin_fmaf(dk[d][e], 0.f, __builtin_fmaf(dv[d][e], 0.f, z));
-        if (!__syncthreads_or(z != 0.f)) break;
+    };
+    pass(std::false_type{});
+    if (a.causal || masks) {
+        if (__syncthreads_or(!all_finite(dk) || !all_finite(dv))) pass(std::true_type{});
     }
     if (!in) return;
     store_row<T, ND>(a.dk.at(wk.b, key, wk.h), dk, live ? a.scale : 0.f, a.dh, lane);
@@ -757,6 +756,7 @@ __global__ void __launch_bounds__(256) distance_rows(const float* __restrict__ i
     const long r0 = x * STEP, r1 = min(n, r0 + STEP);
     for (int d = threadIdx.x; d < width; d += 256) {
         float s = 0.f;
+#pragma unroll 8
         for (long r = r0; r < r1; ++r) s += in[(y * n + r) * width + d];
         out[(y * steps + x) * width + d] = s;
     }
@@ -769,15 +769,18 @@ __global__ void __launch_bounds__(256) distance_buckets(const float* __restrict_
     int* of = reinterpret_cast<int*>(sums + width);
     for (int d = threadIdx.x; d < width; d += 256) {
         float s = 0.f;
+#pragma unroll 8
         for (long r = 0; r < n; ++r) s += in[(blockIdx.x * n + r) * width + d];
         sums[d] = s;
         of[d] = min(max(a.bucket_of[d], 0), a.buckets - 1);
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < a.buckets; b += 256) {
+    const int lane = threadIdx.x & 63;
+    for (int b = threadIdx.x >> 6; b < a.buckets; b += 4) {  // a wave per bucket
         float s = 0.f;
-        for (int d = 0; d < width; ++d) s += of[d] == b ? sums[d] : 0.f;
-        a.dbias[(long)blockIdx.x * a.buckets + b] = s;
+        for (int d = lane; d < width; d += WAVE) s += of[d] == b ? sums[d] : 0.f;
+        s = wave_sum(s);
+        if (lane == 0) a.dbias[(long)blockIdx.x * a.buckets + b] = s;
     }
 }
 
@@ -835,7 +838,7 @@ gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
 }
 template <typename T, int DH, int W, bool BIAS>
 gp_status launch_dkv(const AttendArgs& a, hipStream_t st) {
-    constexpr int QT = 32;
+    constexpr int QT = tile_rows<T>();
     const size_t bytes = 4 * Tile<T, DH, QT>::BYTES + 2 * QT * 8 + (BIAS ? (2 * (a.max_distance + PAD) + 1) * 4 : 0);
     auto* k = attend_dkv<T, DH, QT, W, BIAS>;
     if (bytes > 65536) GP_HIP(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));

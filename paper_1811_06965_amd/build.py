@@ -41,7 +41,8 @@ def sources():
 # with the accumulators in AGPRs each value costs a v_accvgpr_read first, so
 # their MFMAs write ordinary VGPRs instead (the register file is unified on
 # gfx950).
-EXTRA_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attention_mfma.hip", "attention_rows.hip")}
+EXTRA_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attention_mfma.hip", "attention_rows_bf16.hip",
+                                                                  "attention_rows_f32.hip")}
 
 
 def _compile(cc, src):

@@ -25,11 +25,27 @@ struct AttendArgs {
     int buckets = 0, max_distance = 0;
     float* dbias = nullptr;
     // set by the launchers
-    int waves = 0, pack = 1, blocks = 0, splits = 1, stat_rows = 0;
-    float* part = nullptr;   // splits' sums: [splits][B H Sq][width], then their (reference, sum) pairs
+    int keys = 0, pack = 1, blocks = 0, splits = 1, stat_rows = 0;
+    float* part = nullptr;   // splits' sums: [splits][B H Sq][width], the forward's then followed by their (reference, sum) pairs
     f32x2* stats = nullptr;  // (lse / log 2, delta) of each row: [B, H, stat_rows]
-    float* dist = nullptr;   // sums of dS by distance: [H][B blocks][2 max_distance + 1]
+    float* dist = nullptr;   // sums of dS by distance: [H][B blocks splits][2 max_distance + 1]
 };
+
+// How a kernel's work is split.
+struct Shape {
+    bool keys = false;  // few rows: the waves of a workgroup share them and take a part of the keys each
+    int pack = 1;       // heads whose rows are packed together
+    int blocks = 1;     // of rows
+    int splits = 1;     // workgroups of one block
+};
+constexpr int BW = 4;  // waves of the backward's workgroups
+constexpr int head_bucket(int dh) { return (dh + 31) / 32 * 32; }           // features that a kernel is made for
+constexpr int tile_rows(int esize) { return esize == 2 ? 64 : 32; }          // rows of a tile in LDS
+constexpr int key_waves(int row_bytes) { return row_bytes <= 128 ? 8 : row_bytes <= 256 ? 4 : 2; }
+
+// The kernels for one type.
+template <typename T> gp_status attend_forward_as(const AttendArgs& a, hipStream_t st);
+template <typename T> gp_status attend_backward_as(const AttendArgs& a, bool exact, const Shape& dq, const Shape& dkv, hipStream_t st);
 
 // Bytes of scratch, and the calls.  exact: delta from the probabilities, not from out.
 size_t attend_workspace(const AttendArgs& a);

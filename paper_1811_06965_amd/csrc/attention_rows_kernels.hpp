@@ -1,0 +1,939 @@
+// attention_rows_kernels.hpp -- attention on the caller's tensors: queries against
+// keys of another length, ragged batches, heads that share keys, a learned
+// relative position bias by buckets, and the gradients of all of them.
+#pragma once
+
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+#include "attention_rows.hpp"
+#include "common.hpp"
+#include "gemm_tile.hpp"
+
+namespace gp {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+constexpr float NEVER = -1e30f;     // a bias down here is a mask's
+constexpr float NO_REF = -FLT_MAX;  // the reference of a row that has seen no score
+constexpr float AHEAD = 8.f;        // a row's sums change their reference when a score is 2^8 ahead of it
+
+// 16 bytes of one row: the unit in which rows are staged and multiplied.
+template <typename T> struct Elt;
+template <> struct Elt<bf16> {
+    typedef bf16x8 frag;
+    static constexpr int E = 8;    // elements of a chunk
+    static constexpr int RC = 64;  // features of a 128-byte row of an LDS tile
+};
+template <> struct Elt<float> {
+    typedef f32x4 frag;
+    static constexpr int E = 4, RC = 32;
+};
+
+// c += a b over two chunks of features (lanes 0-31 hold the first, 32-63 the second): one
+// product of depth 16 in bf16, four of depth 2 in fp32, whose order of features is
+// the same on both sides.
+__device__ __forceinline__ f32x16 mma(const bf16x8& a, const bf16x8& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const f32x4& a, const f32x4& b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+// Row (within a block of 32) of accumulator register r; the column is lane % 32.
+__device__ __forceinline__ int acc_row(int r, int lane) { return (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3); }
+
+// An LDS tile of R rows x DH features: DH / RC parts of R rows of 128 bytes without padding.
+// The 16-byte chunk c of row r lies at chunk c ^ swizzle(r) of its row: 16 lanes that read the
+// same chunk of 16 consecutive rows, and a half-wave that reads four chunks of four
+// consecutive rows (the transposing reads), then fall into distinct banks.
+__device__ __forceinline__ int swizzle(int r) { return (((r >> 1) & 1) << 2) | ((r >> 2) & 3); }
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16* LdsV4;
+
+template <typename T, int DH, int R> struct Tile {
+    typedef Elt<T> X;
+    typedef typename X::frag frag;
+    static constexpr int PARTS = (DH + X::RC - 1) / X::RC, BYTES = R * PARTS * 128, LOADS = R * PARTS / 8;
+
+    // Loads that one of W waves issues for a tile, 1 KB each straight into LDS: offset of this
+    // lane's chunk in each, out of the buffer's range where the head is narrower than DH.
+    template <int W> struct Loader {
+        static_assert(LOADS % W == 0, "loads of a wave");
+        static constexpr int N = LOADS / W;
+        uint32_t off[N];
+        __device__ __forceinline__ Loader(long row_bytes, int dh, int wave, int lane) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int n = wave * N + i, r = n % (R / 8) * 8 + (lane >> 3);
+                const int f = n / (R / 8) * X::RC + ((lane & 7) ^ swizzle(r)) * X::E;
+                off[i] = f < dh ? (uint32_t)(r * row_bytes) + f * (int)sizeof(T) : OOB;
+            }
+        }
+        // Rows behind `rows` are filled with zeros (they lie behind the buffer's end).
+        __device__ __forceinline__ void operator()(char* s, const char* p, int rows, long row_bytes, int dh, int wave) const {
+            const Rsrc rs = make_rsrc(p, rows > 0 ? (uint32_t)((min(rows, R) - 1) * row_bytes) + dh * (int)sizeof(T) : 0u);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(s + (wave * N + i) * 1024), 16, (int)off[i], 0, 0, 0);
+        }
+    };
+    // Chunks 2 ks, 2 ks + 1 lie within the head; what lies behind it are zeros, which fp32's slow products leave out.
+    static __device__ __forceinline__ bool has(int ks, int dh) { return sizeof(T) == 2 || 2 * ks * X::E < dh; }
+    // Operand of 32 rows over the chunks 2 ks, 2 ks + 1 of features.
+    static __device__ __forceinline__ frag rows(const char* s, int row0, int ks, int lane) {
+        const int r = row0 + (lane & 31);
+        return *reinterpret_cast<const frag*>(s + (ks >> 2) * (R * 128) + r * 128 + (((((ks & 3) << 1) | (lane >> 5)) ^ swizzle(r)) << 4));
+    }
+    // acc (32 features from d0 on x lane's column) += the tile's rows row0 + 16 cc .. + 15, transposed, times the
+    // accumulator registers 8 cc .. 8 cc + 7 of `w`, whose rows those are.  In bf16 one transposing read gives a lane
+    // four rows of its feature, and w is rounded to bf16, the matrix unit's type: by up to 2^-8 of each weight,
+    // while their sums stay in fp32.
+    static __device__ __forceinline__ bf16x8 column(const char* s, int row0, int cc, int d0, int lane) {
+        const int g = lane >> 4, q = lane & 15;
+        const int row = row0 + 16 * cc + 4 * (g >> 1) + (q >> 2), col = (d0 & 63) + 16 * (g & 1) + 4 * (q & 3);
+        const char* p = s + (d0 >> 6) * (R * 128) + (col & 7) * 2;
+        auto at = [&](int r) { return (LdsV4)(p + r * 128 + (((col >> 3) ^ swizzle(r)) << 4)); };
+        const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row)));
+        const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row + 8)));
+        return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    }
+    static __device__ __forceinline__ float element(const char* s, int r, int d0, int lane) {
+        return *reinterpret_cast<const float*>(s + (d0 >> 5) * (R * 128) + (lane & 3) * 4 + r * 128 +
+                                               ((((lane & 31) >> 2) ^ swizzle(r)) << 4));
+    }
+    static __device__ __forceinline__ f32x16 transposed(const char* s, int row0, int cc, int d0, const f32x16& w, int lane,
+                                                        f32x16 acc) {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 b;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) b[e] = (bf16)w[8 * cc + e];
+            return mma(column(s, row0, cc, d0, lane), b, acc);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(element(s, row0 + acc_row(8 * cc + e, lane), d0, lane), w[8 * cc + e], acc, 0, 0, 0);
+            return acc;
+        }
+    }
+    // The same without the pairs marked by a weight of -INFINITY: what a masked row holds, infinities and NaN included,
+    // does not reach the sum.  The finite values are multiplied as above; two more products with weights of 1 find
+    // where an unmasked pair holds +inf or -inf (a NaN counts as both), which is then added.
+    static __device__ __forceinline__ f32x16 unmasked(const char* s, int row0, int cc, int d0, const f32x16& w, int lane,
+                                                      f32x16 acc) {
+        const auto infinite = [](float x, float which) { return x == which || x != x; };
+        const auto finite = [](float x) { return x - x == 0.f ? x : 0.f; };
+        f32x16 found;
+        if constexpr (sizeof(T) == 2) {
+            const bf16x8 x = column(s, row0, cc, d0, lane);
+            bf16x8 f, b, seen;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool m = w[8 * cc + e] == -INFINITY;
+                f[e] = (bf16)finite((float)x[e]);
+                b[e] = (bf16)(m ? 0.f : w[8 * cc + e]);
+                seen[e] = (bf16)(m ? 0.f : 1.f);
+            }
+            acc = mma(f, b, acc);
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const float inf = which ? -INFINITY : INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = (bf16)(infinite((float)x[e], inf) ? 1.f : 0.f);
+                found = mma(f, seen, zero16());
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] = found[e] > 0.f ? acc[e] + inf : acc[e];
+            }
+        } else {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = element(s, row0 + acc_row(8 * cc + e, lane), d0, lane);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(finite(x[e]), w[8 * cc + e] == -INFINITY ? 0.f : w[8 * cc + e], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const float inf = which ? -INFINITY : INFINITY;
+                found = zero16();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    found = __builtin_amdgcn_mfma_f32_32x32x2f32(infinite(x[e], inf) ? 1.f : 0.f, w[8 * cc + e] == -INFINITY ? 0.f : 1.f, found, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] = found[e] > 0.f ? acc[e] + inf : acc[e];
+            }
+        }
+        return acc;
+    }
+    // acc += the tile's 32 rows from row0 on, transposed, times w.
+    template <bool CAREFUL, int ND>
+    static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, int lane, f32x16 (&acc)[ND]) {
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                acc[d] = CAREFUL ? unmasked(s, row0, cc, d * 32, w, lane, acc[d]) : transposed(s, row0, cc, d * 32, w, lane, acc[d]);
+    }
+};
+
+// Operand of 32 rows in memory: the chunk of each feature step of this lane's row (zeros where it has none).
+template <typename T, int NK>
+__device__ __forceinline__ void load_row(const char* row, bool live, int dh, int lane, typename Elt<T>::frag (&f)[NK]) {
+    typedef Elt<T> X;
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) {
+        const int c = (2 * ks + (lane >> 5)) * X::E;
+        typename X::frag z = {};
+        f[ks] = live && c < dh ? *reinterpret_cast<const typename X::frag*>(row + c * (int)sizeof(T)) : z;
+    }
+}
+// This lane's row of a transposed accumulator (features x rows), times f, four features at a time.
+template <typename T, int ND>
+__device__ __forceinline__ void store_row(char* row, const f32x16 (&acc)[ND], float f, int dh, int lane) {
+    typedef T vec __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int rg = 0; rg < 4; ++rg) {
+            const int d = db * 32 + rg * 8 + (lane >> 5) * 4;
+            vec t;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = to_elt<T>(f == 0.f ? 0.f : acc[db][4 * rg + e] * f);
+            if (d < dh) *reinterpret_cast<vec*>(row + d * (int)sizeof(T)) = t;
+        }
+}
+
+template <int ND> __device__ __forceinline__ bool all_finite(const f32x16 (&x)[ND]) {
+    float z = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z = __builtin_fmaf(x[d][e], 0.f, z);
+    return z == 0.f;
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Of lanes l and l + 32 both: the larger value, the sum.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, WAVE); }
+__device__ __forceinline__ float both_max(float x) { return fmaxf(x, other_half(x)); }
+__device__ __forceinline__ float both_sum(float x) { return x + other_half(x); }
+
+// Every LDS read of this wave has returned, and none is moved across.
+__device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Lengths and the position of the first query of one sequence.
+struct Lens {
+    int q, k, start;
+    __device__ __forceinline__ Lens(const AttendArgs& a, int b) {
+        q = a.q_lens ? min(max(a.q_lens[b], 0), a.Sq) : a.Sq;
+        k = a.k_lens ? min(max(a.k_lens[b], 0), a.Sk) : a.Sk;
+        // beyond 2^29 every key is further than any table reaches, on the same side
+        start = a.q_starts ? min(max(a.q_starts[b], -(1 << 29)), 1 << 29) : 0;
+    }
+    // Keys that the query rows up to `last` may see.
+    __device__ __forceinline__ int keys(bool causal, int last) const {
+        return causal ? min(k, max(0, last + start + 1)) : k;
+    }
+};
+
+// The bias of one head by distance, in LDS, in units of log 2: PAD further places on either side hold the outermost
+// values, so that a block of 32 x 32 pairs that any distance of the table meets needs no clamping.  A bias of NEVER
+// or less is -INFINITY.
+constexpr int PAD = 64;
+__device__ __forceinline__ int table_size(const AttendArgs& a) { return 2 * (a.max_distance + PAD) + 1; }
+__device__ __forceinline__ bool load_table(float* t, const AttendArgs& a, int h, int tid, int threads) {
+    bool masks = false;
+    for (int i = tid; i < table_size(a); i += threads) {
+        const int d = min(max(i - PAD, 0), 2 * a.max_distance);
+        const float x = a.bias[(long)h * a.buckets + min(max(a.bucket_of[d], 0), a.buckets - 1)];
+        t[i] = x <= NEVER ? -INFINITY : x * LOG2E;
+        masks = masks || x <= NEVER;
+    }
+    return masks;
+}
+// One block of 32 x 32 pairs whose distances (key - position) go from lo to lo + 62 over the block: where they all lie
+// beyond the table on one side, one value.
+struct Near {
+    bool far;
+    float value;       // far: of every pair
+    const float* at;   // near: of this lane's register 0; register r lies step * (row r - row 0) further
+    __device__ __forceinline__ Near(const float* t, const AttendArgs& a, int lo, int mine) {
+        far = lo >= a.max_distance || lo + 62 <= -a.max_distance;
+        value = t[lo >= a.max_distance ? 2 * (a.max_distance + PAD) : 0];
+        at = t + (far ? 0 : mine + a.max_distance + PAD);
+    }
+};
+
+// Workgroup -> (sequence, head, block of rows, split); the blocks of a head are neighbours on one XCD, whose L2 then
+// serves its keys and values to all of them.
+struct Work {
+    int b, h, blk, split;
+    __device__ __forceinline__ Work(int blocks, int heads, int splits, bool reverse) {
+        int id = xcd_order(blockIdx.x, gridDim.x);
+        split = id % splits;
+        id /= splits;
+        blk = id % blocks;
+        if (reverse) blk = blocks - 1 - blk;  // the longest first
+        id /= blocks;
+        h = id % heads;
+        b = id / heads;
+    }
+};
+
+// ------------------------------------------------------------------ forward
+// A wave owns 32 query rows and goes through the keys once, in tiles of KT that the workgroup's W waves stage in LDS,
+// the next tile on its way while this one is used.  S^T = K Q^T puts a query's scores into one lane and its neighbour
+// half a wave on, so that the softmax needs one exchange per tile; P^T is then already the operand of O^T += V^T P^T.
+// Each row keeps its sums around a reference score, which follows the largest one only where that is 2^8 ahead: most
+// tiles rescale nothing.
+// Few rows (KEYS): the W waves own the same 32 rows and every W-th tile each, without barriers, and join their sums in LDS.
+template <typename T, int DH, int KT, int W, bool BIAS, bool KEYS>
+__global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
+    typedef Tile<T, DH, KT> Tl;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, LW = KEYS ? 1 : W;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    float* const table = reinterpret_cast<float*>(lds + (KEYS ? 4 * W : 4) * Tl::BYTES);
+    const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
+    const Work wk(a.blocks, a.H / a.pack, a.splits, a.causal != 0);
+    const Lens len(a, wk.b);
+    const int rows = a.Sq * a.pack, row0 = KEYS ? wk.blk * 32 : (wk.blk * W + wave) * 32, r = row0 + (lane & 31);
+    const int i = a.pack == 1 ? r : r / a.pack, h = a.pack == 1 ? wk.h : wk.h * a.pack + (r - i * a.pack);
+    const int hk = a.pack == 1 ? wk.h / (a.H / a.HK) : wk.h;
+    const bool in = r < rows, live = in && i < len.q;
+    const int pos = i + len.start, pos0 = row0 / a.pack + len.start;
+
+    bool masks = false;
+    if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
+    typename Elt<T>::frag qf[NK];
+    load_row<T>(a.q.at(wk.b, min(i, a.Sq - 1), min(h, a.H - 1)), live, a.dh, lane, qf);
+
+    // keys that any row of the workgroup, and of this wave, may see
+    auto reach = [&](int first, int end) {
+        return first >= rows || first / a.pack >= len.q ? 0 : len.keys(a.causal, (min(end, rows) - 1) / a.pack);
+    };
+    const int kw = reach(row0, row0 + 32);
+    const int tiles = ((KEYS ? kw : reach(wk.blk * W * 32, (wk.blk + 1) * W * 32)) + KT - 1) / KT;
+    const int t0 = (int)((long)tiles * wk.split / a.splits), t1 = (int)((long)tiles * (wk.split + 1) / a.splits);
+    const char *kp = a.k.at(wk.b, 0, hk), *vp = a.v.at(wk.b, 0, hk);
+    const typename Tl::template Loader<LW> kl(a.k.row, a.dh, KEYS ? 0 : wave, lane), vl(a.v.row, a.dh, KEYS ? 0 : wave, lane);
+    const int own = KEYS ? wave : 0, step = KEYS ? W : 1;  // tiles of this wave: from t0 + own on, every step-th
+    char* const base = lds + own * 4 * Tl::BYTES;
+    auto stage = [&](int t) {
+        char* s = base + ((t - t0) / step & 1) * 2 * Tl::BYTES;
+        kl(s, kp + (long)t * KT * a.k.row, len.k - t * KT, a.k.row, a.dh, KEYS ? 0 : wave);
+        vl(s + Tl::BYTES, vp + (long)t * KT * a.v.row, len.k - t * KT, a.v.row, a.dh, KEYS ? 0 : wave);
+    };
+
+    const float c = a.scale * LOG2E;
+    float m, l;
+    f32x16 o[ND];
+    // A product of a masked pair's weight 0 with an infinity or a NaN is a NaN: where a mask may lie inside a block and
+    // something not finite came out, a second, careful pass leaves those products out.
+    auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        m = NO_REF;
+        l = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[d] = zero16();
+        if (t0 + own < t1) stage(t0 + own);
+        for (int t = t0 + own; t < t1; t += step) {
+            wait_vmcnt<0>();
+            if (KEYS) lds_reads_done(); else lds_barrier();
+            if (t + step < t1) stage(t + step);
+            if (t * KT >= kw) continue;
+            const char *ks = base + ((t - t0) / step & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
+            f32x16 s[NB];
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                s[kb] = zero16();
+#pragma unroll
+                for (int x = 0; x < NK; ++x)
+                    if (Tl::has(x, a.dh)) s[kb] = mma(Tl::rows(ks, kb * 32, x, lane), qf[x], s[kb]);
+            }
+            const bool edge = t * KT + KT > len.k || (a.causal && t * KT + KT - 1 > pos0);
+            float tm = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                const int k0 = t * KT + kb * 32;
+                if (BIAS) {
+                    const Near n(table, a, k0 - pos0 - 31, k0 + 4 * (lane >> 5) - pos);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float bias = n.far ? n.value : n.at[(e >> 2) * 8 + (e & 3)];
+                        const float x = __builtin_fmaf(s[kb][e], c, bias);
+                        s[kb][e] = masks && bias == -INFINITY ? bias : x;
+                    }
+                }
+                if (edge) {
+                    const int last = a.causal ? min(len.k - 1, pos) : len.k - 1;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (k0 + acc_row(e, lane) > last) s[kb][e] = -INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) tm = fmaxf(tm, s[kb][e]);
+            }
+            tm = both_max(BIAS ? tm : tm * c);
+            if (__any(tm > m + AHEAD)) {
+                const float mn = fmaxf(m, tm), f = exp2_hw(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[d][e] *= f;
+            }
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float x = s[kb][e], p = exp2_hw(BIAS ? x - m : __builtin_fmaf(x, c, -m));
+                    sum[e & 3] += p;
+                    s[kb][e] = CAREFUL && x == -INFINITY ? x : p;
+                }
+                Tl::template add<CAREFUL>(vs, kb * 32, s[kb], lane, o);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        }
+    };
+    pass(std::false_type{});
+    if (a.causal || masks) {
+        if (__syncthreads_or(!all_finite(o))) pass(std::true_type{});
+    }
+    l = both_sum(l);
+    if constexpr (KEYS) {
+        lds_reads_done();
+        float* sums = reinterpret_cast<float*>(base);  // [row][DH], in place of this wave's tiles
+        f32x2* stat = reinterpret_cast<f32x2*>(lds + W * 4 * Tl::BYTES + (BIAS ? table_size(a) * 4 + 4 : 0)) + wave * 32;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int rg = 0; rg < 4; ++rg)
+                *reinterpret_cast<f32x4*>(sums + (lane & 31) * DH + d * 32 + rg * 8 + (lane >> 5) * 4) =
+                    f32x4{o[d][4 * rg], o[d][4 * rg + 1], o[d][4 * rg + 2], o[d][4 * rg + 3]};
+        if (lane < 32) stat[lane] = f32x2{m, l};
+        __syncthreads();
+        stat -= wave * 32;
+        for (int x = threadIdx.x; x < 32 * (DH / 4); x += 64 * W) {
+            const int row = x / (DH / 4), d = x % (DH / 4) * 4, rr = row0 + row;
+            if (rr >= rows) break;
+            float M = NO_REF, L = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) M = fmaxf(M, stat[w * 32 + row][0]);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const f32x2 y = stat[w * 32 + row];
+                const float f = exp2_hw(y[0] - M);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(lds + w * 4 * Tl::BYTES + (row * DH + d) * 4);
+                L = __builtin_fmaf(y[1], f, L);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(v[e], f, sum[e]);
+            }
+            const int qi = rr / a.pack, qh = wk.h * a.pack + rr - qi * a.pack;
+            if (a.splits > 1) {
+                const long at = ((long)wk.b * (a.H / a.pack) + wk.h) * rows + rr, n = (long)a.B * a.H * a.Sq;
+                *reinterpret_cast<f32x4*>(a.part + (wk.split * n + at) * DH + d) = sum;
+                if (d == 0) reinterpret_cast<f32x2*>(a.part + a.splits * n * DH)[wk.split * n + at] = f32x2{M, L};
+                continue;
+            }
+            const bool none = L == 0.f || qi >= len.q;
+            typedef T vec __attribute__((ext_vector_type(4)));
+            vec out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = to_elt<T>(none ? 0.f : sum[e] / L);
+            if (d < a.dh) *reinterpret_cast<vec*>(a.o.at(wk.b, qi, qh) + d * (int)sizeof(T)) = out;
+            if (a.lse && d == 0) a.lse[((long)wk.b * a.H + qh) * a.Sq + qi] = none ? -INFINITY : M * LN2 + logf(L);
+        }
+        return;
+    }
+    if (!in) return;
+    if (a.splits > 1) {
+        const long row = ((long)wk.b * (a.H / a.pack) + wk.h) * rows + r, n = (long)a.B * a.H * a.Sq;
+        float* p = a.part + (wk.split * n + row) * DH;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int rg = 0; rg < 4; ++rg)
+                *reinterpret_cast<f32x4*>(p + d * 32 + rg * 8 + (lane >> 5) * 4) =
+                    f32x4{o[d][4 * rg], o[d][4 * rg + 1], o[d][4 * rg + 2], o[d][4 * rg + 3]};
+        if (lane < 32) reinterpret_cast<f32x2*>(a.part + a.splits * n * DH)[wk.split * n + row] = f32x2{m, l};
+        return;
+    }
+    const bool none = l == 0.f || !live;
+    store_row<T, ND>(a.o.at(wk.b, i, h), o, none ? 0.f : 1.f / l, a.dh, lane);
+    if (a.lse && lane < 32) a.lse[((long)wk.b * a.H + h) * a.Sq + i] = none ? -INFINITY : m * LN2 + logf(l);
+}
+
+// Joins the splits of a row: out = sum 2^(m_s - m) O_s / sum 2^(m_s - m) l_s.  A wave per row.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) attend_join(AttendArgs a) {
+    const int lane = threadIdx.x & 63;
+    const long n = (long)a.B * a.H * a.Sq, row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= n) return;
+    const f32x2* st = reinterpret_cast<const f32x2*>(a.part + a.splits * n * DH);
+    const int rows = a.Sq * a.pack;
+    const long group = row / rows;
+    const int r = (int)(row - group * rows), i = r / a.pack, heads = a.H / a.pack;
+    const int b = (int)(group / heads), h = (int)(group % heads) * a.pack + r % a.pack;
+    float m = NO_REF;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, st[s * n + row][0]);
+    constexpr int N = (DH + 63) / 64;
+    float l = 0.f, o[N] = {};
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) {
+        const f32x2 x = st[s * n + row];
+        const float f = exp2_hw(x[0] - m);
+        l = __builtin_fmaf(x[1], f, l);
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+            if (DH % 64 == 0 || d * 64 + lane < DH) o[d] = __builtin_fmaf(a.part[(s * n + row) * DH + d * 64 + lane], f, o[d]);
+    }
+    const Lens len(a, b);
+    const bool none = l == 0.f || i >= len.q;
+    T* out = reinterpret_cast<T*>(a.o.at(b, i, h));
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+        if (d * 64 + lane < a.dh) out[d * 64 + lane] = to_elt<T>(none ? 0.f : o[d] / l);
+    if (a.lse && lane == 0) a.lse[((long)b * a.H + h) * a.Sq + i] = none ? -INFINITY : m * LN2 + logf(l);
+}
+
+// ----------------------------------------------------------------- backward
+// The sums of dS over one distance each, for one wave.  A block's 32 x 32 values go to LDS with each query row one
+// place further left than the one before, so that a distance is a column, which one lane adds up from top to bottom:
+// no atomics, one order.  Distances beyond the table are added in registers.
+constexpr int SKEW = 32 * 64;  // floats of a wave's block
+struct Distances {
+    float *skew, *sums, low, high;
+    int D, lane;
+    __device__ __forceinline__ Distances(float* base, int D_, int wave, int waves, int lane_) : D(D_), lane(lane_) {
+        skew = base + wave * SKEW;
+        sums = base + waves * SKEW + wave * (2 * D + 1);
+        low = high = 0.f;
+    }
+    __device__ __forceinline__ void clear() {
+        for (int i = lane; i < SKEW; i += WAVE) skew[i] = 0.f;
+        for (int i = lane; i < 2 * D + 1; i += WAVE) sums[i] = 0.f;
+        low = high = 0.f;
+    }
+    // lo: distance of the block's first key from its last query
+    __device__ __forceinline__ void add(const f32x16& ds, int lo) {
+        if (lo >= D || lo + 62 <= -D) {
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e & 3] += ds[e];
+            const float x = (s[0] + s[1]) + (s[2] + s[3]);
+            if (lo >= D) high += x; else low += x;
+            return;
+        }
+        float* p = skew + (lane & 31) * 63 + 31 + 4 * (lane >> 5);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[(e >> 2) * 8 + (e & 3)] = ds[e];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i & 3] += skew[i * 64 + lane];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const float x = (s[0] + s[1]) + (s[2] + s[3]);
+        const int rel = lo + lane;  // lane 63 has no pairs
+        if (rel <= -D) low += x;
+        else if (rel >= D) high += x;
+        else sums[rel + D] += x;
+    }
+    __device__ __forceinline__ void finish() {
+        const float a = wave_sum(low), b = wave_sum(high);
+        if (lane == 0) {
+            sums[0] += a;
+            sums[2 * D] += b;
+        }
+    }
+};
+
+// dQ: a wave owns 32 queries and goes through the keys as the forward does:
+//   P = 2^(S - lse), dP^T = V dO^T, dS = P (dP - delta), dQ^T += K^T dS^T.
+// delta_i = sum_j P_ij dP_ij = dO_i . O_i.  EXACT takes the first form, in a pass of its own over the keys: O in bf16
+// is off by up to 2^-8 of itself, and so would each row's sum of dS be, which all the row's pairs share and the bias's
+// gradient adds up.  Writes (lse, delta) of each row for dK and dV.
+template <typename T, int DH, int KT, int W, bool BIAS, bool EXACT>
+__global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
+    typedef Tile<T, DH, KT> Tl;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    float* const table = reinterpret_cast<float*>(lds + 4 * Tl::BYTES);
+    const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
+    const Work wk(a.blocks, a.H, a.splits, a.causal != 0);
+    const Lens len(a, wk.b);
+    const int row0 = (wk.blk * W + wave) * 32, i = row0 + (lane & 31), hk = wk.h / (a.H / a.HK);
+    const bool in = i < a.Sq, live = i < len.q;
+    const int pos = i + len.start, pos0 = row0 + len.start;
+    const long stat = ((long)wk.b * a.H + wk.h) * a.stat_rows;
+
+    bool masks = false;
+    if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
+    Distances dist(table + (BIAS ? table_size(a) : 0), a.max_distance, wave, W, lane);
+
+    typename Elt<T>::frag qf[NK], gf[NK];
+    const int ic = min(i, a.Sq - 1);
+    load_row<T>(a.q.at(wk.b, ic, wk.h), live, a.dh, lane, qf);
+    load_row<T>(a.dout.at(wk.b, ic, wk.h), live, a.dh, lane, gf);
+    float delta = 0.f;
+    if (!EXACT) {
+        typename Elt<T>::frag of[NK];
+        load_row<T>(a.o.at(wk.b, ic, wk.h), live, a.dh, lane, of);
+#pragma unroll
+        for (int x = 0; x < NK; ++x)
+#pragma unroll
+            for (int e = 0; e < Elt<T>::E; ++e) delta = __builtin_fmaf(to_f32((T)of[x][e]), to_f32((T)gf[x][e]), delta);
+        delta = both_sum(delta);
+    }
+    // a row that sees nothing has weights of 0: its lse is taken as +inf
+    float lse2 = live ? a.lse_in[((long)wk.b * a.H + wk.h) * a.Sq + ic] * LOG2E : INFINITY;
+    if (lse2 == -INFINITY) lse2 = INFINITY;
+
+    auto reach = [&](int first, int end) { return first >= len.q ? 0 : len.keys(a.causal, min(end, a.Sq) - 1); };
+    const int kw = reach(row0, row0 + 32);
+    const int tiles = (reach(wk.blk * W * 32, (wk.blk + 1) * W * 32) + KT - 1) / KT;
+    const int t0 = (int)((long)tiles * wk.split / a.splits), t1 = (int)((long)tiles * (wk.split + 1) / a.splits);
+    const char *kp = a.k.at(wk.b, 0, hk), *vp = a.v.at(wk.b, 0, hk);
+    const typename Tl::template Loader<W> kl(a.k.row, a.dh, wave, lane), vl(a.v.row, a.dh, wave, lane);
+    auto stage = [&](int t) {
+        char* s = lds + (t & 1) * 2 * Tl::BYTES;
+        kl(s, kp + (long)t * KT * a.k.row, len.k - t * KT, a.k.row, a.dh, wave);
+        vl(s + Tl::BYTES, vp + (long)t * KT * a.v.row, len.k - t * KT, a.v.row, a.dh, wave);
+    };
+    const float c = a.scale * LOG2E;
+    // the weights of one block (s) and dP (dp); -INFINITY marks a masked pair's weight where `mark` asks for it
+    auto block = [&](const char* ks, const char* vs, int k0, int kb, bool edge, bool mark, f32x16& s, f32x16& dp) {
+        s = zero16();
+        dp = zero16();
+#pragma unroll
+        for (int x = 0; x < NK; ++x) {
+            if (!Tl::has(x, a.dh)) continue;
+            s = mma(Tl::rows(ks, kb * 32, x, lane), qf[x], s);
+            dp = mma(Tl::rows(vs, kb * 32, x, lane), gf[x], dp);
+        }
+        const int last = !live ? -1 : a.causal ? min(len.k - 1, pos) : len.k - 1;
+        const Near n(table, a, BIAS ? k0 - pos0 - 31 : 0, BIAS ? k0 + 4 * (lane >> 5) - pos : 0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float bias = !BIAS ? 0.f : n.far ? n.value : n.at[(e >> 2) * 8 + (e & 3)];
+            float p = exp2_hw(BIAS ? __builtin_fmaf(s[e], c, bias) - lse2 : __builtin_fmaf(s[e], c, -lse2));
+            if ((edge && k0 + acc_row(e, lane) > last) || (BIAS && masks && bias == -INFINITY)) {
+                p = mark ? -INFINITY : 0.f;
+                dp[e] = 0.f;
+            }
+            s[e] = p;
+        }
+    };
+    const bool short_rows = row0 + 32 > len.q;  // a row that is not in use has no weights, whatever the keys hold
+    auto tile_edge = [&](int t) { return short_rows || t * KT + KT > len.k || (a.causal && t * KT + KT - 1 > pos0); };
+    if (EXACT) {
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (tiles > 0) stage(0);
+        for (int t = 0; t < tiles; ++t) {
+            wait_vmcnt<0>();
+            lds_barrier();
+            if (t + 1 < tiles) stage(t + 1);
+            if (t * KT >= kw) continue;
+            const char *ks = lds + (t & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                f32x16 s, dp;
+                block(ks, vs, t * KT + kb * 32, kb, tile_edge(t), false, s, dp);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[e & 3] = __builtin_fmaf(s[e], dp[e], sum[e & 3]);
+            }
+        }
+        delta = both_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        lds_barrier();
+    }
+    f32x16 dq[ND];
+    auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        if (BIAS && a.dist) dist.clear();
+#pragma unroll
+        for (int d = 0; d < ND; ++d) dq[d] = zero16();
+        if (t0 < t1) stage(t0);
+        for (int t = t0; t < t1; ++t) {
+            wait_vmcnt<0>();
+            lds_barrier();
+            if (t + 1 < t1) stage(t + 1);
+            if (t * KT >= kw) continue;
+            const char *ks = lds + (t & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
+            const bool edge = tile_edge(t);
+#pragma unroll 1
+            for (int kb = 0; kb < NB; ++kb) {
+                f32x16 s, dp;
+                block(ks, vs, t * KT + kb * 32, kb, edge, CAREFUL, s, dp);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float d = s[e] * (dp[e] - delta);
+                    s[e] = !CAREFUL ? d : s[e] == -INFINITY ? s[e] : d == -INFINITY ? NAN : d;
+                }
+                Tl::template add<CAREFUL>(ks, kb * 32, s, lane, dq);
+                if (CAREFUL) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = s[e] == -INFINITY ? 0.f : s[e];
+                }
+                if (BIAS && a.dist) dist.add(s, t * KT + kb * 32 - pos0 - 31);
+            }
+        }
+    };
+    pass(std::false_type{});
+    if (a.causal || masks) {
+        if (__syncthreads_or(!all_finite(dq))) pass(std::true_type{});
+    }
+    if (in && a.splits > 1)
+        store_row<float, ND>(reinterpret_cast<char*>(a.part + ((((long)wk.split * a.B + wk.b) * a.H + wk.h) * a.Sq + i) * DH), dq, live ? 1.f : 0.f, DH, lane);
+    else if (in)
+        store_row<T, ND>(a.dq.at(wk.b, i, wk.h), dq, live ? a.scale : 0.f, a.dh, lane);
+    if (wk.split == 0 && lane < 32 && i < a.stat_rows) a.stats[stat + i] = f32x2{lse2, delta};
+    if (wk.split == 0 && wk.blk == a.blocks - 1)  // the rows that a tile of queries may read behind the last one
+        for (int x = a.blocks * W * 32 + (int)threadIdx.x; x < a.stat_rows; x += 64 * W) a.stats[stat + x] = f32x2{INFINITY, 0.f};
+    if (BIAS && a.dist) {
+        dist.finish();
+        __syncthreads();
+        const int n = 2 * a.max_distance + 1;
+        float* out = a.dist + ((((long)wk.h * a.B + wk.b) * a.blocks + wk.blk) * a.splits + wk.split) * n;
+        const float* sums = table + table_size(a) + W * SKEW;
+        for (int d = threadIdx.x; d < n; d += 64 * W) {
+            float x = sums[d];
+            for (int w = 1; w < W; ++w) x += sums[w * n + d];
+            out[d] = x;
+        }
+    }
+}
+
+// dK and dV: a wave owns 32 keys and goes through the queries of all the heads that share them, in tiles of QT:
+//   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+template <typename T, int DH, int QT, int W, bool BIAS>
+__global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
+    typedef Tile<T, DH, QT> Tl;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = QT / 32;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    f32x2* const stats = reinterpret_cast<f32x2*>(lds + 4 * Tl::BYTES);  // two tiles' rows
+    float* const table = reinterpret_cast<float*>(stats + 2 * QT);
+    const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
+    const Work wk(a.blocks, a.HK, a.splits, false);
+    const Lens len(a, wk.b);
+    const int group = a.H / a.HK, k0 = (wk.blk * W + wave) * 32, key = k0 + (lane & 31);
+    const bool in = key < a.Sk, live = key < len.k;
+
+    typename Elt<T>::frag kf[NK], vf[NK];
+    const int kc = min(key, a.Sk - 1);
+    load_row<T>(a.k.at(wk.b, kc, wk.h), live, a.dh, lane, kf);
+    load_row<T>(a.v.at(wk.b, kc, wk.h), live, a.dh, lane, vf);
+
+    // query tiles that see any key of the workgroup
+    const int first = wk.blk * W * 32, t1 = first < len.k ? (len.q + QT - 1) / QT : 0;
+    const int t0 = a.causal ? min(max(first - len.start, 0) / QT, t1) : 0;
+    // this split's share of the tiles of all the heads
+    const long all = (long)group * (t1 - t0), u0 = all * wk.split / a.splits, u1 = all * (wk.split + 1) / a.splits;
+    const typename Tl::template Loader<W> ql(a.q.row, a.dh, wave, lane), gl(a.dout.row, a.dh, wave, lane);
+    const float c = a.scale * LOG2E;
+    bool masks = false;
+    f32x16 dk[ND], dv[ND];
+    auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) dk[d] = dv[d] = zero16();
+        for (int g = 0; g < group; ++g) {
+            const long at = (long)g * (t1 - t0);  // of this head's first tile
+            const int ta = t0 + (int)max(0l, u0 - at), tb = t0 + (int)min((long)(t1 - t0), u1 - at);
+            if (ta >= tb) continue;
+            const int h = wk.h * group + g;
+            const char *qp = a.q.at(wk.b, 0, h), *gp = a.dout.at(wk.b, 0, h);
+            const f32x2* sp = a.stats + ((long)wk.b * a.H + h) * a.stat_rows;
+            auto stage = [&](int t) {
+                char* s = lds + (t & 1) * 2 * Tl::BYTES;
+                ql(s, qp + (long)t * QT * a.q.row, len.q - t * QT, a.q.row, a.dh, wave);
+                gl(s + Tl::BYTES, gp + (long)t * QT * a.dout.row, len.q - t * QT, a.dout.row, a.dh, wave);
+                if (wave < QT / 32)  // 32 rows' pairs a load
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(sp + t * QT, QT * 8), (LdsPtr)(stats + (t & 1) * QT + wave * 32), 4,
+                                                             wave * 256 + lane * 4, 0, 0, 0);
+            };
+            __syncthreads();  // the last head's tiles are done with
+            if (BIAS) masks = masks | (__syncthreads_or(load_table(table, a, h, threadIdx.x, 64 * W)) != 0);
+            stage(ta);
+            for (int t = ta; t < tb; ++t) {
+                wait_vmcnt<0>();
+                lds_barrier();
+                if (t + 1 < tb) stage(t + 1);
+                const int pos0 = t * QT + len.start;
+                if (k0 >= len.k || (a.causal && pos0 + QT - 1 < k0)) continue;
+                const char *qs = lds + (t & 1) * 2 * Tl::BYTES, *gs = qs + Tl::BYTES;
+                const bool edge = t * QT + QT > len.q || (a.causal && pos0 < k0 + 31);
+#pragma unroll 1
+                for (int qb = 0; qb < NB; ++qb) {
+                    f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+                    for (int x = 0; x < NK; ++x) {
+                        if (!Tl::has(x, a.dh)) continue;
+                        s = mma(Tl::rows(qs, qb * 32, x, lane), kf[x], s);
+                        dp = mma(Tl::rows(gs, qb * 32, x, lane), vf[x], dp);
+                    }
+                    const int p0 = pos0 + qb * 32;
+                    const int r0 = a.causal ? key - p0 : 0, r1 = len.q - t * QT - qb * 32;  // rows of the block that see the key
+                    // distances fall with the register here
+                    const Near n(table, a, BIAS ? k0 - p0 - 31 : 0, BIAS ? key - p0 - 4 * (lane >> 5) : 0);
+                    const f32x2* st = stats + (t & 1) * QT + qb * 32 + 4 * (lane >> 5);
+                    f32x16 ds;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const f32x2 row = st[(e >> 2) * 8 + (e & 3)];
+                        const float bias = !BIAS ? 0.f : n.far ? n.value : n.at[-((e >> 2) * 8 + (e & 3))];
+                        float p = exp2_hw(BIAS ? __builtin_fmaf(s[e], c, bias) - row[0] : __builtin_fmaf(s[e], c, -row[0]));
+                        float d = p * (dp[e] - row[1]);
+                        if (CAREFUL && d == -INFINITY) d = NAN;
+                        if ((edge && (acc_row(e, lane) < r0 || acc_row(e, lane) >= r1)) || (BIAS && masks && bias == -INFINITY)) {
+                            p = CAREFUL ? -INFINITY : 0.f;
+                            d = p;
+                        }
+                        s[e] = p;
+                        ds[e] = d;
+                    }
+                    Tl::template add<CAREFUL>(gs, qb * 32, s, lane, dv);
+                    Tl::template add<CAREFUL>(qs, qb * 32, ds, lane, dk);
+                }
+            }
+        }
+    };
+    pass(std::false_type{});
+    if (a.causal || masks) {
+        if (__syncthreads_or(!all_finite(dk) || !all_finite(dv))) pass(std::true_type{});
+    }
+    if (!in) return;
+    if (a.splits > 1) {
+        const long n = (long)a.B * a.HK * a.Sk, row = ((long)wk.b * a.HK + wk.h) * a.Sk + key;
+        store_row<float, ND>(reinterpret_cast<char*>(a.part + (wk.split * n + row) * DH), dk, live ? 1.f : 0.f, DH, lane);
+        store_row<float, ND>(reinterpret_cast<char*>(a.part + ((a.splits + wk.split) * n + row) * DH), dv, live ? 1.f : 0.f, DH, lane);
+        return;
+    }
+    store_row<T, ND>(a.dk.at(wk.b, key, wk.h), dk, live ? a.scale : 0.f, a.dh, lane);
+    store_row<T, ND>(a.dv.at(wk.b, key, wk.h), dv, live ? 1.f : 0.f, a.dh, lane);
+}
+
+// A gradient's rows from the splits' sums [splits][B][heads][len][DH]: added up in order, times f.  Four features a thread.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) attend_sum(AttendArgs a, const float* __restrict__ part, HeadRows out, int heads, int len, float f) {
+    const long n = (long)a.B * heads * len, x = (long)blockIdx.x * 256 + threadIdx.x, row = x / (DH / 4);
+    const int d = (int)(x % (DH / 4)) * 4;
+    if (row >= n || d >= a.dh) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int i = 0; i < a.splits; ++i) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(part + (i * n + row) * DH + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
+    typedef T vec __attribute__((ext_vector_type(4)));
+    vec t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = to_elt<T>(s[e] * f);
+    const long group = row / len;
+    *reinterpret_cast<vec*>(out.at((int)(group / heads), (int)(row - group * len), (int)(group % heads)) + d * (int)sizeof(T)) = t;
+}
+
+// ---------------------------------------------------------------- launches
+template <typename K> gp_status allow_lds(K* k, size_t bytes) {
+    if (bytes > 65536) GP_HIP(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    return GP_OK;
+}
+size_t table_bytes(const AttendArgs& a) { return (2 * ((size_t)a.max_distance + PAD) + 1) * 4; }
+
+template <typename T, int DH, int KT, int W, bool BIAS, bool KEYS>
+gp_status launch_fwd(const AttendArgs& a, hipStream_t st) {
+    const size_t bytes = (KEYS ? 4 * W : 4) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + 4 : 0) + (KEYS ? W * 32 * 8 : 0);
+    auto* k = attend_fwd<T, DH, KT, W, BIAS, KEYS>;
+    GP_TRY(allow_lds(k, bytes));
+    klaunch(k, dim3((unsigned)((long)a.B * (a.H / a.pack) * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
+    if (a.splits > 1)
+        klaunch(attend_join<T, DH>, dim3((unsigned)(((long)a.B * a.H * a.Sq + 3) / 4)), dim3(256), 0, st, a);
+    GP_LAUNCH_CHECK();
+    return GP_OK;
+}
+template <typename T, int DH> gp_status forward(const AttendArgs& a, hipStream_t st) {
+    constexpr int KT = tile_rows(sizeof(T)), W = key_waves(DH * sizeof(T));
+    if (a.keys) return a.bias ? launch_fwd<T, DH, 32, W, true, true>(a, st) : launch_fwd<T, DH, 32, W, false, true>(a, st);
+    return a.bias ? launch_fwd<T, DH, KT, 4, true, false>(a, st) : launch_fwd<T, DH, KT, 4, false, false>(a, st);
+}
+
+template <typename T, int DH>
+void launch_sum(const AttendArgs& a, const float* part, const HeadRows& out, int heads, int len, float f, hipStream_t st) {
+    const long n = (long)a.B * heads * len * (DH / 4);
+    klaunch(attend_sum<T, DH>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, part, out, heads, len, f);
+}
+template <typename T, int DH, int W, bool BIAS, bool EXACT>
+gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
+    constexpr int KT = tile_rows(sizeof(T));
+    const size_t bytes = 4 * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + W * (SKEW + 2 * a.max_distance + 1) * 4 : 0);
+    auto* k = attend_dq<T, DH, KT, W, BIAS, EXACT>;
+    GP_TRY(allow_lds(k, bytes));
+    klaunch(k, dim3((unsigned)((long)a.B * a.H * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
+    if (a.splits > 1) launch_sum<T, DH>(a, a.part, a.dq, a.H, a.Sq, a.scale, st);
+    GP_LAUNCH_CHECK();
+    return GP_OK;
+}
+template <typename T, int DH, int W, bool BIAS>
+gp_status launch_dkv(const AttendArgs& a, hipStream_t st) {
+    constexpr int QT = tile_rows(sizeof(T));
+    const size_t bytes = 4 * Tile<T, DH, QT>::BYTES + 2 * QT * 8 + (BIAS ? table_bytes(a) : 0);
+    auto* k = attend_dkv<T, DH, QT, W, BIAS>;
+    GP_TRY(allow_lds(k, bytes));
+    klaunch(k, dim3((unsigned)((long)a.B * a.HK * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
+    if (a.splits > 1) {
+        launch_sum<T, DH>(a, a.part, a.dk, a.HK, a.Sk, a.scale, st);
+        launch_sum<T, DH>(a, a.part + (size_t)a.splits * a.B * a.HK * a.Sk * DH, a.dv, a.HK, a.Sk, 1.f, st);
+    }
+    GP_LAUNCH_CHECK();
+    return GP_OK;
+}
+template <typename T, int DH> gp_status backward(const AttendArgs& a, bool exact, const Shape& dq, const Shape& dkv, hipStream_t st) {
+    AttendArgs q = a;
+    q.blocks = dq.blocks;
+    q.splits = dq.splits;
+    if (q.blocks) {
+        if (a.bias)
+            GP_TRY(exact ? (launch_dq<T, DH, BW, true, true>(q, st)) : (launch_dq<T, DH, BW, true, false>(q, st)));
+        else
+            GP_TRY(exact ? (launch_dq<T, DH, BW, false, true>(q, st)) : (launch_dq<T, DH, BW, false, false>(q, st)));
+    }
+    AttendArgs k = a;
+    k.blocks = dkv.blocks;
+    k.splits = dkv.splits;
+    if (k.blocks) GP_TRY(a.bias ? (launch_dkv<T, DH, BW, true>(k, st)) : (launch_dkv<T, DH, BW, false>(k, st)));
+    return GP_OK;
+}
+
+} // namespace
+
+// The widths that a head is padded to.
+template <typename T> gp_status attend_forward_as(const AttendArgs& a, hipStream_t st) {
+    switch (head_bucket(a.dh)) {
+    case 32: return forward<T, 32>(a, st);
+    case 64: return forward<T, 64>(a, st);
+    case 96: return forward<T, 96>(a, st);
+    default: return forward<T, 128>(a, st);
+    }
+}
+template <typename T> gp_status attend_backward_as(const AttendArgs& a, bool exact, const Shape& dq, const Shape& dkv, hipStream_t st) {
+    switch (head_bucket(a.dh)) {
+    case 32: return backward<T, 32>(a, exact, dq, dkv, st);
+    case 64: return backward<T, 64>(a, exact, dq, dkv, st);
+    case 96: return backward<T, 96>(a, exact, dq, dkv, st);
+    default: return backward<T, 128>(a, exact, dq, dkv, st);
+    }
+}
+
+} // namespace gp

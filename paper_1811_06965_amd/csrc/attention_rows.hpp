@@ -41,6 +41,7 @@ struct Shape {
 constexpr int BW = 4;  // waves of the backward's workgroups
 constexpr int head_bucket(int dh) { return (dh + 31) / 32 * 32; }           // features that a kernel is made for
 constexpr int tile_rows(int esize) { return esize == 2 ? 64 : 32; }          // rows of a tile in LDS
+constexpr int stages(int width) { return width <= 64 ? 3 : 2; }                // tiles in LDS at a time
 constexpr int key_waves(int row_bytes) { return row_bytes <= 128 ? 8 : row_bytes <= 256 ? 4 : 2; }
 
 // The kernels for one type.

@@ -58,8 +58,7 @@ __device__ __forceinline__ int acc_row(int r, int lane) { return (r >> 2) * 8 + 
 // consecutive rows (the transposing reads), then fall into distinct banks.
 __device__ __forceinline__ int swizzle(int r) { return (((r >> 1) & 1) << 2) | ((r >> 2) & 3); }
 
-typedef short v4i16 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) v4i16* LdsV4;
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 template <typename T, int DH, int R> struct Tile {
     typedef Elt<T> X;
@@ -95,93 +94,125 @@ template <typename T, int DH, int R> struct Tile {
         const int r = row0 + (lane & 31);
         return *reinterpret_cast<const frag*>(s + (ks >> 2) * (R * 128) + r * 128 + (((((ks & 3) << 1) | (lane >> 5)) ^ swizzle(r)) << 4));
     }
-    // acc (32 features from d0 on x lane's column) += the tile's rows row0 + 16 cc .. + 15, transposed, times the
-    // accumulator registers 8 cc .. 8 cc + 7 of `w`, whose rows those are.  In bf16 one transposing read gives a lane
-    // four rows of its feature, and w is rounded to bf16, the matrix unit's type: by up to 2^-8 of each weight,
-    // while their sums stay in fp32.
-    static __device__ __forceinline__ bf16x8 column(const char* s, int row0, int cc, int d0, int lane) {
-        const int g = lane >> 4, q = lane & 15;
-        const int row = row0 + 16 * cc + 4 * (g >> 1) + (q >> 2), col = (d0 & 63) + 16 * (g & 1) + 4 * (q & 3);
-        const char* p = s + (d0 >> 6) * (R * 128) + (col & 7) * 2;
-        auto at = [&](int r) { return (LdsV4)(p + r * 128 + (((col >> 3) ^ swizzle(r)) << 4)); };
-        const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row)));
-        const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row + 8)));
-        return bf16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-    }
+    // The tile's rows row0 .. row0 + 31 transposed, for acc (32 features x lane's column) += rows^T w, w the accumulator
+    // registers whose rows those are.  In bf16 one transposing read gives a lane four rows of its feature.  The reads wait for
+    // themselves: as builtins they count as writes, before which the compiler waits for the tiles on their way.
+    template <int ND> struct Columns {
+        bf16x8 x[2][ND];
+        __device__ __forceinline__ Columns(const char* s, int row0, int lane) {
+            const int g = lane >> 4, q = lane & 15, r = row0 + 4 * (g >> 1) + (q >> 2), col = 16 * (g & 1) + 4 * (q & 3);
+            const uint32_t at = (uint32_t)(size_t)(LdsPtr)s + r * 128 + (col & 7) * 2;
+            // rows 8 on: swizzle ^ 2; features 32 on: chunk ^ 4; rows 16 on and parts of 64 features: a constant further
+            const uint32_t a0 = at + (((col >> 3) ^ swizzle(r)) << 4), a1 = (a0 ^ 32) + 1024;
+#pragma unroll
+            for (int d = 0; d < ND; d += 2) {
+                if (d + 1 < ND)
+                    read(a0, a1, a0 ^ 64, a1 ^ 64, d / 2, x[0][d], x[1][d], x[0][d + 1], x[1][d + 1]);
+                else
+                    read(a0, a1, d / 2, x[0][d], x[1][d]);
+            }
+        }
+        static __device__ __forceinline__ bf16x8 pair(i32x2 x, i32x2 y) { return __builtin_bit_cast(bf16x8, i32x4{x[0], x[1], y[0], y[1]}); }
+        static __device__ __forceinline__ void read(uint32_t a0, uint32_t a1, int part, bf16x8& x0, bf16x8& x1) {
+            i32x2 v[4];
+            a0 += part * (R * 128);
+            a1 += part * (R * 128);
+            asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %2, %4 offset:2048\n\t"
+                         "ds_read_b64_tr_b16 %3, %5 offset:2048\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                         : "v"(a0), "v"(a1));
+            x0 = pair(v[0], v[1]);
+            x1 = pair(v[2], v[3]);
+        }
+        static __device__ __forceinline__ void read(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, int part, bf16x8& x0, bf16x8& x1,
+                                                    bf16x8& y0, bf16x8& y1) {
+            i32x2 v[8];
+            a0 += part * (R * 128);
+            a1 += part * (R * 128);
+            b0 += part * (R * 128);
+            b1 += part * (R * 128);
+            asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %2, %8 offset:2048\n\t"
+                         "ds_read_b64_tr_b16 %3, %9 offset:2048\n\tds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %11\n\t"
+                         "ds_read_b64_tr_b16 %6, %10 offset:2048\n\tds_read_b64_tr_b16 %7, %11 offset:2048\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+                         : "v"(a0), "v"(a1), "v"(b0), "v"(b1));
+            x0 = pair(v[0], v[1]);
+            x1 = pair(v[2], v[3]);
+            y0 = pair(v[4], v[5]);
+            y1 = pair(v[6], v[7]);
+        }
+    };
     static __device__ __forceinline__ float element(const char* s, int r, int d0, int lane) {
         return *reinterpret_cast<const float*>(s + (d0 >> 5) * (R * 128) + (lane & 3) * 4 + r * 128 +
                                                ((((lane & 31) >> 2) ^ swizzle(r)) << 4));
     }
-    static __device__ __forceinline__ f32x16 transposed(const char* s, int row0, int cc, int d0, const f32x16& w, int lane,
-                                                        f32x16 acc) {
-        if constexpr (sizeof(T) == 2) {
-            bf16x8 b;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) b[e] = (bf16)w[8 * cc + e];
-            return mma(column(s, row0, cc, d0, lane), b, acc);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(element(s, row0 + acc_row(8 * cc + e, lane), d0, lane), w[8 * cc + e], acc, 0, 0, 0);
-            return acc;
-        }
-    }
-    // The same without the pairs marked by a weight of -INFINITY: what a masked row holds, infinities and NaN included,
-    // does not reach the sum.  The finite values are multiplied as above; two more products with weights of 1 find
+    // acc += the tile's 32 rows from row0 on, transposed, times w.  In bf16 w is rounded, the matrix unit's type: by up to
+    // 2^-8 of each weight, while their sums stay in fp32.
+    // CAREFUL: without the pairs marked by a weight of -INFINITY: what a masked row holds, infinities and NaN included,
+    // does not reach the sum.  The finite values are multiplied as always; two more products with weights of 1 find
     // where an unmasked pair holds +inf or -inf (a NaN counts as both), which is then added.
-    static __device__ __forceinline__ f32x16 unmasked(const char* s, int row0, int cc, int d0, const f32x16& w, int lane,
-                                                      f32x16 acc) {
-        const auto infinite = [](float x, float which) { return x == which || x != x; };
-        const auto finite = [](float x) { return x - x == 0.f ? x : 0.f; };
-        f32x16 found;
-        if constexpr (sizeof(T) == 2) {
-            const bf16x8 x = column(s, row0, cc, d0, lane);
-            bf16x8 f, b, seen;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool m = w[8 * cc + e] == -INFINITY;
-                f[e] = (bf16)finite((float)x[e]);
-                b[e] = (bf16)(m ? 0.f : w[8 * cc + e]);
-                seen[e] = (bf16)(m ? 0.f : 1.f);
-            }
-            acc = mma(f, b, acc);
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                const float inf = which ? -INFINITY : INFINITY;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (bf16)(infinite((float)x[e], inf) ? 1.f : 0.f);
-                found = mma(f, seen, zero16());
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] = found[e] > 0.f ? acc[e] + inf : acc[e];
-            }
-        } else {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = element(s, row0 + acc_row(8 * cc + e, lane), d0, lane);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(finite(x[e]), w[8 * cc + e] == -INFINITY ? 0.f : w[8 * cc + e], acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                const float inf = which ? -INFINITY : INFINITY;
-                found = zero16();
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    found = __builtin_amdgcn_mfma_f32_32x32x2f32(infinite(x[e], inf) ? 1.f : 0.f, w[8 * cc + e] == -INFINITY ? 0.f : 1.f, found, 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] = found[e] > 0.f ? acc[e] + inf : acc[e];
-            }
-        }
-        return acc;
-    }
-    // acc += the tile's 32 rows from row0 on, transposed, times w.
     template <bool CAREFUL, int ND>
     static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, int lane, f32x16 (&acc)[ND]) {
+        if constexpr (sizeof(T) == 2) {
+            const Columns<ND> c(s, row0, lane);
 #pragma unroll
-        for (int cc = 0; cc < 2; ++cc)
+            for (int cc = 0; cc < 2; ++cc) {
+                bf16x8 b, seen;
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
-                acc[d] = CAREFUL ? unmasked(s, row0, cc, d * 32, w, lane, acc[d]) : transposed(s, row0, cc, d * 32, w, lane, acc[d]);
+                for (int e = 0; e < 8; ++e) {
+                    const float x = w[8 * cc + e];
+                    b[e] = (bf16)(CAREFUL && x == -INFINITY ? 0.f : x);
+                    if (CAREFUL) seen[e] = (bf16)(x == -INFINITY ? 0.f : 1.f);
+                }
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    if (!CAREFUL) {
+                        acc[d] = mma(c.x[cc][d], b, acc[d]);
+                        continue;
+                    }
+                    bf16x8 f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = (bf16)finite((float)c.x[cc][d][e]);
+                    acc[d] = mma(f, b, acc[d]);
+#pragma unroll
+                    for (int which = 0; which < 2; ++which) {
+                        const float inf = which ? -INFINITY : INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = (bf16)(infinite((float)c.x[cc][d][e], inf) ? 1.f : 0.f);
+                        found(mma(f, seen, zero16()), inf, acc[d]);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float y = w[8 * cc + e];
+                        x[e] = element(s, row0 + acc_row(8 * cc + e, lane), d * 32, lane);
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(CAREFUL ? finite(x[e]) : x[e], CAREFUL && y == -INFINITY ? 0.f : y, acc[d], 0, 0, 0);
+                    }
+                    if (!CAREFUL) continue;
+#pragma unroll
+                    for (int which = 0; which < 2; ++which) {
+                        const float inf = which ? -INFINITY : INFINITY;
+                        f32x16 n = zero16();
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            n = __builtin_amdgcn_mfma_f32_32x32x2f32(infinite(x[e], inf) ? 1.f : 0.f, w[8 * cc + e] == -INFINITY ? 0.f : 1.f, n, 0, 0, 0);
+                        found(n, inf, acc[d]);
+                    }
+                }
+        }
+    }
+    static __device__ __forceinline__ float finite(float x) { return x - x == 0.f ? x : 0.f; }
+    static __device__ __forceinline__ bool infinite(float x, float which) { return x == which || x != x; }
+    static __device__ __forceinline__ void found(const f32x16& n, float inf, f32x16& acc) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = n[e] > 0.f ? acc[e] + inf : acc[e];
     }
 };
 
@@ -228,6 +259,9 @@ __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 
 __device__ __forceinline__ float both_max(float x) { return fmaxf(x, other_half(x)); }
 __device__ __forceinline__ float both_sum(float x) { return x + other_half(x); }
 
+// Tiles in LDS at a time, all but one on their way; the ring's next place.
+template <int ST> __device__ __forceinline__ int ring(int buf, int by) { return buf + by < ST ? buf + by : buf + by - ST; }
+
 // Every LDS read of this wave has returned, and none is moved across.
 __device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -262,15 +296,38 @@ __device__ __forceinline__ bool load_table(float* t, const AttendArgs& a, int h,
     return masks;
 }
 // One block of 32 x 32 pairs whose distances (key - position) go from lo to lo + 62 over the block: where they all lie
-// beyond the table on one side, one value.
+// beyond the table on one side, one value.  The branches on that and on masks are of whole blocks.
 struct Near {
     bool far;
     float value;       // far: of every pair
-    const float* at;   // near: of this lane's register 0; register r lies step * (row r - row 0) further
+    const float* at;   // near: of this lane's register 0; that of register r lies STEP * (row r - row 0) further
     __device__ __forceinline__ Near(const float* t, const AttendArgs& a, int lo, int mine) {
         far = lo >= a.max_distance || lo + 62 <= -a.max_distance;
         value = t[lo >= a.max_distance ? 2 * (a.max_distance + PAD) : 0];
         at = t + (far ? 0 : mine + a.max_distance + PAD);
+    }
+    // s = s c + bias
+    template <int STEP> __device__ __forceinline__ void add(f32x16& s, float c) const {
+        if (far) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], c, value);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], c, at[STEP * ((e >> 2) * 8 + (e & 3))]);
+        }
+    }
+    // f(e) for the registers whose bias is a mask's
+    template <int STEP, typename F> __device__ __forceinline__ void mask(F f) const {
+        if (far) {
+            if (value == -INFINITY) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) f(e);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (at[STEP * ((e >> 2) * 8 + (e & 3))] == -INFINITY) f(e);
+        }
     }
 };
 
@@ -300,9 +357,10 @@ struct Work {
 template <typename T, int DH, int KT, int W, bool BIAS, bool KEYS>
 __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
     typedef Tile<T, DH, KT> Tl;
-    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, LW = KEYS ? 1 : W;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, LW = KEYS ? 1 : W, ST = KEYS ? 2 : stages(DH);
+    constexpr int TB = 2 * Tl::BYTES;  // a tile of keys and one of values
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    float* const table = reinterpret_cast<float*>(lds + (KEYS ? 4 * W : 4) * Tl::BYTES);
+    float* const table = reinterpret_cast<float*>(lds + (KEYS ? W : 1) * ST * TB);
     const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
     const Work wk(a.blocks, a.H / a.pack, a.splits, a.causal != 0);
     const Lens len(a, wk.b);
@@ -327,9 +385,9 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
     const char *kp = a.k.at(wk.b, 0, hk), *vp = a.v.at(wk.b, 0, hk);
     const typename Tl::template Loader<LW> kl(a.k.row, a.dh, KEYS ? 0 : wave, lane), vl(a.v.row, a.dh, KEYS ? 0 : wave, lane);
     const int own = KEYS ? wave : 0, step = KEYS ? W : 1;  // tiles of this wave: from t0 + own on, every step-th
-    char* const base = lds + own * 4 * Tl::BYTES;
-    auto stage = [&](int t) {
-        char* s = base + ((t - t0) / step & 1) * 2 * Tl::BYTES;
+    char* const base = lds + own * ST * TB;
+    auto stage = [&](int t, int buf) {
+        char* s = base + buf * TB;
         kl(s, kp + (long)t * KT * a.k.row, len.k - t * KT, a.k.row, a.dh, KEYS ? 0 : wave);
         vl(s + Tl::BYTES, vp + (long)t * KT * a.v.row, len.k - t * KT, a.v.row, a.dh, KEYS ? 0 : wave);
     };
@@ -345,13 +403,15 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
         l = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] = zero16();
-        if (t0 + own < t1) stage(t0 + own);
-        for (int t = t0 + own; t < t1; t += step) {
-            wait_vmcnt<0>();
+#pragma unroll
+        for (int x = 0; x < ST - 1; ++x)
+            if (t0 + own + x * step < t1) stage(t0 + own + x * step, x);
+        for (int t = t0 + own, buf = 0; t < t1; t += step, buf = ring<ST>(buf, 1)) {
+            if (ST > 2 && t + step < t1) wait_vmcnt<2 * decltype(kl)::N>(); else wait_vmcnt<0>();
             if (KEYS) lds_reads_done(); else lds_barrier();
-            if (t + step < t1) stage(t + step);
+            if (t + (ST - 1) * step < t1) stage(t + (ST - 1) * step, ring<ST>(buf, ST - 1));
             if (t * KT >= kw) continue;
-            const char *ks = base + ((t - t0) / step & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
+            const char *ks = base + buf * TB, *vs = ks + Tl::BYTES;
             f32x16 s[NB];
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
@@ -367,12 +427,8 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
                 const int k0 = t * KT + kb * 32;
                 if (BIAS) {
                     const Near n(table, a, k0 - pos0 - 31, k0 + 4 * (lane >> 5) - pos);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float bias = n.far ? n.value : n.at[(e >> 2) * 8 + (e & 3)];
-                        const float x = __builtin_fmaf(s[kb][e], c, bias);
-                        s[kb][e] = masks && bias == -INFINITY ? bias : x;
-                    }
+                    n.add<1>(s[kb], c);
+                    if (masks) n.mask<1>([&](int e) { s[kb][e] = -INFINITY; });
                 }
                 if (edge) {
                     const int last = a.causal ? min(len.k - 1, pos) : len.k - 1;
@@ -415,7 +471,7 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
     if constexpr (KEYS) {
         lds_reads_done();
         float* sums = reinterpret_cast<float*>(base);  // [row][DH], in place of this wave's tiles
-        f32x2* stat = reinterpret_cast<f32x2*>(lds + W * 4 * Tl::BYTES + (BIAS ? table_size(a) * 4 + 4 : 0)) + wave * 32;
+        f32x2* stat = reinterpret_cast<f32x2*>(lds + W * ST * TB + (BIAS ? table_size(a) * 4 + 4 : 0)) + wave * 32;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -436,7 +492,7 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
             for (int w = 0; w < W; ++w) {
                 const f32x2 y = stat[w * 32 + row];
                 const float f = exp2_hw(y[0] - M);
-                const f32x4 v = *reinterpret_cast<const f32x4*>(lds + w * 4 * Tl::BYTES + (row * DH + d) * 4);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(lds + w * ST * TB + (row * DH + d) * 4);
                 L = __builtin_fmaf(y[1], f, L);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(v[e], f, sum[e]);
@@ -568,9 +624,9 @@ struct Distances {
 template <typename T, int DH, int KT, int W, bool BIAS, bool EXACT>
 __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     typedef Tile<T, DH, KT> Tl;
-    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, ST = BIAS ? 2 : stages(DH), TB = 2 * Tl::BYTES;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    float* const table = reinterpret_cast<float*>(lds + 4 * Tl::BYTES);
+    float* const table = reinterpret_cast<float*>(lds + ST * TB);
     const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
     const Work wk(a.blocks, a.H, a.splits, a.causal != 0);
     const Lens len(a, wk.b);
@@ -607,10 +663,20 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     const int t0 = (int)((long)tiles * wk.split / a.splits), t1 = (int)((long)tiles * (wk.split + 1) / a.splits);
     const char *kp = a.k.at(wk.b, 0, hk), *vp = a.v.at(wk.b, 0, hk);
     const typename Tl::template Loader<W> kl(a.k.row, a.dh, wave, lane), vl(a.v.row, a.dh, wave, lane);
-    auto stage = [&](int t) {
-        char* s = lds + (t & 1) * 2 * Tl::BYTES;
+    auto stage = [&](int t, int buf) {
+        char* s = lds + buf * TB;
         kl(s, kp + (long)t * KT * a.k.row, len.k - t * KT, a.k.row, a.dh, wave);
         vl(s + Tl::BYTES, vp + (long)t * KT * a.v.row, len.k - t * KT, a.v.row, a.dh, wave);
+    };
+    auto first_tiles = [&](int t, int end) {
+#pragma unroll
+        for (int x = 0; x < ST - 1; ++x)
+            if (t + x < end) stage(t + x, x);
+    };
+    auto next_tile = [&](int t, int end, int buf) {  // tile t is there; the one ST - 1 on is sent for
+        if (ST > 2 && t + 1 < end) wait_vmcnt<2 * decltype(kl)::N>(); else wait_vmcnt<0>();
+        lds_barrier();
+        if (t + ST - 1 < end) stage(t + ST - 1, ring<ST>(buf, ST - 1));
     };
     const float c = a.scale * LOG2E;
     // the weights of one block (s) and dP (dp); -INFINITY marks a masked pair's weight where `mark` asks for it
@@ -623,30 +689,31 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
             s = mma(Tl::rows(ks, kb * 32, x, lane), qf[x], s);
             dp = mma(Tl::rows(vs, kb * 32, x, lane), gf[x], dp);
         }
-        const int last = !live ? -1 : a.causal ? min(len.k - 1, pos) : len.k - 1;
         const Near n(table, a, BIAS ? k0 - pos0 - 31 : 0, BIAS ? k0 + 4 * (lane >> 5) - pos : 0);
+        if (BIAS) n.add<1>(s, c);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float bias = !BIAS ? 0.f : n.far ? n.value : n.at[(e >> 2) * 8 + (e & 3)];
-            float p = exp2_hw(BIAS ? __builtin_fmaf(s[e], c, bias) - lse2 : __builtin_fmaf(s[e], c, -lse2));
-            if ((edge && k0 + acc_row(e, lane) > last) || (BIAS && masks && bias == -INFINITY)) {
-                p = mark ? -INFINITY : 0.f;
-                dp[e] = 0.f;
-            }
-            s[e] = p;
+        for (int e = 0; e < 16; ++e) s[e] = exp2_hw(BIAS ? s[e] - lse2 : __builtin_fmaf(s[e], c, -lse2));
+        auto hide = [&](int e) {
+            s[e] = mark ? -INFINITY : 0.f;
+            dp[e] = 0.f;
+        };
+        if (edge) {
+            const int last = !live ? -1 : a.causal ? min(len.k - 1, pos) : len.k - 1;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (k0 + acc_row(e, lane) > last) hide(e);
         }
+        if (BIAS && masks) n.mask<1>(hide);
     };
     const bool short_rows = row0 + 32 > len.q;  // a row that is not in use has no weights, whatever the keys hold
     auto tile_edge = [&](int t) { return short_rows || t * KT + KT > len.k || (a.causal && t * KT + KT - 1 > pos0); };
     if (EXACT) {
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        if (tiles > 0) stage(0);
-        for (int t = 0; t < tiles; ++t) {
-            wait_vmcnt<0>();
-            lds_barrier();
-            if (t + 1 < tiles) stage(t + 1);
+        first_tiles(0, tiles);
+        for (int t = 0, buf = 0; t < tiles; ++t, buf = ring<ST>(buf, 1)) {
+            next_tile(t, tiles, buf);
             if (t * KT >= kw) continue;
-            const char *ks = lds + (t & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
+            const char *ks = lds + buf * TB, *vs = ks + Tl::BYTES;
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
                 f32x16 s, dp;
@@ -664,13 +731,11 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         if (BIAS && a.dist) dist.clear();
 #pragma unroll
         for (int d = 0; d < ND; ++d) dq[d] = zero16();
-        if (t0 < t1) stage(t0);
-        for (int t = t0; t < t1; ++t) {
-            wait_vmcnt<0>();
-            lds_barrier();
-            if (t + 1 < t1) stage(t + 1);
+        first_tiles(t0, t1);
+        for (int t = t0, buf = 0; t < t1; ++t, buf = ring<ST>(buf, 1)) {
+            next_tile(t, t1, buf);
             if (t * KT >= kw) continue;
-            const char *ks = lds + (t & 1) * 2 * Tl::BYTES, *vs = ks + Tl::BYTES;
+            const char *ks = lds + buf * TB, *vs = ks + Tl::BYTES;
             const bool edge = tile_edge(t);
 #pragma unroll 1
             for (int kb = 0; kb < NB; ++kb) {
@@ -720,10 +785,10 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
 template <typename T, int DH, int QT, int W, bool BIAS>
 __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
     typedef Tile<T, DH, QT> Tl;
-    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = QT / 32;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = QT / 32, ST = stages(DH), TB = 2 * Tl::BYTES;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    f32x2* const stats = reinterpret_cast<f32x2*>(lds + 4 * Tl::BYTES);  // two tiles' rows
-    float* const table = reinterpret_cast<float*>(stats + 2 * QT);
+    f32x2* const stats = reinterpret_cast<f32x2*>(lds + ST * TB);  // of the tiles' rows
+    float* const table = reinterpret_cast<float*>(stats + ST * QT);
     const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
     const Work wk(a.blocks, a.HK, a.splits, false);
     const Lens len(a, wk.b);
@@ -755,24 +820,27 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
             const int h = wk.h * group + g;
             const char *qp = a.q.at(wk.b, 0, h), *gp = a.dout.at(wk.b, 0, h);
             const f32x2* sp = a.stats + ((long)wk.b * a.H + h) * a.stat_rows;
-            auto stage = [&](int t) {
-                char* s = lds + (t & 1) * 2 * Tl::BYTES;
+            auto stage = [&](int t, int buf) {
+                char* s = lds + buf * TB;
                 ql(s, qp + (long)t * QT * a.q.row, len.q - t * QT, a.q.row, a.dh, wave);
                 gl(s + Tl::BYTES, gp + (long)t * QT * a.dout.row, len.q - t * QT, a.dout.row, a.dh, wave);
-                if (wave < QT / 32)  // 32 rows' pairs a load
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(sp + t * QT, QT * 8), (LdsPtr)(stats + (t & 1) * QT + wave * 32), 4,
-                                                             wave * 256 + lane * 4, 0, 0, 0);
+                // 32 rows' pairs a load; each wave issues one, so that all have as many on their way
+                const int part = wave % (QT / 32);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(sp + t * QT, QT * 8), (LdsPtr)(stats + buf * QT + part * 32), 4,
+                                                         part * 256 + lane * 4, 0, 0, 0);
             };
             __syncthreads();  // the last head's tiles are done with
             if (BIAS) masks = masks | (__syncthreads_or(load_table(table, a, h, threadIdx.x, 64 * W)) != 0);
-            stage(ta);
-            for (int t = ta; t < tb; ++t) {
-                wait_vmcnt<0>();
+#pragma unroll
+            for (int x = 0; x < ST - 1; ++x)
+                if (ta + x < tb) stage(ta + x, x);
+            for (int t = ta, buf = 0; t < tb; ++t, buf = ring<ST>(buf, 1)) {
+                if (ST > 2 && t + 1 < tb) wait_vmcnt<2 * decltype(ql)::N + 1>(); else wait_vmcnt<0>();
                 lds_barrier();
-                if (t + 1 < tb) stage(t + 1);
+                if (t + ST - 1 < tb) stage(t + ST - 1, ring<ST>(buf, ST - 1));
                 const int pos0 = t * QT + len.start;
                 if (k0 >= len.k || (a.causal && pos0 + QT - 1 < k0)) continue;
-                const char *qs = lds + (t & 1) * 2 * Tl::BYTES, *gs = qs + Tl::BYTES;
+                const char *qs = lds + buf * TB, *gs = qs + Tl::BYTES;
                 const bool edge = t * QT + QT > len.q || (a.causal && pos0 < k0 + 31);
 #pragma unroll 1
                 for (int qb = 0; qb < NB; ++qb) {
@@ -784,25 +852,26 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                         dp = mma(Tl::rows(gs, qb * 32, x, lane), vf[x], dp);
                     }
                     const int p0 = pos0 + qb * 32;
-                    const int r0 = a.causal ? key - p0 : 0, r1 = len.q - t * QT - qb * 32;  // rows of the block that see the key
                     // distances fall with the register here
                     const Near n(table, a, BIAS ? k0 - p0 - 31 : 0, BIAS ? key - p0 - 4 * (lane >> 5) : 0);
-                    const f32x2* st = stats + (t & 1) * QT + qb * 32 + 4 * (lane >> 5);
+                    const f32x2* st = stats + buf * QT + qb * 32 + 4 * (lane >> 5);
                     f32x16 ds;
+                    if (BIAS) n.add<-1>(s, c);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const f32x2 row = st[(e >> 2) * 8 + (e & 3)];
-                        const float bias = !BIAS ? 0.f : n.far ? n.value : n.at[-((e >> 2) * 8 + (e & 3))];
-                        float p = exp2_hw(BIAS ? __builtin_fmaf(s[e], c, bias) - row[0] : __builtin_fmaf(s[e], c, -row[0]));
-                        float d = p * (dp[e] - row[1]);
-                        if (CAREFUL && d == -INFINITY) d = NAN;
-                        if ((edge && (acc_row(e, lane) < r0 || acc_row(e, lane) >= r1)) || (BIAS && masks && bias == -INFINITY)) {
-                            p = CAREFUL ? -INFINITY : 0.f;
-                            d = p;
-                        }
-                        s[e] = p;
-                        ds[e] = d;
+                        s[e] = exp2_hw(BIAS ? s[e] - row[0] : __builtin_fmaf(s[e], c, -row[0]));
+                        ds[e] = s[e] * (dp[e] - row[1]);
+                        if (CAREFUL && ds[e] == -INFINITY) ds[e] = NAN;
                     }
+                    auto hide = [&](int e) { s[e] = ds[e] = CAREFUL ? -INFINITY : 0.f; };
+                    if (edge) {  // rows of the block that see the key
+                        const int r0 = a.causal ? key - p0 : 0, r1 = len.q - t * QT - qb * 32;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (acc_row(e, lane) < r0 || acc_row(e, lane) >= r1) hide(e);
+                    }
+                    if (BIAS && masks) n.mask<-1>(hide);
                     Tl::template add<CAREFUL>(gs, qb * 32, s, lane, dv);
                     Tl::template add<CAREFUL>(qs, qb * 32, ds, lane, dk);
                 }
@@ -854,7 +923,7 @@ size_t table_bytes(const AttendArgs& a) { return (2 * ((size_t)a.max_distance + 
 
 template <typename T, int DH, int KT, int W, bool BIAS, bool KEYS>
 gp_status launch_fwd(const AttendArgs& a, hipStream_t st) {
-    const size_t bytes = (KEYS ? 4 * W : 4) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + 4 : 0) + (KEYS ? W * 32 * 8 : 0);
+    const size_t bytes = (KEYS ? 4 * W : 2 * stages(DH)) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + 4 : 0) + (KEYS ? W * 32 * 8 : 0);
     auto* k = attend_fwd<T, DH, KT, W, BIAS, KEYS>;
     GP_TRY(allow_lds(k, bytes));
     klaunch(k, dim3((unsigned)((long)a.B * (a.H / a.pack) * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
@@ -877,7 +946,7 @@ void launch_sum(const AttendArgs& a, const float* part, const HeadRows& out, int
 template <typename T, int DH, int W, bool BIAS, bool EXACT>
 gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
     constexpr int KT = tile_rows(sizeof(T));
-    const size_t bytes = 4 * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + W * (SKEW + 2 * a.max_distance + 1) * 4 : 0);
+    const size_t bytes = 2 * (BIAS ? 2 : stages(DH)) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + W * (SKEW + 2 * a.max_distance + 1) * 4 : 0);
     auto* k = attend_dq<T, DH, KT, W, BIAS, EXACT>;
     GP_TRY(allow_lds(k, bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.H * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
@@ -888,7 +957,7 @@ gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
 template <typename T, int DH, int W, bool BIAS>
 gp_status launch_dkv(const AttendArgs& a, hipStream_t st) {
     constexpr int QT = tile_rows(sizeof(T));
-    const size_t bytes = 4 * Tile<T, DH, QT>::BYTES + 2 * QT * 8 + (BIAS ? table_bytes(a) : 0);
+    const size_t bytes = 2 * stages(DH) * Tile<T, DH, QT>::BYTES + stages(DH) * QT * 8 + (BIAS ? table_bytes(a) : 0);
     auto* k = attend_dkv<T, DH, QT, W, BIAS>;
     GP_TRY(allow_lds(k, bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.HK * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);

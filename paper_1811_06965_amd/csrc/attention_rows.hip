@@ -13,33 +13,40 @@ namespace gp {
 namespace {
 
 // Sums of n rows of `width` floats, STEP rows at a time: out row x = rows x STEP .. of head blockIdx.y.
-constexpr int STEP = 32;
-__global__ void __launch_bounds__(256) distance_rows(const float* __restrict__ in, long n, int width, float* __restrict__ out) {
-    const long x = blockIdx.x, y = blockIdx.y, steps = gridDim.x;
-    const long r0 = x * STEP, r1 = min(n, r0 + STEP);
-    for (int d = threadIdx.x; d < width; d += 256) {
+constexpr int STEP = 128;
+// rows r0 .. r1 - 1 added up into sums[width]: the 1024 threads make groups that take every n-th row, whose sums are
+// added in order.
+__device__ __forceinline__ void add_rows(const float* in, long r0, long r1, int width, float* sums, float* groups) {
+    const int cols = min(1024, (width + 63) / 64 * 64), n = 1024 / cols, g = threadIdx.x / cols, c = threadIdx.x - g * cols;
+    for (int d0 = 0; d0 < width; d0 += cols) {
+        const int d = d0 + c;
         float s = 0.f;
+        if (d < width && g < n) {
 #pragma unroll 8
-        for (long r = r0; r < r1; ++r) s += in[(y * n + r) * width + d];
-        out[(y * steps + x) * width + d] = s;
+            for (long r = r0 + g; r < r1; r += n) s += in[r * width + d];
+        }
+        groups[threadIdx.x] = s;
+        __syncthreads();
+        if (d < width && g == 0) {
+            for (int x = 1; x < n; ++x) s += groups[x * cols + c];
+            sums[d] = s;
+        }
+        __syncthreads();
     }
 }
-// dbias of head blockIdx.x: its n rows of distances added up, then the distances of each bucket, in their order.
-__global__ void __launch_bounds__(256) distance_buckets(const float* __restrict__ in, long n, AttendArgs a) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int width = 2 * a.max_distance + 1;
-    float* sums = reinterpret_cast<float*>(lds);
-    int* of = reinterpret_cast<int*>(sums + width);
-    for (int d = threadIdx.x; d < width; d += 256) {
-        float s = 0.f;
-#pragma unroll 8
-        for (long r = 0; r < n; ++r) s += in[(blockIdx.x * n + r) * width + d];
-        sums[d] = s;
-        of[d] = min(max(a.bucket_of[d], 0), a.buckets - 1);
-    }
-    __syncthreads();
-    const int lane = threadIdx.x & 63;
-    for (int b = threadIdx.x >> 6; b < a.buckets; b += 4) {  // a wave per bucket
+__global__ void __launch_bounds__(1024) distance_rows(const float* __restrict__ in, long n, int width, float* __restrict__ out) {
+    __shared__ float groups[1024];
+    const long x = blockIdx.x, y = blockIdx.y, steps = gridDim.x;
+    add_rows(in + y * n * width, x * STEP, min(n, x * STEP + STEP), width, out + (y * steps + x) * width, groups);
+}
+// dbias of head blockIdx.x: its n rows of distances added up, then the distances of each bucket by a wave.
+__global__ void __launch_bounds__(1024) distance_buckets(const float* __restrict__ in, long n, AttendArgs a) {
+    __shared__ float groups[1024], sums[2 * GP_DISTANCE_MAX + 1];
+    __shared__ int of[2 * GP_DISTANCE_MAX + 1];
+    const int width = 2 * a.max_distance + 1, lane = threadIdx.x & 63;
+    for (int d = threadIdx.x; d < width; d += 1024) of[d] = min(max(a.bucket_of[d], 0), a.buckets - 1);
+    add_rows(in + blockIdx.x * n * width, 0, n, width, sums, groups);
+    for (int b = threadIdx.x >> 6; b < a.buckets; b += 16) {
         float s = 0.f;
         for (int d = lane; d < width; d += WAVE) s += of[d] == b ? sums[d] : 0.f;
         s = wave_sum(s);
@@ -65,21 +72,22 @@ Shape forward_shape(const AttendArgs& a) {
         s.splits = (int)std::max(1l, std::min<long>(std::min(64, tiles / (s.keys ? 4 * waves : 4)), 2048 / (groups * waves)));
     return s;
 }
-// Blocks of 128 rows (`rows` of them in each of `groups`), whose work is `tiles` tiles long.
-Shape backward_shape(long groups, int rows, long tiles) {
+// Blocks of 128 rows (`rows` of them in each of `groups`), whose work is `tiles` tiles long.  A tile is a few us of
+// fp32's products, but a fraction of one of bf16's.
+Shape backward_shape(const AttendArgs& a, long groups, int rows, long tiles) {
     Shape s;
     s.blocks = (rows + 32 * BW - 1) / (32 * BW);
     groups = std::max(1l, groups * s.blocks);
-    if (groups < 256) s.splits = (int)std::max(1l, std::min(std::min(32l, tiles / 2), 512 / groups));
+    if (groups < 256) s.splits = (int)std::max(1l, std::min(std::min(32l, a.dtype == GP_BF16 ? tiles / 2 : tiles), 512 / groups));
     return s;
 }
 Shape dq_shape(const AttendArgs& a) {
     const int kt = tile_rows(esize(a));
-    return backward_shape((long)a.B * a.H, a.Sq, (a.Sk + kt - 1) / kt);
+    return backward_shape(a, (long)a.B * a.H, a.Sq, (a.Sk + kt - 1) / kt);
 }
 Shape dkv_shape(const AttendArgs& a) {
     const int qt = tile_rows(esize(a));
-    return backward_shape((long)a.B * a.HK, a.Sk, (long)(a.H / a.HK) * ((a.Sq + qt - 1) / qt));
+    return backward_shape(a, (long)a.B * a.HK, a.Sk, (long)(a.H / a.HK) * ((a.Sq + qt - 1) / qt));
 }
 // Rows of distances of one head that the dQ kernel writes.
 long distance_rows_of(const AttendArgs& a) {
@@ -90,12 +98,12 @@ size_t distance_floats(const AttendArgs& a) {
     const size_t rows = (size_t)distance_rows_of(a);
     return a.bias ? a.H * (rows + (rows + STEP - 1) / STEP) * (2 * (size_t)a.max_distance + 1) : 0;
 }
-// The splits' sums: dQ's, then in the same place dK's and dV's.
+// The splits' sums of dQ, dK and dV.
 size_t part_floats(const AttendArgs& a) {
     const Shape q = dq_shape(a), k = dkv_shape(a);
     const size_t nq = q.splits > 1 ? (size_t)q.splits * a.B * a.H * a.Sq : 0;
     const size_t nk = k.splits > 1 ? (size_t)k.splits * a.B * a.HK * a.Sk * 2 : 0;
-    return std::max(nq, nk) * head_bucket(a.dh);
+    return (nq + nk) * head_bucket(a.dh);
 }
 
 } // namespace
@@ -136,11 +144,11 @@ gp_status attend_backward(AttendArgs a, bool exact, void* ws, hipStream_t st) {
     if (n > STEP) {
         float* out = dist + (size_t)a.H * n * width;
         const long steps = (n + STEP - 1) / STEP;
-        klaunch(distance_rows, dim3((unsigned)steps, (unsigned)a.H), dim3(256), 0, st, in, n, width, out);
+        klaunch(distance_rows, dim3((unsigned)steps, (unsigned)a.H), dim3(1024), 0, st, in, n, width, out);
         in = out;
         n = steps;
     }
-    klaunch(distance_buckets, dim3((unsigned)a.H), dim3(256), (uint32_t)(width * 8), st, in, n, a);
+    klaunch(distance_buckets, dim3((unsigned)a.H), dim3(1024), 0, st, in, n, a);
     GP_LAUNCH_CHECK();
     return GP_OK;
 }

@@ -4,6 +4,7 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <type_traits>
 
@@ -893,30 +894,48 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
     store_row<T, ND>(a.dv.at(wk.b, key, wk.h), dv, live ? 1.f : 0.f, a.dh, lane);
 }
 
-// A gradient's rows from the splits' sums [splits][B][heads][len][DH]: added up in order, times f.  Four features a thread.
-template <typename T, int DH>
-__global__ void __launch_bounds__(256) attend_sum(AttendArgs a, const float* __restrict__ part, HeadRows out, int heads, int len, float f) {
-    const long n = (long)a.B * heads * len, x = (long)blockIdx.x * 256 + threadIdx.x, row = x / (DH / 4);
+// The gradients' rows from the splits' sums [splits][B][heads][len][DH]: added up in order, times f.  Four features a thread,
+// a gradient per blockIdx.y.
+struct SumOf {
+    const float* part;
+    HeadRows out;
+    int heads, len, splits;
+    float f;
+};
+struct Sums {
+    SumOf of[3];
+};
+template <typename T, int DH> __global__ void __launch_bounds__(256) attend_sum(Sums sums, int B, int dh) {
+    const SumOf& o = sums.of[blockIdx.y];
+    const long n = (long)B * o.heads * o.len, x = (long)blockIdx.x * 256 + threadIdx.x, row = x / (DH / 4);
     const int d = (int)(x % (DH / 4)) * 4;
-    if (row >= n || d >= a.dh) return;
+    if (row >= n || d >= dh) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int i = 0; i < a.splits; ++i) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(part + (i * n + row) * DH + d);
+    for (int i = 0; i < o.splits; ++i) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(o.part + (i * n + row) * DH + d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += v[e];
     }
     typedef T vec __attribute__((ext_vector_type(4)));
     vec t;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = to_elt<T>(s[e] * f);
-    const long group = row / len;
-    *reinterpret_cast<vec*>(out.at((int)(group / heads), (int)(row - group * len), (int)(group % heads)) + d * (int)sizeof(T)) = t;
+    for (int e = 0; e < 4; ++e) t[e] = to_elt<T>(s[e] * o.f);
+    const long group = row / o.len;
+    *reinterpret_cast<vec*>(o.out.at((int)(group / o.heads), (int)(row - group * o.len), (int)(group % o.heads)) + d * (int)sizeof(T)) = t;
 }
 
 // ---------------------------------------------------------------- launches
-template <typename K> gp_status allow_lds(K* k, size_t bytes) {
-    if (bytes > 65536) GP_HIP(hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+// A kernel's dynamic LDS beyond 64 KB is allowed once per device.
+template <auto K> gp_status allow_lds(size_t bytes) {
+    static std::atomic<uint64_t> allowed{0};
+    if (bytes <= 65536) return GP_OK;
+    int dev = 0;
+    GP_HIP(hipGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (allowed.load(std::memory_order_relaxed) & bit) return GP_OK;
+    GP_HIP(hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, 159 * 1024));
+    if (dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
     return GP_OK;
 }
 size_t table_bytes(const AttendArgs& a) { return (2 * ((size_t)a.max_distance + PAD) + 1) * 4; }
@@ -924,8 +943,8 @@ size_t table_bytes(const AttendArgs& a) { return (2 * ((size_t)a.max_distance + 
 template <typename T, int DH, int KT, int W, bool BIAS, bool KEYS>
 gp_status launch_fwd(const AttendArgs& a, hipStream_t st) {
     const size_t bytes = (KEYS ? 4 * W : 2 * stages(DH)) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + 4 : 0) + (KEYS ? W * 32 * 8 : 0);
-    auto* k = attend_fwd<T, DH, KT, W, BIAS, KEYS>;
-    GP_TRY(allow_lds(k, bytes));
+    constexpr auto k = attend_fwd<T, DH, KT, W, BIAS, KEYS>;
+    GP_TRY(allow_lds<k>(bytes));
     klaunch(k, dim3((unsigned)((long)a.B * (a.H / a.pack) * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
     if (a.splits > 1)
         klaunch(attend_join<T, DH>, dim3((unsigned)(((long)a.B * a.H * a.Sq + 3) / 4)), dim3(256), 0, st, a);
@@ -938,19 +957,13 @@ template <typename T, int DH> gp_status forward(const AttendArgs& a, hipStream_t
     return a.bias ? launch_fwd<T, DH, KT, 4, true, false>(a, st) : launch_fwd<T, DH, KT, 4, false, false>(a, st);
 }
 
-template <typename T, int DH>
-void launch_sum(const AttendArgs& a, const float* part, const HeadRows& out, int heads, int len, float f, hipStream_t st) {
-    const long n = (long)a.B * heads * len * (DH / 4);
-    klaunch(attend_sum<T, DH>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, part, out, heads, len, f);
-}
 template <typename T, int DH, int W, bool BIAS, bool EXACT>
 gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
     constexpr int KT = tile_rows(sizeof(T));
     const size_t bytes = 2 * (BIAS ? 2 : stages(DH)) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + W * (SKEW + 2 * a.max_distance + 1) * 4 : 0);
-    auto* k = attend_dq<T, DH, KT, W, BIAS, EXACT>;
-    GP_TRY(allow_lds(k, bytes));
+    constexpr auto k = attend_dq<T, DH, KT, W, BIAS, EXACT>;
+    GP_TRY(allow_lds<k>(bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.H * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
-    if (a.splits > 1) launch_sum<T, DH>(a, a.part, a.dq, a.H, a.Sq, a.scale, st);
     GP_LAUNCH_CHECK();
     return GP_OK;
 }
@@ -958,13 +971,9 @@ template <typename T, int DH, int W, bool BIAS>
 gp_status launch_dkv(const AttendArgs& a, hipStream_t st) {
     constexpr int QT = tile_rows(sizeof(T));
     const size_t bytes = 2 * stages(DH) * Tile<T, DH, QT>::BYTES + stages(DH) * QT * 8 + (BIAS ? table_bytes(a) : 0);
-    auto* k = attend_dkv<T, DH, QT, W, BIAS>;
-    GP_TRY(allow_lds(k, bytes));
+    constexpr auto k = attend_dkv<T, DH, QT, W, BIAS>;
+    GP_TRY(allow_lds<k>(bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.HK * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
-    if (a.splits > 1) {
-        launch_sum<T, DH>(a, a.part, a.dk, a.HK, a.Sk, a.scale, st);
-        launch_sum<T, DH>(a, a.part + (size_t)a.splits * a.B * a.HK * a.Sk * DH, a.dv, a.HK, a.Sk, 1.f, st);
-    }
     GP_LAUNCH_CHECK();
     return GP_OK;
 }
@@ -981,7 +990,21 @@ template <typename T, int DH> gp_status backward(const AttendArgs& a, bool exact
     AttendArgs k = a;
     k.blocks = dkv.blocks;
     k.splits = dkv.splits;
+    const size_t nq = (size_t)a.B * a.H * a.Sq * DH, nk = (size_t)a.B * a.HK * a.Sk * DH;
+    if (q.splits > 1) k.part += q.splits * nq;
     if (k.blocks) GP_TRY(a.bias ? (launch_dkv<T, DH, BW, true>(k, st)) : (launch_dkv<T, DH, BW, false>(k, st)));
+    Sums sums;
+    int n = 0;
+    if (q.blocks && q.splits > 1) sums.of[n++] = {q.part, a.dq, a.H, a.Sq, q.splits, a.scale};
+    if (k.blocks && k.splits > 1) {
+        sums.of[n++] = {k.part, a.dk, a.HK, a.Sk, k.splits, a.scale};
+        sums.of[n++] = {k.part + k.splits * nk, a.dv, a.HK, a.Sk, k.splits, 1.f};
+    }
+    if (n) {
+        const size_t most = std::max(q.splits > 1 ? nq : 0, k.splits > 1 ? nk : 0) / 4;
+        klaunch(attend_sum<T, DH>, dim3((unsigned)((most + 255) / 256), n), dim3(256), 0, st, sums, a.B, a.dh);
+        GP_LAUNCH_CHECK();
+    }
     return GP_OK;
 }
 

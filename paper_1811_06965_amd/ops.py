@@ -459,14 +459,17 @@ def _attention_bytes(backward, *sizes):
 
 def _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, backward):
     """(config, gp_head_rows of q, k and v, bytes of scratch)."""
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t.dim() != 4 or t.dtype not in DTYPE:
-            raise ValueError(f"{name} must be [batch, len, heads, head_dim] in float32 or bfloat16")
+    if q.dim() != 4 or k.dim() != 4 or q.dtype not in DTYPE:
+        raise ValueError("q, k and v must be [batch, len, heads, head_dim] in float32 or bfloat16")
     B, Sq, H, dh = q.shape
     Sk, K = k.shape[1], k.shape[2]
     dev = _gpu(q)
-    for name, t in (("q_lens", q_lens), ("k_lens", k_lens), ("q_starts", q_starts)):
-        _vector(name, t, B, torch.int32, dev)
+    if q_lens is not None:
+        _vector("q_lens", q_lens, B, torch.int32, dev)
+    if k_lens is not None:
+        _vector("k_lens", k_lens, B, torch.int32, dev)
+    if q_starts is not None:
+        _vector("q_starts", q_starts, B, torch.int32, dev)
     cfg = gp.gp_attention_config(DTYPE[q.dtype], B, H, K, Sq, Sk, dh, causal, dh ** -0.5 if scale is None else scale,
                                  _ptr(q_lens), _ptr(k_lens), _ptr(q_starts))
     buckets = distance = 0
@@ -494,11 +497,11 @@ def attention(q, k, v, q_lens=None, k_lens=None, q_starts=None, causal=False, sc
     by itself: attention_backward gives the gradients."""
     _no_graph(q, k, v, None if bias is None else bias.table, gradient="attention_backward")
     cfg, rows, need = _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, 0)
-    dev = q.device
-    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    lse = torch.empty((cfg.batch, cfg.heads, cfg.q_len), dtype=torch.float32, device=dev)
+    dev, (B, Sq, H, dh) = q.device, q.shape
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    lse = torch.empty((B, H, Sq), dtype=torch.float32, device=dev)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    o = _head_rows("out", out, q, q.shape)
+    o = gp.gp_head_rows(out.data_ptr(), Sq * H * dh, H * dh, dh)
     _on(dev, lambda stream: gp.gp_attention(cfg, *rows, o, lse.data_ptr(), _ptr(ws), need, stream))
     return Attention(out, lse)
 

@@ -25,12 +25,13 @@ __device__ __forceinline__ Sum wave_join(Sum p, float c2) {
 }
 
 // A row's tokens in LDS.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 struct Named {
-    int id[GP_DISTILL_MAX];       // GP_NO_TOKEN: none, or not a token
-    float teacher[GP_DISTILL_MAX];
-    float x[GP_DISTILL_MAX];      // the student's logit, bounded
-    float first[GP_DISTILL_MAX];  // the same where the token is named for the first time, else a mask
-    int wrong;                    // an id that is not a token
+    alignas(16) int id[GP_DISTILL_MAX];        // negative: none, or not a token; so are those behind the last, in fours
+    alignas(16) float teacher[GP_DISTILL_MAX];
+    alignas(16) float x[GP_DISTILL_MAX];       // the student's logit, bounded
+    float first[GP_DISTILL_MAX];               // the same where the token is named for the first time, else a mask
+    int wrong;                                 // an id that is not a token
 };
 struct Logits {
     int V;
@@ -41,12 +42,16 @@ struct Logits {
     float scale, clip;
 };
 
-// Loads a row's tokens; a barrier must follow, then find_first (its results need another).
+// Loads a row's tokens; a barrier must follow, then find_first (whose results need another).
 template <typename T, bool CLIP>
 __device__ __forceinline__ void load_named(Named& s, const T* zr, const Logits& a, long row, int tid, int threads) {
     if (tid == 0) s.wrong = 0;
     const float lo = CLIP ? lower_bound(a.clip) : NEVER, hi = CLIP ? a.clip : INFINITY;
-    for (int j = tid; j < a.top; j += threads) {
+    for (int j = tid; j < (a.top + 3) / 4 * 4; j += threads) {
+        if (j >= a.top) {
+            s.id[j] = GP_NO_TOKEN;
+            continue;
+        }
         const int id = a.ids[row * a.top + j];
         const bool is = id >= 0 && id < a.V;
         s.id[j] = is ? id : id == GP_NO_TOKEN ? GP_NO_TOKEN : GP_NO_TOKEN - 1;
@@ -54,15 +59,18 @@ __device__ __forceinline__ void load_named(Named& s, const T* zr, const Logits& 
         if (is) s.x[j] = min_nan(max_nan(to_f32(zr[id]), lo), hi);
     }
 }
-__device__ __forceinline__ void find_first(Named& s, int top, int tid, int threads) {
+template <bool REST> __device__ __forceinline__ void find_first(Named& s, int top, int tid, int threads) {
     for (int j = tid; j < top; j += threads) {
         const int id = s.id[j];
-        if (id < 0) {
-            if (id != GP_NO_TOKEN) s.wrong = 1;
-            continue;
-        }
+        if (id < GP_NO_TOKEN) s.wrong = 1;
+        if (!REST || id < 0) continue;
         bool again = false;
-        for (int k = 0; k < j; ++k) again = again || s.id[k] == id;
+#pragma unroll 4
+        for (int k = 0; k < j; k += 4) {  // four at a time: one by one this took longer than the logits of a row
+            const i32x4 v = *reinterpret_cast<const i32x4*>(s.id + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) again = again || (v[e] == id && k + e < j);
+        }
         s.first[j] = again ? NEVER : s.x[j];
     }
 }
@@ -174,7 +182,7 @@ __global__ void __launch_bounds__(NT) distill_kernel(const T* __restrict__ z, Lo
     };
     load_named<T, CLIP>(named, zr, a, row, tid, NT);
     __syncthreads();
-    find_first(named, a.top, tid, NT);
+    find_first<REST>(named, a.top, tid, NT);
     const unsigned char* mark = reinterpret_cast<const unsigned char*>(marks);
     for (int w0 = c0; w0 < c1; w0 += WINDOW) {
         const int w1 = min(w0 + WINDOW, c1), f1 = min(w1, V / N);  // f1: whole chunks
@@ -234,7 +242,7 @@ __global__ void __launch_bounds__(64) distill_join_kernel(const T* __restrict__ 
     const int lane = threadIdx.x;
     load_named<T, CLIP>(named, z + row * a.ld, a, row, lane, WAVE);
     __syncthreads();
-    find_first(named, a.top, lane, WAVE);
+    find_first<REST>(named, a.top, lane, WAVE);
     __syncthreads();
     const Sum p = wave_join(lane < splits ? parts[row * splits + lane] : Sum{NO_REF, 0.f}, a.scale * LOG2E);
     finish_row<REST>(out, row, p, named, a, lane);
@@ -270,6 +278,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const T* z, Logits a,
     if (tid == 0) named.wrong = 0;
     float mine = 0.f;
     bool owner = false;
+    if (tid >= a.top && tid < (a.top + 3) / 4 * 4) named.id[tid] = GP_NO_TOKEN;
     if (tid < a.top) {
         const int id = a.ids[row * a.top + tid];
         const bool is = id >= 0 && id < V;
@@ -302,7 +311,8 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const T* z, Logits a,
         }
     }
     __syncthreads();
-    const float base = base_coef[0], coef = base_coef[1] * dloss, shift = named.first[0], total = named.first[1];
+    if (tid < (a.top + 3) / 4 * 4) named.x[tid] = tid < a.top ? expf(named.teacher[tid] - named.first[0]) : 0.f;  // q
+    const float base = base_coef[0], coef = base_coef[1] * dloss, total = named.first[1];
     const bool flat = named.wrong || lse == -INFINITY || named.first[2] == 0.f;  // the whole row is `fill`
     const float fill = named.wrong ? NAN : 0.f;
     auto bounded = [&](float x) { return CLIP ? min_nan(max_nan(x, -a.clip), a.clip) : x; };
@@ -342,15 +352,20 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const T* z, Logits a,
             if (f1 * N + e < V) dr[(long)f1 * N + e] = to_elt<T>(d[e]);
     }
     if (flat) return;
-    float q = 0.f;
-    if (owner)  // a token that is named twice has both its weights
-        for (int k = 0; k < a.top; ++k)
-            if (named.id[k] == named.id[tid]) q += expf(named.teacher[k] - shift);
     __syncthreads();
     if (owner) {
+        float q = 0.f;  // a token that is named twice has both its weights
+        const int id = named.id[tid];
+#pragma unroll 4
+        for (int k = 0; k < a.top; k += 4) {
+            const i32x4 v = *reinterpret_cast<const i32x4*>(named.id + k);
+            const f32x4 w = *reinterpret_cast<const f32x4*>(named.x + k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q += v[e] == id ? w[e] : 0.f;
+        }
         float d = dloss * (total * __builtin_amdgcn_exp2f(__builtin_fmaf(bounded(mine), a.scale, -lse) * LOG2E) - q);
         if (CLIP) d = fabsf(mine) > a.clip ? 0.f : d;
-        dr[named.id[tid]] = to_elt<T>(d);
+        dr[id] = to_elt<T>(d);
     }
 }
 

@@ -674,7 +674,7 @@ typedef struct {
     int batch, heads, kv_heads;    /* heads / kv_heads neighbouring query heads share a key and value head */
     int q_len, k_len, head_dim;    /* head_dim: whole 16 bytes, at most 128 */
     int causal;                    /* nonzero: keys up to the query's position alone */
-    float scale;                   /* > 0; 1 / sqrt(head_dim) as a rule */
+    float scale;                   /* in [1e-6, 1e6]; 1 / sqrt(head_dim) as a rule */
     const int* q_lens;             /* device int32 [batch]: rows in use of each sequence, cut to [0, q_len]; NULL: q_len */
     const int* k_lens;             /* the same of the keys; NULL: k_len */
     const int* q_starts;           /* device int32 [batch]; NULL: 0 */
@@ -700,7 +700,7 @@ typedef struct {
  * must not overlap the inputs (tensors beside each other in every period of a stride that both have are fine).
  * GP_ERR_INVALID_ARG: NULL tensors, sizes out of range (lengths up to 2^28, 65535 heads, batch x heads x
  *   (length / 128 + 1) below 2^24), heads not a multiple of kv_heads, an output that overlaps an input, a
- *   misaligned address or stride, scale not > 0, a bias without its buckets, a workspace that is NULL or too small.  GP_ERR_UNSUPPORTED: head_dim > 128, more buckets or a further
+ *   misaligned address or stride, scale out of range, a bias without its buckets, a workspace that is NULL or too small.  GP_ERR_UNSUPPORTED: head_dim > 128, more buckets or a further
  *   distance than above.
  */
 gp_status gp_attention(const gp_attention_config* cfg, const gp_head_rows* q, const gp_head_rows* k,

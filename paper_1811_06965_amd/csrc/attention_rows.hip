@@ -130,8 +130,8 @@ size_t attend_backward_workspace(const AttendArgs& a) {
 
 gp_status attend_backward(AttendArgs a, bool exact, void* ws, hipStream_t st) {
     a.stat_rows = (int)stat_rows(a.Sq);
-    a.stats = static_cast<f32x2*>(ws);
-    a.part = reinterpret_cast<float*>(a.stats + (size_t)a.B * a.H * a.stat_rows);
+    a.stats = static_cast<float*>(ws);
+    a.part = a.stats + (size_t)a.B * a.H * 2 * a.stat_rows;
     float* dist = a.part + part_floats(a);
     a.dist = a.bias && a.dbias ? dist : nullptr;
     if (a.B)
@@ -174,7 +174,7 @@ gp_status read_config(const gp_attention_config* c, AttendArgs& a, const char*& 
     if (c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads) return bad("heads must be a multiple of kv_heads");
     const int esz = c->dtype == GP_BF16 ? 2 : 4;
     if (c->head_dim < 1 || c->head_dim * esz % 16) return bad("head_dim must fill whole 16 bytes");
-    if (!(c->scale > 0.f) || !(c->scale <= FLT_MAX)) return bad("scale must be finite and > 0");
+    if (!(c->scale >= 1e-6f && c->scale <= 1e6f)) return bad("scale must be in [1e-6, 1e6]");
     for (const int* p : {c->q_lens, c->k_lens, c->q_starts})
         if (!aligned(p, 4)) return bad("misaligned lengths or positions");
     if (c->bias) {

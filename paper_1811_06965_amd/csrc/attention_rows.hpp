@@ -27,7 +27,7 @@ struct AttendArgs {
     // set by the launchers
     int keys = 0, pack = 1, blocks = 0, splits = 1, stat_rows = 0;
     float* part = nullptr;   // splits' sums: [splits][B H Sq][width], the forward's then followed by their (reference, sum) pairs
-    f32x2* stats = nullptr;  // (lse / log 2, delta) of each row: [B, H, stat_rows]
+    float* stats = nullptr;  // lse / log 2, then delta, of each row (negative, the first over the scale, where sums start from them): [B, H, 2, stat_rows]
     float* dist = nullptr;   // sums of dS by distance: [H][B blocks splits][2 max_distance + 1]
 };
 

@@ -44,12 +44,16 @@ __device__ __forceinline__ f32x16 mma(const f32x4& a, const f32x4& b, f32x16 c) 
     for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
     return c;
 }
-__device__ __forceinline__ f32x16 zero16() {
+__device__ __forceinline__ f32x16 splat16(float x) {
     f32x16 z;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    for (int i = 0; i < 16; ++i) z[i] = x;
     return z;
 }
+__device__ __forceinline__ f32x16 zero16() { return splat16(0.f); }
+// The backward's products start from -lse / c and -delta, which saves their subtractions: in bf16, whose vector
+// instructions bound it.  fp32's products take long, and each of their many sums would be rounded at the lse's size.
+template <typename T> constexpr bool starts_sums() { return sizeof(T) == 2; }
 // Row (within a block of 32) of accumulator register r; the column is lane % 32.
 __device__ __forceinline__ int acc_row(int r, int lane) { return (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3); }
 
@@ -626,6 +630,7 @@ template <typename T, int DH, int KT, int W, bool BIAS, bool EXACT>
 __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     typedef Tile<T, DH, KT> Tl;
     constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, ST = BIAS ? 2 : stages(DH), TB = 2 * Tl::BYTES;
+    constexpr bool INIT = starts_sums<T>() && BIAS;  // without a bias its registers cost the third wave: 63 us for 57
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     float* const table = reinterpret_cast<float*>(lds + ST * TB);
     const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
@@ -634,7 +639,7 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     const int row0 = (wk.blk * W + wave) * 32, i = row0 + (lane & 31), hk = wk.h / (a.H / a.HK);
     const bool in = i < a.Sq, live = i < len.q;
     const int pos = i + len.start, pos0 = row0 + len.start;
-    const long stat = ((long)wk.b * a.H + wk.h) * a.stat_rows;
+    const long stat = ((long)wk.b * a.H + wk.h) * 2 * a.stat_rows;
 
     bool masks = false;
     if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
@@ -680,10 +685,11 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         if (t + ST - 1 < end) stage(t + ST - 1, ring<ST>(buf, ST - 1));
     };
     const float c = a.scale * LOG2E;
-    // the weights of one block (s) and dP (dp); -INFINITY marks a masked pair's weight where `mark` asks for it
-    auto block = [&](const char* ks, const char* vs, int k0, int kb, bool edge, bool mark, f32x16& s, f32x16& dp) {
-        s = zero16();
-        dp = zero16();
+    const f32x16 s0 = splat16(INIT ? -lse2 / c : 0.f);
+    // the weights of one block (s) and dP from dp0 on (dp); -INFINITY marks a masked pair's weight where `mark` asks for it
+    auto block = [&](const char* ks, const char* vs, int k0, int kb, bool edge, bool mark, const f32x16& dp0, f32x16& s, f32x16& dp) {
+        s = s0;
+        dp = dp0;
 #pragma unroll
         for (int x = 0; x < NK; ++x) {
             if (!Tl::has(x, a.dh)) continue;
@@ -693,7 +699,8 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         const Near n(table, a, BIAS ? k0 - pos0 - 31 : 0, BIAS ? k0 + 4 * (lane >> 5) - pos : 0);
         if (BIAS) n.add<1>(s, c);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = exp2_hw(BIAS ? s[e] - lse2 : __builtin_fmaf(s[e], c, -lse2));
+        for (int e = 0; e < 16; ++e)
+            s[e] = exp2_hw(INIT ? (BIAS ? s[e] : s[e] * c) : BIAS ? s[e] - lse2 : __builtin_fmaf(s[e], c, -lse2));
         auto hide = [&](int e) {
             s[e] = mark ? -INFINITY : 0.f;
             dp[e] = 0.f;
@@ -718,7 +725,7 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
                 f32x16 s, dp;
-                block(ks, vs, t * KT + kb * 32, kb, tile_edge(t), false, s, dp);
+                block(ks, vs, t * KT + kb * 32, kb, tile_edge(t), false, zero16(), s, dp);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sum[e & 3] = __builtin_fmaf(s[e], dp[e], sum[e & 3]);
             }
@@ -726,6 +733,7 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         delta = both_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
         lds_barrier();
     }
+    const f32x16 dp0 = splat16(INIT ? -delta : 0.f);
     f32x16 dq[ND];
     auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
@@ -741,10 +749,10 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
 #pragma unroll 1
             for (int kb = 0; kb < NB; ++kb) {
                 f32x16 s, dp;
-                block(ks, vs, t * KT + kb * 32, kb, edge, CAREFUL, s, dp);
+                block(ks, vs, t * KT + kb * 32, kb, edge, CAREFUL, dp0, s, dp);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float d = s[e] * (dp[e] - delta);
+                    const float d = s[e] * (INIT ? dp[e] : dp[e] - delta);
                     s[e] = !CAREFUL ? d : s[e] == -INFINITY ? s[e] : d == -INFINITY ? NAN : d;
                 }
                 Tl::template add<CAREFUL>(ks, kb * 32, s, lane, dq);
@@ -764,9 +772,10 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         store_row<float, ND>(reinterpret_cast<char*>(a.part + ((((long)wk.split * a.B + wk.b) * a.H + wk.h) * a.Sq + i) * DH), dq, live ? 1.f : 0.f, DH, lane);
     else if (in)
         store_row<T, ND>(a.dq.at(wk.b, i, wk.h), dq, live ? a.scale : 0.f, a.dh, lane);
-    if (wk.split == 0 && lane < 32 && i < a.stat_rows) a.stats[stat + i] = f32x2{lse2, delta};
-    if (wk.split == 0 && wk.blk == a.blocks - 1)  // the rows that a tile of queries may read behind the last one
-        for (int x = a.blocks * W * 32 + (int)threadIdx.x; x < a.stat_rows; x += 64 * W) a.stats[stat + x] = f32x2{INFINITY, 0.f};
+    if (wk.split == 0 && lane < 32 && i < a.stat_rows) {
+        a.stats[stat + i] = starts_sums<T>() ? -lse2 / c : lse2;
+        a.stats[stat + a.stat_rows + i] = starts_sums<T>() ? -delta : delta;
+    }
     if (BIAS && a.dist) {
         dist.finish();
         __syncthreads();
@@ -787,9 +796,10 @@ template <typename T, int DH, int QT, int W, bool BIAS>
 __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
     typedef Tile<T, DH, QT> Tl;
     constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = QT / 32, ST = stages(DH), TB = 2 * Tl::BYTES;
+    constexpr bool INIT = starts_sums<T>();
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    f32x2* const stats = reinterpret_cast<f32x2*>(lds + ST * TB);  // of the tiles' rows
-    float* const table = reinterpret_cast<float*>(stats + ST * QT);
+    float* const stats = reinterpret_cast<float*>(lds + ST * TB);  // of the tiles' rows: two planes of 64
+    float* const table = stats + ST * 128;
     const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
     const Work wk(a.blocks, a.HK, a.splits, false);
     const Lens len(a, wk.b);
@@ -820,15 +830,15 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
             if (ta >= tb) continue;
             const int h = wk.h * group + g;
             const char *qp = a.q.at(wk.b, 0, h), *gp = a.dout.at(wk.b, 0, h);
-            const f32x2* sp = a.stats + ((long)wk.b * a.H + h) * a.stat_rows;
+            const float* sp = a.stats + ((long)wk.b * a.H + h) * 2 * a.stat_rows;
             auto stage = [&](int t, int buf) {
                 char* s = lds + buf * TB;
                 ql(s, qp + (long)t * QT * a.q.row, len.q - t * QT, a.q.row, a.dh, wave);
                 gl(s + Tl::BYTES, gp + (long)t * QT * a.dout.row, len.q - t * QT, a.dout.row, a.dh, wave);
-                // 32 rows' pairs a load; each wave issues one, so that all have as many on their way
-                const int part = wave % (QT / 32);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(sp + t * QT, QT * 8), (LdsPtr)(stats + buf * QT + part * 32), 4,
-                                                         part * 256 + lane * 4, 0, 0, 0);
+                // a plane a load (zeros behind QT rows); each wave issues one, so that all have as many on their way
+                const int plane = wave & 1;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(sp + plane * a.stat_rows + t * QT, QT * 4), (LdsPtr)(stats + buf * 128 + plane * 64),
+                                                         4, lane * 4, 0, 0, 0);
             };
             __syncthreads();  // the last head's tiles are done with
             if (BIAS) masks = masks | (__syncthreads_or(load_table(table, a, h, threadIdx.x, 64 * W)) != 0);
@@ -845,7 +855,19 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                 const bool edge = t * QT + QT > len.q || (a.causal && pos0 < k0 + 31);
 #pragma unroll 1
                 for (int qb = 0; qb < NB; ++qb) {
-                    f32x16 s = zero16(), dp = zero16();
+                    // rows of the registers: (reference, delta) as the dQ kernel left them
+                    const float* st = stats + buf * 128 + qb * 32 + 4 * (lane >> 5);
+                    f32x16 lse, delta;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(st + 2 * e), y = *reinterpret_cast<const f32x4*>(st + 64 + 2 * e);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            lse[e + k] = x[k];
+                            delta[e + k] = y[k];
+                        }
+                    }
+                    f32x16 s = INIT ? lse : zero16(), dp = INIT ? delta : zero16();
 #pragma unroll
                     for (int x = 0; x < NK; ++x) {
                         if (!Tl::has(x, a.dh)) continue;
@@ -855,14 +877,12 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                     const int p0 = pos0 + qb * 32;
                     // distances fall with the register here
                     const Near n(table, a, BIAS ? k0 - p0 - 31 : 0, BIAS ? key - p0 - 4 * (lane >> 5) : 0);
-                    const f32x2* st = stats + buf * QT + qb * 32 + 4 * (lane >> 5);
                     f32x16 ds;
                     if (BIAS) n.add<-1>(s, c);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const f32x2 row = st[(e >> 2) * 8 + (e & 3)];
-                        s[e] = exp2_hw(BIAS ? s[e] - row[0] : __builtin_fmaf(s[e], c, -row[0]));
-                        ds[e] = s[e] * (dp[e] - row[1]);
+                        s[e] = exp2_hw(INIT ? (BIAS ? s[e] : s[e] * c) : BIAS ? s[e] - lse[e] : __builtin_fmaf(s[e], c, -lse[e]));
+                        ds[e] = s[e] * (INIT ? dp[e] : dp[e] - delta[e]);
                         if (CAREFUL && ds[e] == -INFINITY) ds[e] = NAN;
                     }
                     auto hide = [&](int e) { s[e] = ds[e] = CAREFUL ? -INFINITY : 0.f; };
@@ -970,7 +990,7 @@ gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
 template <typename T, int DH, int W, bool BIAS>
 gp_status launch_dkv(const AttendArgs& a, hipStream_t st) {
     constexpr int QT = tile_rows(sizeof(T));
-    const size_t bytes = 2 * stages(DH) * Tile<T, DH, QT>::BYTES + stages(DH) * QT * 8 + (BIAS ? table_bytes(a) : 0);
+    const size_t bytes = 2 * stages(DH) * Tile<T, DH, QT>::BYTES + stages(DH) * 512 + (BIAS ? table_bytes(a) : 0);
     constexpr auto k = attend_dkv<T, DH, QT, W, BIAS>;
     GP_TRY(allow_lds<k>(bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.HK * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);

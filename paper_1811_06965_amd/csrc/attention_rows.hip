@@ -89,9 +89,9 @@ Shape dkv_shape(const AttendArgs& a) {
     const int qt = tile_rows(esize(a));
     return backward_shape(a, (long)a.B * a.HK, a.Sk, (long)(a.H / a.HK) * ((a.Sq + qt - 1) / qt));
 }
-// Rows of distances of one head that the dQ kernel writes.
+// Rows of distances of one head that the dK and dV kernel writes.
 long distance_rows_of(const AttendArgs& a) {
-    const Shape s = dq_shape(a);
+    const Shape s = dkv_shape(a);
     return (long)a.B * s.blocks * s.splits;
 }
 size_t distance_floats(const AttendArgs& a) {
@@ -425,7 +425,7 @@ gp_status gp_attention_backward(const gp_attention_config* cfg, const gp_head_ro
     a.dv = grad[2].t;
     a.lse_in = lse;
     a.dbias = dbias;
-    return attend_backward(a, !out || (a.bias && a.dtype == GP_BF16), ws, (hipStream_t)stream);
+    return attend_backward(a, !out, ws, (hipStream_t)stream);
 }
 
 } // extern "C"

@@ -104,17 +104,18 @@ template <typename T, int DH, int R> struct Tile {
     // themselves: as builtins they count as writes, before which the compiler waits for the tiles on their way.
     template <int ND> struct Columns {
         bf16x8 x[2][ND];
-        __device__ __forceinline__ Columns(const char* s, int row0, int lane) {
+        // of the 32 features from 32 first on
+        __device__ __forceinline__ Columns(const char* s, int row0, int lane, int first = 0) {
             const int g = lane >> 4, q = lane & 15, r = row0 + 4 * (g >> 1) + (q >> 2), col = 16 * (g & 1) + 4 * (q & 3);
             const uint32_t at = (uint32_t)(size_t)(LdsPtr)s + r * 128 + (col & 7) * 2;
             // rows 8 on: swizzle ^ 2; features 32 on: chunk ^ 4; rows 16 on and parts of 64 features: a constant further
-            const uint32_t a0 = at + (((col >> 3) ^ swizzle(r)) << 4), a1 = (a0 ^ 32) + 1024;
+            const uint32_t a0 = (at + (((col >> 3) ^ swizzle(r)) << 4)) ^ ((first & 1) << 6), a1 = (a0 ^ 32) + 1024;
 #pragma unroll
             for (int d = 0; d < ND; d += 2) {
                 if (d + 1 < ND)
-                    read(a0, a1, a0 ^ 64, a1 ^ 64, d / 2, x[0][d], x[1][d], x[0][d + 1], x[1][d + 1]);
+                    read(a0, a1, a0 ^ 64, a1 ^ 64, (first + d) / 2, x[0][d], x[1][d], x[0][d + 1], x[1][d + 1]);
                 else
-                    read(a0, a1, d / 2, x[0][d], x[1][d]);
+                    read(a0, a1, (first + d) / 2, x[0][d], x[1][d]);
             }
         }
         static __device__ __forceinline__ bf16x8 pair(i32x2 x, i32x2 y) { return __builtin_bit_cast(bf16x8, i32x4{x[0], x[1], y[0], y[1]}); }
@@ -158,60 +159,87 @@ template <typename T, int DH, int R> struct Tile {
     // where an unmasked pair holds +inf or -inf (a NaN counts as both), which is then added.
     template <bool CAREFUL, int ND>
     static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, int lane, f32x16 (&acc)[ND]) {
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2 && CAREFUL) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {  // one by one, in fewer registers
+                f32x16 one[1] = {acc[d]};
+                add_columns<CAREFUL>(Columns<1>(s, row0, lane, d), w, one);
+                acc[d] = one[0];
+            }
+        } else if constexpr (sizeof(T) == 2)
+            add_columns<CAREFUL>(Columns<ND>(s, row0, lane), w, acc);
+        else
+            add_elements<CAREFUL>(s, row0, w, lane, acc);
+    }
+    // Two sums from one reading of the rows.
+    template <bool CAREFUL, int ND>
+    static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, const f32x16& w2, int lane, f32x16 (&acc)[ND],
+                                               f32x16 (&acc2)[ND]) {
+        static_assert(sizeof(T) == 2, "fp32 reads its elements one by one");
+        if constexpr (CAREFUL) {
+            add<CAREFUL>(s, row0, w, lane, acc);
+            add<CAREFUL>(s, row0, w2, lane, acc2);
+        } else {
             const Columns<ND> c(s, row0, lane);
+            add_columns<CAREFUL>(c, w, acc);
+            add_columns<CAREFUL>(c, w2, acc2);
+        }
+    }
+    template <bool CAREFUL, int ND>
+    static __device__ __forceinline__ void add_columns(const Columns<ND>& c, const f32x16& w, f32x16 (&acc)[ND]) {
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc) {
-                bf16x8 b, seen;
+        for (int cc = 0; cc < 2; ++cc) {
+            bf16x8 b, seen;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = w[8 * cc + e];
-                    b[e] = (bf16)(CAREFUL && x == -INFINITY ? 0.f : x);
-                    if (CAREFUL) seen[e] = (bf16)(x == -INFINITY ? 0.f : 1.f);
+            for (int e = 0; e < 8; ++e) {
+                const float x = w[8 * cc + e];
+                b[e] = (bf16)(CAREFUL && x == -INFINITY ? 0.f : x);
+                if (CAREFUL) seen[e] = (bf16)(x == -INFINITY ? 0.f : 1.f);
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                if (!CAREFUL) {
+                    acc[d] = mma(c.x[cc][d], b, acc[d]);
+                    continue;
                 }
+                bf16x8 f;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    if (!CAREFUL) {
-                        acc[d] = mma(c.x[cc][d], b, acc[d]);
-                        continue;
-                    }
-                    bf16x8 f;
+                for (int e = 0; e < 8; ++e) f[e] = (bf16)finite((float)c.x[cc][d][e]);
+                acc[d] = mma(f, b, acc[d]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] = (bf16)finite((float)c.x[cc][d][e]);
-                    acc[d] = mma(f, b, acc[d]);
+                for (int which = 0; which < 2; ++which) {
+                    const float inf = which ? -INFINITY : INFINITY;
 #pragma unroll
-                    for (int which = 0; which < 2; ++which) {
-                        const float inf = which ? -INFINITY : INFINITY;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] = (bf16)(infinite((float)c.x[cc][d][e], inf) ? 1.f : 0.f);
-                        found(mma(f, seen, zero16()), inf, acc[d]);
-                    }
+                    for (int e = 0; e < 8; ++e) f[e] = (bf16)(infinite((float)c.x[cc][d][e], inf) ? 1.f : 0.f);
+                    found(mma(f, seen, zero16()), inf, acc[d]);
                 }
             }
-        } else {
-#pragma unroll
-            for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float y = w[8 * cc + e];
-                        x[e] = element(s, row0 + acc_row(8 * cc + e, lane), d * 32, lane);
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(CAREFUL ? finite(x[e]) : x[e], CAREFUL && y == -INFINITY ? 0.f : y, acc[d], 0, 0, 0);
-                    }
-                    if (!CAREFUL) continue;
-#pragma unroll
-                    for (int which = 0; which < 2; ++which) {
-                        const float inf = which ? -INFINITY : INFINITY;
-                        f32x16 n = zero16();
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            n = __builtin_amdgcn_mfma_f32_32x32x2f32(infinite(x[e], inf) ? 1.f : 0.f, w[8 * cc + e] == -INFINITY ? 0.f : 1.f, n, 0, 0, 0);
-                        found(n, inf, acc[d]);
-                    }
-                }
         }
+    }
+    template <bool CAREFUL, int ND>
+    static __device__ __forceinline__ void add_elements(const char* s, int row0, const f32x16& w, int lane, f32x16 (&acc)[ND]) {
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = w[8 * cc + e];
+                    x[e] = element(s, row0 + acc_row(8 * cc + e, lane), d * 32, lane);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(CAREFUL ? finite(x[e]) : x[e], CAREFUL && y == -INFINITY ? 0.f : y, acc[d], 0, 0, 0);
+                }
+                if (!CAREFUL) continue;
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {
+                    const float inf = which ? -INFINITY : INFINITY;
+                    f32x16 n = zero16();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        n = __builtin_amdgcn_mfma_f32_32x32x2f32(infinite(x[e], inf) ? 1.f : 0.f, w[8 * cc + e] == -INFINITY ? 0.f : 1.f, n, 0, 0, 0);
+                    found(n, inf, acc[d]);
+                }
+            }
     }
     static __device__ __forceinline__ float finite(float x) { return x - x == 0.f ? x : 0.f; }
     static __device__ __forceinline__ bool infinite(float x, float which) { return x == which || x != x; }
@@ -588,23 +616,26 @@ struct Distances {
         for (int i = lane; i < 2 * D + 1; i += WAVE) sums[i] = 0.f;
         low = high = 0.f;
     }
-    // lo: distance of the block's first key from its last query
-    __device__ __forceinline__ void add(const f32x16& ds, int lo) {
+    // lo: distance of the block's first key from its last query.  MARKED: a pair of -INFINITY is a masked one
+    template <bool MARKED> __device__ __forceinline__ void add(const f32x16& ds, int lo) {
+        const auto value = [](float x) { return MARKED && x == -INFINITY ? 0.f : x; };
         if (lo >= D || lo + 62 <= -D) {
             float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e & 3] += ds[e];
+            for (int e = 0; e < 16; ++e) s[e & 3] += value(ds[e]);
             const float x = (s[0] + s[1]) + (s[2] + s[3]);
             if (lo >= D) high += x; else low += x;
             return;
         }
-        float* p = skew + (lane & 31) * 63 + 31 + 4 * (lane >> 5);
+        float* p = skew + 4 * (lane >> 5) * 63 + 31 + (lane & 31);  // query row r of the block, key lane % 32: row r, place 31 - r + key
 #pragma unroll
-        for (int e = 0; e < 16; ++e) p[(e >> 2) * 8 + (e & 3)] = ds[e];
+        for (int e = 0; e < 16; ++e) p[((e >> 2) * 8 + (e & 3)) * 63] = value(ds[e]);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 8)  // in steps: few registers
 #pragma unroll
-        for (int i = 0; i < 32; ++i) s[i & 3] += skew[i * 64 + lane];
+            for (int j = 0; j < 8; ++j) s[j & 3] += skew[(i + j) * 64 + lane];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const float x = (s[0] + s[1]) + (s[2] + s[3]);
         const int rel = lo + lane;  // lane 63 has no pairs
@@ -623,13 +654,19 @@ struct Distances {
 
 // dQ: a wave owns 32 queries and goes through the keys as the forward does:
 //   P = 2^(S - lse), dP^T = V dO^T, dS = P (dP - delta), dQ^T += K^T dS^T.
-// delta_i = sum_j P_ij dP_ij = dO_i . O_i.  EXACT takes the first form, in a pass of its own over the keys: O in bf16
-// is off by up to 2^-8 of itself, and so would each row's sum of dS be, which all the row's pairs share and the bias's
-// gradient adds up.  Writes (lse, delta) of each row for dK and dV.
-template <typename T, int DH, int KT, int W, bool BIAS, bool EXACT>
+// delta_i = sum_j P_ij dP_ij = dO_i . O_i.  O in bf16 is off by up to 2^-8 of itself, and so would each row's sum of dS be,
+// which all the row's pairs share and the bias's gradient adds up.  So delta is made
+//   FROM_OUT: by the second form (fp32, and calls without a bias);
+//   FROM_WEIGHTS: by the first, in a pass of its own over the keys;
+//   REFINED: by the second, d, and with the sums of dS' = P (dP - d), which are the error e = delta - d (the weights add
+//   up to 1), and dQ'^T = K^T dS'^T, R^T = K^T P^T, dQ = dQ' - e R: one product for the three, and the
+//   exponential, of a pass of its own.  4 x 2048 queries, 16 heads of 64: 280 us by a pass, 175 refined.
+// Writes (lse, delta) of each row for dK and dV.
+enum Delta { FROM_OUT, FROM_WEIGHTS, REFINED };
+template <typename T, int DH, int KT, int W, bool BIAS, int DELTA>
 __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     typedef Tile<T, DH, KT> Tl;
-    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, ST = BIAS ? 2 : stages(DH), TB = 2 * Tl::BYTES;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, ST = stages(DH), TB = 2 * Tl::BYTES;
     constexpr bool INIT = starts_sums<T>() && BIAS;  // without a bias its registers cost the third wave: 63 us for 57
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     float* const table = reinterpret_cast<float*>(lds + ST * TB);
@@ -643,14 +680,13 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
 
     bool masks = false;
     if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
-    Distances dist(table + (BIAS ? table_size(a) : 0), a.max_distance, wave, W, lane);
 
     typename Elt<T>::frag qf[NK], gf[NK];
     const int ic = min(i, a.Sq - 1);
     load_row<T>(a.q.at(wk.b, ic, wk.h), live, a.dh, lane, qf);
     load_row<T>(a.dout.at(wk.b, ic, wk.h), live, a.dh, lane, gf);
     float delta = 0.f;
-    if (!EXACT) {
+    if (DELTA != FROM_WEIGHTS) {
         typename Elt<T>::frag of[NK];
         load_row<T>(a.o.at(wk.b, ic, wk.h), live, a.dh, lane, of);
 #pragma unroll
@@ -715,7 +751,7 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     };
     const bool short_rows = row0 + 32 > len.q;  // a row that is not in use has no weights, whatever the keys hold
     auto tile_edge = [&](int t) { return short_rows || t * KT + KT > len.k || (a.causal && t * KT + KT - 1 > pos0); };
-    if (EXACT) {
+    if (DELTA == FROM_WEIGHTS) {
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         first_tiles(0, tiles);
         for (int t = 0, buf = 0; t < tiles; ++t, buf = ring<ST>(buf, 1)) {
@@ -734,12 +770,13 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         lds_barrier();
     }
     const f32x16 dp0 = splat16(INIT ? -delta : 0.f);
-    f32x16 dq[ND];
+    f32x16 dq[ND], r[DELTA == REFINED ? ND : 1];
+    float error = 0.f;
     auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
-        if (BIAS && a.dist) dist.clear();
+        error = 0.f;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) dq[d] = zero16();
+        for (int d = 0; d < ND; ++d) dq[d] = r[DELTA == REFINED ? d : 0] = zero16();
         first_tiles(t0, t1);
         for (int t = t0, buf = 0; t < t1; ++t, buf = ring<ST>(buf, 1)) {
             next_tile(t, t1, buf);
@@ -750,23 +787,33 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
             for (int kb = 0; kb < NB; ++kb) {
                 f32x16 s, dp;
                 block(ks, vs, t * KT + kb * 32, kb, edge, CAREFUL, dp0, s, dp);
+                f32x16 ds;
+                float sum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float d = s[e] * (INIT ? dp[e] : dp[e] - delta);
-                    s[e] = !CAREFUL ? d : s[e] == -INFINITY ? s[e] : d == -INFINITY ? NAN : d;
+                    ds[e] = s[e] * (INIT ? dp[e] : dp[e] - delta);
+                    if (CAREFUL) ds[e] = s[e] == -INFINITY ? s[e] : ds[e] == -INFINITY ? NAN : ds[e];
+                    if (DELTA == REFINED) sum[e & 1] += CAREFUL && s[e] == -INFINITY ? 0.f : ds[e];
                 }
-                Tl::template add<CAREFUL>(ks, kb * 32, s, lane, dq);
-                if (CAREFUL) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] = s[e] == -INFINITY ? 0.f : s[e];
-                }
-                if (BIAS && a.dist) dist.add(s, t * KT + kb * 32 - pos0 - 31);
+                error += sum[0] + sum[1];
+                if constexpr (DELTA == REFINED)
+                    Tl::template add<CAREFUL>(ks, kb * 32, ds, s, lane, dq, r);
+                else
+                    Tl::template add<CAREFUL>(ks, kb * 32, ds, lane, dq);
             }
         }
     };
     pass(std::false_type{});
     if (a.causal || masks) {
         if (__syncthreads_or(!all_finite(dq))) pass(std::true_type{});
+    }
+    if constexpr (DELTA == REFINED) {
+        error = both_sum(error);
+        delta += error;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dq[d][e] = __builtin_fmaf(-error, r[d][e], dq[d][e]);
     }
     if (in && a.splits > 1)
         store_row<float, ND>(reinterpret_cast<char*>(a.part + ((((long)wk.split * a.B + wk.b) * a.H + wk.h) * a.Sq + i) * DH), dq, live ? 1.f : 0.f, DH, lane);
@@ -776,26 +823,15 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         a.stats[stat + i] = starts_sums<T>() ? -lse2 / c : lse2;
         a.stats[stat + a.stat_rows + i] = starts_sums<T>() ? -delta : delta;
     }
-    if (BIAS && a.dist) {
-        dist.finish();
-        __syncthreads();
-        const int n = 2 * a.max_distance + 1;
-        float* out = a.dist + ((((long)wk.h * a.B + wk.b) * a.blocks + wk.blk) * a.splits + wk.split) * n;
-        const float* sums = table + table_size(a) + W * SKEW;
-        for (int d = threadIdx.x; d < n; d += 64 * W) {
-            float x = sums[d];
-            for (int w = 1; w < W; ++w) x += sums[w * n + d];
-            out[d] = x;
-        }
-    }
 }
 
 // dK and dV: a wave owns 32 keys and goes through the queries of all the heads that share them, in tiles of QT:
-//   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+//   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS,
+// and dS by distance for the bias's gradient.
 template <typename T, int DH, int QT, int W, bool BIAS>
-__global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
+__global__ void __launch_bounds__(64 * W, DH <= 64 ? 2 : 1) attend_dkv(AttendArgs a) {
     typedef Tile<T, DH, QT> Tl;
-    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = QT / 32, ST = stages(DH), TB = 2 * Tl::BYTES;
+    constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = QT / 32, ST = BIAS ? 2 : stages(DH), TB = 2 * Tl::BYTES;
     constexpr bool INIT = starts_sums<T>();
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     float* const stats = reinterpret_cast<float*>(lds + ST * TB);  // of the tiles' rows: two planes of 64
@@ -819,6 +855,8 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
     const typename Tl::template Loader<W> ql(a.q.row, a.dh, wave, lane), gl(a.dout.row, a.dh, wave, lane);
     const float c = a.scale * LOG2E;
     bool masks = false;
+    Distances dist(table + (BIAS ? table_size(a) : 0), a.max_distance, wave, W, lane);
+    const int distances = 2 * a.max_distance + 1;
     f32x16 dk[ND], dv[ND];
     auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
@@ -827,8 +865,13 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
         for (int g = 0; g < group; ++g) {
             const long at = (long)g * (t1 - t0);  // of this head's first tile
             const int ta = t0 + (int)max(0l, u0 - at), tb = t0 + (int)min((long)(t1 - t0), u1 - at);
-            if (ta >= tb) continue;
             const int h = wk.h * group + g;
+            float* const dist_out = BIAS ? a.dist + ((((long)h * a.B + wk.b) * a.blocks + wk.blk) * a.splits + wk.split) * distances : nullptr;
+            if (ta >= tb) {
+                if (BIAS && a.dist)
+                    for (int x = threadIdx.x; x < distances; x += 64 * W) dist_out[x] = 0.f;
+                continue;
+            }
             const char *qp = a.q.at(wk.b, 0, h), *gp = a.dout.at(wk.b, 0, h);
             const float* sp = a.stats + ((long)wk.b * a.H + h) * 2 * a.stat_rows;
             auto stage = [&](int t, int buf) {
@@ -842,6 +885,7 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
             };
             __syncthreads();  // the last head's tiles are done with
             if (BIAS) masks = masks | (__syncthreads_or(load_table(table, a, h, threadIdx.x, 64 * W)) != 0);
+            if (BIAS && a.dist) dist.clear();
 #pragma unroll
             for (int x = 0; x < ST - 1; ++x)
                 if (ta + x < tb) stage(ta + x, x);
@@ -852,7 +896,7 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                 const int pos0 = t * QT + len.start;
                 if (k0 >= len.k || (a.causal && pos0 + QT - 1 < k0)) continue;
                 const char *qs = lds + buf * TB, *gs = qs + Tl::BYTES;
-                const bool edge = t * QT + QT > len.q || (a.causal && pos0 < k0 + 31);
+                const bool edge = t * QT + QT > len.q || k0 + 32 > len.k || (a.causal && pos0 < k0 + 31);
 #pragma unroll 1
                 for (int qb = 0; qb < NB; ++qb) {
                     // rows of the registers: (reference, delta) as the dQ kernel left them
@@ -887,14 +931,26 @@ __global__ void __launch_bounds__(64 * W) attend_dkv(AttendArgs a) {
                     }
                     auto hide = [&](int e) { s[e] = ds[e] = CAREFUL ? -INFINITY : 0.f; };
                     if (edge) {  // rows of the block that see the key
-                        const int r0 = a.causal ? key - p0 : 0, r1 = len.q - t * QT - qb * 32;
+                        const int r0 = a.causal ? key - p0 : 0, r1 = live ? len.q - t * QT - qb * 32 : 0;
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
                             if (acc_row(e, lane) < r0 || acc_row(e, lane) >= r1) hide(e);
                     }
                     if (BIAS && masks) n.mask<-1>(hide);
+                    // here: behind the products it took more registers, and the second wave
+                    if (BIAS && a.dist) dist.template add<CAREFUL>(ds, k0 - p0 - 31);
                     Tl::template add<CAREFUL>(gs, qb * 32, s, lane, dv);
                     Tl::template add<CAREFUL>(qs, qb * 32, ds, lane, dk);
+                }
+            }
+            if (BIAS && a.dist) {
+                dist.finish();
+                __syncthreads();
+                const float* sums = table + table_size(a) + W * SKEW;
+                for (int x = threadIdx.x; x < distances; x += 64 * W) {
+                    float y = sums[x];
+                    for (int w = 1; w < W; ++w) y += sums[w * distances + x];
+                    dist_out[x] = y;
                 }
             }
         }
@@ -952,10 +1008,10 @@ template <auto K> gp_status allow_lds(size_t bytes) {
     if (bytes <= 65536) return GP_OK;
     int dev = 0;
     GP_HIP(hipGetDevice(&dev));
-    const uint64_t bit = 1ull << (dev & 63);
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
     if (allowed.load(std::memory_order_relaxed) & bit) return GP_OK;
     GP_HIP(hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, 159 * 1024));
-    if (dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
+    allowed.fetch_or(bit, std::memory_order_relaxed);
     return GP_OK;
 }
 size_t table_bytes(const AttendArgs& a) { return (2 * ((size_t)a.max_distance + PAD) + 1) * 4; }
@@ -977,11 +1033,11 @@ template <typename T, int DH> gp_status forward(const AttendArgs& a, hipStream_t
     return a.bias ? launch_fwd<T, DH, KT, 4, true, false>(a, st) : launch_fwd<T, DH, KT, 4, false, false>(a, st);
 }
 
-template <typename T, int DH, int W, bool BIAS, bool EXACT>
+template <typename T, int DH, int W, bool BIAS, int DELTA>
 gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
     constexpr int KT = tile_rows(sizeof(T));
-    const size_t bytes = 2 * (BIAS ? 2 : stages(DH)) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) + W * (SKEW + 2 * a.max_distance + 1) * 4 : 0);
-    constexpr auto k = attend_dq<T, DH, KT, W, BIAS, EXACT>;
+    const size_t bytes = 2 * stages(DH) * Tile<T, DH, KT>::BYTES + (BIAS ? table_bytes(a) : 0);
+    constexpr auto k = attend_dq<T, DH, KT, W, BIAS, DELTA>;
     GP_TRY(allow_lds<k>(bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.H * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
     GP_LAUNCH_CHECK();
@@ -990,7 +1046,8 @@ gp_status launch_dq(const AttendArgs& a, hipStream_t st) {
 template <typename T, int DH, int W, bool BIAS>
 gp_status launch_dkv(const AttendArgs& a, hipStream_t st) {
     constexpr int QT = tile_rows(sizeof(T));
-    const size_t bytes = 2 * stages(DH) * Tile<T, DH, QT>::BYTES + stages(DH) * 512 + (BIAS ? table_bytes(a) : 0);
+    constexpr int ST = BIAS ? 2 : stages(DH);
+    const size_t bytes = ST * (2 * Tile<T, DH, QT>::BYTES + 512) + (BIAS ? table_bytes(a) + W * (SKEW + 2 * a.max_distance + 1) * 4 : 0);
     constexpr auto k = attend_dkv<T, DH, QT, W, BIAS>;
     GP_TRY(allow_lds<k>(bytes));
     klaunch(k, dim3((unsigned)((long)a.B * a.HK * a.blocks * a.splits)), dim3(64 * W), (uint32_t)bytes, st, a);
@@ -1002,10 +1059,12 @@ template <typename T, int DH> gp_status backward(const AttendArgs& a, bool exact
     q.blocks = dq.blocks;
     q.splits = dq.splits;
     if (q.blocks) {
-        if (a.bias)
-            GP_TRY(exact ? (launch_dq<T, DH, BW, true, true>(q, st)) : (launch_dq<T, DH, BW, true, false>(q, st)));
+        constexpr int BY_BIAS = sizeof(T) == 2 ? REFINED : FROM_OUT;
+        if (a.bias)  // a split of a row's keys has but its share of the error
+            GP_TRY(exact || (BY_BIAS == REFINED && q.splits > 1) ? (launch_dq<T, DH, BW, true, FROM_WEIGHTS>(q, st))
+                                                                : (launch_dq<T, DH, BW, true, BY_BIAS>(q, st)));
         else
-            GP_TRY(exact ? (launch_dq<T, DH, BW, false, true>(q, st)) : (launch_dq<T, DH, BW, false, false>(q, st)));
+            GP_TRY(exact ? (launch_dq<T, DH, BW, false, FROM_WEIGHTS>(q, st)) : (launch_dq<T, DH, BW, false, FROM_OUT>(q, st)));
     }
     AttendArgs k = a;
     k.blocks = dkv.blocks;

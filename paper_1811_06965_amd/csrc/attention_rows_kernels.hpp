@@ -403,8 +403,6 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
     const bool in = r < rows, live = in && i < len.q;
     const int pos = i + len.start, pos0 = row0 / a.pack + len.start;
 
-    bool masks = false;
-    if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
     typename Elt<T>::frag qf[NK];
     load_row<T>(a.q.at(wk.b, min(i, a.Sq - 1), min(h, a.H - 1)), live, a.dh, lane, qf);
 
@@ -425,6 +423,14 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
         vl(s + Tl::BYTES, vp + (long)t * KT * a.v.row, len.k - t * KT, a.v.row, a.dh, KEYS ? 0 : wave);
     };
 
+    auto first_tiles = [&] {
+#pragma unroll
+        for (int x = 0; x < ST - 1; ++x)
+            if (t0 + own + x * step < t1) stage(t0 + own + x * step, x);
+    };
+    first_tiles();  // on their way while the table is made
+    bool masks = false;
+    if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
     const float c = a.scale * LOG2E;
     float m, l;
     f32x16 o[ND];
@@ -436,9 +442,6 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
         l = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[d] = zero16();
-#pragma unroll
-        for (int x = 0; x < ST - 1; ++x)
-            if (t0 + own + x * step < t1) stage(t0 + own + x * step, x);
         for (int t = t0 + own, buf = 0; t < t1; t += step, buf = ring<ST>(buf, 1)) {
             if (ST > 2 && t + step < t1) wait_vmcnt<2 * decltype(kl)::N>(); else wait_vmcnt<0>();
             if (KEYS) lds_reads_done(); else lds_barrier();
@@ -498,7 +501,10 @@ __global__ void __launch_bounds__(64 * W) attend_fwd(AttendArgs a) {
     };
     pass(std::false_type{});
     if (a.causal || masks) {
-        if (__syncthreads_or(!all_finite(o))) pass(std::true_type{});
+        if (__syncthreads_or(!all_finite(o))) {
+            first_tiles();
+            pass(std::true_type{});
+        }
     }
     l = both_sum(l);
     if constexpr (KEYS) {
@@ -678,8 +684,6 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     const int pos = i + len.start, pos0 = row0 + len.start;
     const long stat = ((long)wk.b * a.H + wk.h) * 2 * a.stat_rows;
 
-    bool masks = false;
-    if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
 
     typename Elt<T>::frag qf[NK], gf[NK];
     const int ic = min(i, a.Sq - 1);
@@ -720,6 +724,9 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         lds_barrier();
         if (t + ST - 1 < end) stage(t + ST - 1, ring<ST>(buf, ST - 1));
     };
+    if (DELTA == FROM_WEIGHTS) first_tiles(0, tiles); else first_tiles(t0, t1);  // on their way while the table is made
+    bool masks = false;
+    if (BIAS) masks = __syncthreads_or(load_table(table, a, wk.h, threadIdx.x, 64 * W));
     const float c = a.scale * LOG2E;
     const f32x16 s0 = splat16(INIT ? -lse2 / c : 0.f);
     // the weights of one block (s) and dP from dp0 on (dp); -INFINITY marks a masked pair's weight where `mark` asks for it
@@ -753,7 +760,6 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     auto tile_edge = [&](int t) { return short_rows || t * KT + KT > len.k || (a.causal && t * KT + KT - 1 > pos0); };
     if (DELTA == FROM_WEIGHTS) {
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        first_tiles(0, tiles);
         for (int t = 0, buf = 0; t < tiles; ++t, buf = ring<ST>(buf, 1)) {
             next_tile(t, tiles, buf);
             if (t * KT >= kw) continue;
@@ -768,6 +774,7 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         }
         delta = both_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
         lds_barrier();
+        first_tiles(t0, t1);
     }
     const f32x16 dp0 = splat16(INIT ? -delta : 0.f);
     f32x16 dq[ND], r[DELTA == REFINED ? ND : 1];
@@ -777,7 +784,6 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         error = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) dq[d] = r[DELTA == REFINED ? d : 0] = zero16();
-        first_tiles(t0, t1);
         for (int t = t0, buf = 0; t < t1; ++t, buf = ring<ST>(buf, 1)) {
             next_tile(t, t1, buf);
             if (t * KT >= kw) continue;
@@ -805,7 +811,10 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     };
     pass(std::false_type{});
     if (a.causal || masks) {
-        if (__syncthreads_or(!all_finite(dq))) pass(std::true_type{});
+        if (__syncthreads_or(!all_finite(dq))) {
+            first_tiles(t0, t1);
+            pass(std::true_type{});
+        }
     }
     if constexpr (DELTA == REFINED) {
         error = both_sum(error);
@@ -884,11 +893,11 @@ __global__ void __launch_bounds__(64 * W, DH <= 64 ? 2 : 1) attend_dkv(AttendArg
                                                          4, lane * 4, 0, 0, 0);
             };
             __syncthreads();  // the last head's tiles are done with
-            if (BIAS) masks = masks | (__syncthreads_or(load_table(table, a, h, threadIdx.x, 64 * W)) != 0);
-            if (BIAS && a.dist) dist.clear();
 #pragma unroll
             for (int x = 0; x < ST - 1; ++x)
                 if (ta + x < tb) stage(ta + x, x);
+            if (BIAS) masks = masks | (__syncthreads_or(load_table(table, a, h, threadIdx.x, 64 * W)) != 0);
+            if (BIAS && a.dist) dist.clear();
             for (int t = ta, buf = 0; t < tb; ++t, buf = ring<ST>(buf, 1)) {
                 if (ST > 2 && t + 1 < tb) wait_vmcnt<2 * decltype(ql)::N + 1>(); else wait_vmcnt<0>();
                 lds_barrier();

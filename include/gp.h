@@ -699,7 +699,7 @@ typedef struct {
  * bf16 the weights p are rounded to bf16 before they meet v), the softmax in fp32.  out
  * must not overlap the inputs (tensors beside each other in every period of a stride that both have are fine).
  * GP_ERR_INVALID_ARG: NULL tensors, sizes out of range (lengths up to 2^28, 65535 heads, batch x heads x
- *   (length / 128 + 1) below 2^24), heads not a multiple of kv_heads, an output that overlaps an input, a
+ *   (length / 128 + 1) below 2^23), heads not a multiple of kv_heads, an output that overlaps an input, a
  *   misaligned address or stride, scale out of range, a bias without its buckets, a workspace that is NULL or too small.  GP_ERR_UNSUPPORTED: head_dim > 128, more buckets or a further
  *   distance than above.
  */

@@ -183,10 +183,10 @@ gp_status read_config(const gp_attention_config* c, AttendArgs& a, const char*& 
     } else if (c->bucket_of || c->buckets || c->max_distance) {
         return bad("bucket_of, buckets and max_distance belong to a bias");
     }
-    // a launch holds fewer than 2^32 threads, 256 of them take 128 rows; a head's own grid dimension 2^16
+    // a launch holds fewer than 2^32 threads, 256 of them take 128 rows and 512 a few; a head's own grid dimension 2^16
     const long groups = (long)c->batch * c->heads;
-    if (c->heads > 65535 || groups >= (1l << 24) || groups * (c->q_len / 128 + 1l) >= (1l << 24) ||
-        groups * (c->k_len / 128 + 1l) >= (1l << 24))
+    if (c->heads > 65535 || groups >= (1l << 23) || groups * (c->q_len / 128 + 1l) >= (1l << 23) ||
+        groups * (c->k_len / 128 + 1l) >= (1l << 23))
         return bad("more heads (65535) or rows than a launch holds");
     a = AttendArgs{};
     a.dtype = c->dtype;
@@ -281,8 +281,10 @@ const char* read_rows(const AttendArgs& a, const gp_head_rows* t, int len, int h
     if (!aligned(r.p, 16) || r.seq % 16 || r.row % 16 || r.head % 16) return "addresses and strides must be multiples of 16 bytes";
     if (r.row < a.dh * esz || r.row > (1l << 24)) return "rows must not overlap, and lie at most 2^24 bytes apart";
     out.inner = a.dh * esz;
-    for (const Rows::Dim& d : {Rows::Dim{r.seq, a.B}, Rows::Dim{r.row, len}, Rows::Dim{r.head, heads}})
+    for (const Rows::Dim& d : {Rows::Dim{r.seq, a.B}, Rows::Dim{r.row, len}, Rows::Dim{r.head, heads}}) {
+        if (d.stride > (1l << 47) / d.n) return "a stride is out of range";  // of any address
         if (d.n > 1) out.dim[out.dims++] = d;
+    }
     std::sort(out.dim, out.dim + out.dims, [](const Rows::Dim& x, const Rows::Dim& y) { return x.stride > y.stride; });
     return nullptr;
 }

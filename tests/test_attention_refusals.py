@@ -60,7 +60,7 @@ BIAS = dict(bias=A, bucket_of=A, buckets=32, max_distance=128)
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=2), INVALID), (dict(batch=-1), INVALID), (dict(q_len=-1), INVALID), (dict(k_len=-1), INVALID),
     (dict(k_len=(1 << 28) + 1), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=3), INVALID),
-    (dict(heads=65536, kv_heads=65536), INVALID), (dict(batch=1 << 22), INVALID), (dict(q_len=1 << 28), INVALID),
+    (dict(heads=65536, kv_heads=65536), INVALID), (dict(batch=1 << 22), INVALID), (dict(batch=1 << 21), INVALID), (dict(q_len=1 << 28), INVALID),
     (dict(head_dim=0), INVALID), (dict(head_dim=60), INVALID), (dict(head_dim=136), UNSUPPORTED), (dict(scale=0.0), INVALID),
     (dict(scale=-1.0), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID), (dict(q_lens=A + 1), INVALID),
     (dict(k_lens=A + 2), INVALID), (dict(q_starts=A + 2), INVALID), (dict(buckets=4), INVALID), (dict(max_distance=4), INVALID),
@@ -80,6 +80,11 @@ def test_tensors(gp, name, d):
     backward = name.startswith("d")
     assert call(gp, backward=backward, change={name: d}) == INVALID
     assert "attention" in gp.gp_last_error()
+
+
+def test_strides_past_any_address(gp):
+    assert call(gp, config(gp, heads=512, kv_heads=2), change={"q": dict(head=1 << 40)}) == INVALID
+    assert call(gp, config(gp, batch=1 << 20, heads=2), change={"k": dict(seq=1 << 30)}) == INVALID
 
 
 def test_other_arguments(gp):

@@ -134,6 +134,25 @@ def test_bias(ops, dtype, causal, Sq, Sk, buckets, distance, dh, K):
     compare(ops, *args, distance=distance)
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("bf16", 96), ("bf16", 32), ("f32", 40)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_bias_without_splits(ops, dtype, dh, causal):
+    """Enough rows that no workgroup's keys are split, over several tiles of them."""
+    compare(ops, *make(dtype=dtype, B=16, H=16, K=8, Sq=150, Sk=200, dh=dh, buckets=32, causal=causal, ragged=True, seed=dh), distance=60)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_few_queries_before_keys_that_are_not_finite(ops, dtype, bad):
+    q, k, v, dout, kw, _ = make(dtype=dtype, Sq=3, Sk=400, H=6, K=2, causal=True, starts=200)
+    clean = compare(ops, q, k, v, dout, kw)
+    k[0, 203:], v[0, 203:], k[1, 206:], v[1, 206:] = bad, bad, bad, bad
+    again = compare(ops, q, k, v, dout, kw)
+    for x, y in zip(clean, again):
+        for s, t in zip(x, y):
+            assert s is None or torch.equal(s, t)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("low", [-1e30, -math.inf, torch.finfo(torch.float32).min])
 def test_masking_bias(ops, dtype, low):

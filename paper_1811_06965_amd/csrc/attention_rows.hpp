@@ -39,9 +39,14 @@ struct Shape {
     int splits = 1;     // workgroups of one block
 };
 constexpr int BW = 4;  // waves of the backward's workgroups
-constexpr int head_bucket(int dh) { return (dh + 31) / 32 * 32; }           // features that a kernel is made for
-constexpr int tile_rows(int esize) { return esize == 2 ? 64 : 32; }          // rows of a tile in LDS
-constexpr int stages(int width) { return width <= 64 ? 3 : 2; }                // tiles in LDS at a time
+// Features that a kernel is made for: whole matrix blocks (4 x 2048, 16 heads, bf16 forward: 73 us at 32, 95 at 64, 130 at 96).
+constexpr int head_bucket(int dh) { return (dh + 31) / 32 * 32; }
+// Rows of a tile in LDS: 64 in bf16 (us at 32 / 64: 1000 queries to 50000 keys 455 / 432, backward of 4 x 2048 with a bias
+// 367 / 350, of 64 x 256 149 / 143), in fp32 as many bytes.
+constexpr int tile_rows(int esize) { return esize == 2 ? 64 : 32; }
+// Tiles in LDS at a time: three where two workgroups of them fit a CU (dK and dV with two: 94 us for 85).
+constexpr int stages(int width) { return width <= 64 ? 3 : 2; }
+// Waves that share few rows, each with two tiles of keys and values of 32 rows in LDS: as many as 128 KB hold.
 constexpr int key_waves(int row_bytes) { return row_bytes <= 128 ? 8 : row_bytes <= 256 ? 4 : 2; }
 
 // The kernels for one type.

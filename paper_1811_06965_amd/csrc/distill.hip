@@ -149,7 +149,9 @@ __device__ __forceinline__ void finish_row(const DistillOut& o, long row, Sum aw
 // A workgroup of NT threads per row, or `splits` of them, each over `per` chunks of it; one pass over the logits
 // with a running reference, four loads ahead of their use.  REST: the named tokens are left out of the sum, which
 // alone keeps the rest's share exact where the student gives it little (the difference of the sums would not): a byte
-// in LDS marks them in each chunk, WINDOW chunks at a time.
+// in LDS marks them in each chunk, WINDOW chunks at a time.  Bound by HBM where rows are many: 4096 of 128000 bf16 with 64 tokens
+// 183 us (5.7 TB/s), else by a row's chain of tokens, marks, loads and reductions: 93 rows of 50021 fp32 with 100 tokens 13.
+// The next loads before these sums, in more registers, made the long rows 7% slower.
 constexpr int WINDOW = 16384;
 template <typename T, bool CLIP, bool REST, int NT>
 __global__ void __launch_bounds__(NT) distill_kernel(const T* __restrict__ z, Logits a, DistillOut out, int splits, int per,
@@ -252,7 +254,8 @@ __global__ void __launch_bounds__(64) distill_join_kernel(const T* __restrict__ 
 //   dz_v = dloss scale (W p_v - q_v) for a named token,
 //   dz_v = dloss scale (W - left / R) p_v else, R = exp(rest_lse - lse): written as
 //          (W R - left) exp(s - rest_lse), neither of whose factors passes 1 by much.
-// One pass writes the second form everywhere, then the named tokens, each by the thread that holds it.
+// One pass writes the second form everywhere, then the named tokens, each by the thread that holds it.  Bound by HBM: 1024 rows of
+// 32000 bf16 28 us (131 MB, 4.6 TB/s).
 struct DistillGrad {
     const float* lse;
     const float* rest_lse;
@@ -369,8 +372,13 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const T* z, Logits a,
     }
 }
 
+// Threads of a workgroup: a wave for short rows, whose reductions wait for nobody; for few or long rows the most loads in
+// flight.  us at 64 / 256 / 1024 threads, bf16 with 32 tokens unless noted: 4096 x 1000 with 8 8.8 / 11.9 / 34.6; 3000 x 4111 14.3 /
+// 17.2 / 42.9; 1024 x 8000 12.0 / 10.1 / 15.3; 512 x 9000 fp32 with 20 12.7 / 8.4 / 8.5; 256 x 14000 13.5 / 8.6 / 8.0; 512 x
+// 27000 21.9 / 12.3 / 11.6; 93 x 50021 fp32 with 100 44.3 / 17.7 / 13.2; 1024 x 32000 26.1 / 19.1 / 23.3.  Rows are split as for log
+// probabilities, whole / split: 1 x 131072 14.6 / 10.7, 32 15.3 / 12.0, 96 15.6 / 14.8, but 64 x 65536 fp32 11.4 / 12.3.
 int distill_threads(long rows, int chunks, int splits) {
-    if (chunks <= 256 || (chunks <= 1024 && rows >= 1024)) return 64;
+    if (chunks <= 256 || (chunks <= 700 && rows >= 1024)) return 64;
     if (splits > 1 || chunks <= (rows <= 256 ? 2048 : 3200)) return 256;
     return rows < 768 || chunks > 8192 ? 1024 : 256;
 }

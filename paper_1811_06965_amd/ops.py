@@ -36,7 +36,7 @@ class TokenLogprobs(NamedTuple):
 def _on(device, call):
     """call(stream) with the device current and its current stream's handle."""
     i = device.index
-    if i == torch.cuda.current_device():
+    if i == torch._C._cuda_getDevice():
         call(torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(i):
@@ -437,14 +437,14 @@ class AttentionGrads(NamedTuple):
     dbias: Optional[torch.Tensor]  # fp32 [heads, buckets]; None without a bias
 
 
-def _head_rows(name, t, like, shape):
-    """gp_head_rows of a tensor [batch, len, heads, head_dim] of the type and device of `like`."""
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name} must be {list(shape)} in {like.dtype} on {like.device}")
-    s = t.stride()
-    if s[3] != 1 and shape[3] > 1:
+def _head_rows(name, t, kind, device, shape):
+    """gp_head_rows of a tensor [batch, len, heads, head_dim] of this type, on the device of this index."""
+    if t.shape != shape or t.dtype != kind or t.get_device() != device:
+        raise ValueError(f"{name} must be {list(shape)} in {kind} on GPU {device}")
+    a, b, c, d = t.stride()
+    if d != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the features of a head must be adjacent")
-    return gp.gp_head_rows(t.data_ptr(), s[0], s[1], s[2])
+    return gp.gp_head_rows(t.data_ptr(), a, b, c)
 
 
 @functools.lru_cache(maxsize=256)
@@ -459,32 +459,36 @@ def _attention_bytes(backward, *sizes):
 
 def _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, backward):
     """(config, gp_head_rows of q, k and v, bytes of scratch)."""
-    if q.dim() != 4 or k.dim() != 4 or q.dtype not in DTYPE:
+    kind = q.dtype
+    if q.dim() != 4 or k.dim() != 4 or kind not in DTYPE:
         raise ValueError("q, k and v must be [batch, len, heads, head_dim] in float32 or bfloat16")
-    B, Sq, H, dh = q.shape
-    Sk, K = k.shape[1], k.shape[2]
+    shape, like = q.shape, k.shape
+    B, Sq, H, dh = shape
+    _, Sk, K, _ = like
+    if like[0] != B or like[3] != dh:
+        raise ValueError("q, k and v must have the same batch and head_dim")
     dev = _gpu(q)
+    at = dev.index
+    rows = (_head_rows("q", q, kind, at, shape), _head_rows("k", k, kind, at, like), _head_rows("v", v, kind, at, like))
     if q_lens is not None:
         _vector("q_lens", q_lens, B, torch.int32, dev)
     if k_lens is not None:
         _vector("k_lens", k_lens, B, torch.int32, dev)
     if q_starts is not None:
         _vector("q_starts", q_starts, B, torch.int32, dev)
-    cfg = gp.gp_attention_config(DTYPE[q.dtype], B, H, K, Sq, Sk, dh, causal, dh ** -0.5 if scale is None else scale,
-                                 _ptr(q_lens), _ptr(k_lens), _ptr(q_starts))
+    dt = DTYPE[kind]
+    cfg = gp.gp_attention_config(dt, B, H, K, Sq, Sk, dh, causal, dh ** -0.5 if scale is None else scale, _ptr(q_lens),
+                                 _ptr(k_lens), _ptr(q_starts))
     buckets = distance = 0
     if bias is not None:
         table = bias.table
-        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[0] != H or table.device != dev or not table.is_contiguous():
+        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[0] != H or table.get_device() != at or not table.is_contiguous():
             raise ValueError(f"the bias must have a contiguous float32 table of {H} heads on {dev}")
-        if bias.bucket_of.device != dev:
+        if bias.bucket_of.get_device() != at:
             raise ValueError(f"the bias was made on {bias.bucket_of.device}")
         buckets, distance = table.shape[1], bias.max_distance
         cfg.bias, cfg.bucket_of, cfg.buckets, cfg.max_distance = table.data_ptr(), bias.bucket_of.data_ptr(), buckets, distance
-    like = (B, Sk, K, dh)
-    rows = (_head_rows("q", q, q, q.shape), _head_rows("k", k, q, like), _head_rows("v", v, q, like))
-    need = _attention_bytes(backward, cfg.dtype, B, H, K, Sq, Sk, dh, buckets, distance)
-    return cfg, rows, need
+    return cfg, rows, _attention_bytes(backward, dt, B, H, K, Sq, Sk, dh, buckets, distance)
 
 
 def attention(q, k, v, q_lens=None, k_lens=None, q_starts=None, causal=False, scale=None,
@@ -499,7 +503,7 @@ def attention(q, k, v, q_lens=None, k_lens=None, q_starts=None, causal=False, sc
     cfg, rows, need = _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, 0)
     dev, (B, Sq, H, dh) = q.device, q.shape
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    lse = torch.empty((B, H, Sq), dtype=torch.float32, device=dev)
+    lse = torch.empty_strided((B, H, Sq), (H * Sq, Sq, 1), dtype=torch.float32, device=dev)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     o = gp.gp_head_rows(out.data_ptr(), Sq * H * dh, H * dh, dh)
     _on(dev, lambda stream: gp.gp_attention(cfg, *rows, o, lse.data_ptr(), _ptr(ws), need, stream))
@@ -514,15 +518,16 @@ def attention_backward(q, k, v, out, lse, dout, q_lens=None, k_lens=None, q_star
     the shapes of q, k and v that receive them; allocated otherwise."""
     _no_graph(q, k, v, out, lse, dout, None if bias is None else bias.table, *(grads or ()), gradient="this call's results")
     cfg, rows, need = _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, 1)
-    dev = q.device
-    if lse.shape != (cfg.batch, cfg.heads, cfg.q_len) or lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous():
+    dev, kind, shape, like = q.device, q.dtype, q.shape, k.shape
+    at = dev.index
+    if lse.shape != (shape[0], shape[2], shape[1]) or lse.dtype != torch.float32 or lse.get_device() != at or not lse.is_contiguous():
         raise ValueError("lse must be contiguous float32 [batch, heads, q_len], as attention gives it")
-    o = None if out is None else _head_rows("out", out, q, q.shape)
-    g = _head_rows("dout", dout, q, q.shape)
+    o = None if out is None else _head_rows("out", out, kind, at, shape)
+    g = _head_rows("dout", dout, kind, at, shape)
     if grads is None:
-        grads = [torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v)]
+        grads = [torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v)]
     dq, dk, dv = grads
-    to = (_head_rows("dq", dq, q, q.shape), _head_rows("dk", dk, q, k.shape), _head_rows("dv", dv, q, k.shape))
+    to = (_head_rows("dq", dq, kind, at, shape), _head_rows("dk", dk, kind, at, like), _head_rows("dv", dv, kind, at, like))
     dbias = None if bias is None else torch.empty_like(bias.table)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _on(dev, lambda stream: gp.gp_attention_backward(cfg, *rows, o, lse.data_ptr(), g, *to, _ptr(dbias), _ptr(ws), need,

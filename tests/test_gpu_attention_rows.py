@@ -109,6 +109,19 @@ def test_layouts(ops, dtype, layout_q, layout_kv):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_broadcast_inputs(ops, dtype):
+    """One sequence's keys for all of a batch, one head's for all heads, one query row's gradient for all rows: strides of 0."""
+    q, k, v, dout, kw, _ = make(dtype=dtype, B=3, Sq=40, Sk=100, H=4, K=4)
+    k, v = k[:1].expand(3, -1, -1, -1), v[:, :, :1].expand(-1, -1, 4, -1)
+    one = dout[:, :, :1].expand(-1, -1, 4, -1)
+    compare(ops, q, k, v, one, kw)
+    r = ops.attention(q, k, v)
+    for a, b in zip(ops.attention_backward(q, k, v, r.out, r.lse, one),
+                    ops.attention_backward(q, k.contiguous(), v.contiguous(), r.out, r.lse, one.contiguous())):
+        assert a is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("starts", [-40, 0, 25, 400, 2 ** 30, -2 ** 31 + 1])
 def test_starts(ops, dtype, starts):
     """A chunk of queries at a later position; before all keys (empty rows) and far behind them."""

@@ -64,6 +64,7 @@ __device__ __forceinline__ int acc_row(int r, int lane) { return (r >> 2) * 8 + 
 __device__ __forceinline__ int swizzle(int r) { return (((r >> 1) & 1) << 2) | ((r >> 2) & 3); }
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 template <typename T, int DH, int R> struct Tile {
     typedef Elt<T> X;
@@ -171,10 +172,15 @@ template <typename T, int DH, int R> struct Tile {
         else
             add_elements<CAREFUL>(s, row0, w, lane, acc);
     }
-    // Two sums from one reading of the rows.
+    // Two sums from one reading of the rows.  total += the sum of this lane's w as they are rounded.
     template <bool CAREFUL, int ND>
     static __device__ __forceinline__ void add(const char* s, int row0, const f32x16& w, const f32x16& w2, int lane, f32x16 (&acc)[ND],
-                                               f32x16 (&acc2)[ND]) {
+                                               f32x16 (&acc2)[ND], float& total) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const auto rounded = [&](int i) { return (bf16)(CAREFUL && w[i] == -INFINITY ? 0.f : w[i]); };
+            total = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{rounded(e), rounded(e + 1)}, bf16x2{(bf16)1.f, (bf16)1.f}, total, false);
+        }
         static_assert(sizeof(T) == 2, "fp32 reads its elements one by one");
         if constexpr (CAREFUL) {
             add<CAREFUL>(s, row0, w, lane, acc);
@@ -799,10 +805,10 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     }
     const f32x16 dp0 = splat16(INIT ? -delta : 0.f);
     f32x16 dq[ND], r[DELTA == REFINED ? ND : 1];
-    float error = 0.f;
+    float error = 0.f, rounded = 0.f;  // sums of dS, and of dS as it is multiplied
     auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
-        error = 0.f;
+        error = rounded = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d) dq[d] = r[DELTA == REFINED ? d : 0] = zero16();
         for (int t = t0, buf = 0; t < t1; ++t, buf = ring<ST>(buf, 1)) {
@@ -824,7 +830,7 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
                 }
                 error += sum[0] + sum[1];
                 if constexpr (DELTA == REFINED)
-                    Tl::template add<CAREFUL>(ks, kb * 32, ds, s, lane, dq, r);
+                    Tl::template add<CAREFUL>(ks, kb * 32, ds, s, lane, dq, r, rounded);
                 else
                     Tl::template add<CAREFUL>(ks, kb * 32, ds, lane, dq);
             }
@@ -838,12 +844,12 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
         }
     }
     if constexpr (DELTA == REFINED) {
-        error = both_sum(error);
-        delta += error;
+        delta += both_sum(error);
+        rounded = both_sum(rounded);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) dq[d][e] = __builtin_fmaf(-error, r[d][e], dq[d][e]);
+            for (int e = 0; e < 16; ++e) dq[d][e] = __builtin_fmaf(-rounded, r[d][e], dq[d][e]);
     }
     if (in && a.splits > 1)
         store_row<float, ND>(reinterpret_cast<char*>(a.part + ((((long)wk.split * a.B + wk.b) * a.H + wk.h) * a.Sq + i) * DH), dq, live ? 1.f : 0.f, DH, lane);

@@ -414,15 +414,23 @@ class RelativeBias:
     added to the scores of head h.  table: contiguous fp32 [heads, buckets], read at every
     call (an optimiser updates it in place).  The buckets are gp_relative_buckets': half of
     one side's hold one distance each, the others grow with the logarithm up to max_distance,
-    beyond which all share the last; bidirectional: one half for keys behind the query."""
+    beyond which all share the last; bidirectional: one half for keys behind the query.  The map of
+    distances is made here, once: another number of buckets or distance takes another
+    RelativeBias (table may be replaced by one of the same shape)."""
 
     def __init__(self, table: torch.Tensor, max_distance=128, bidirectional=True):
         if table.dim() != 2 or table.dtype != torch.float32:
             raise ValueError("table must be float32 [heads, buckets]")
         dev = _gpu(table)
-        self.table, self.max_distance, self.bidirectional = table, max_distance, bidirectional
+        self.table = table
+        self._buckets, self._max_distance, self._bidirectional = table.shape[1], max_distance, bidirectional
         of = gp.gp_relative_buckets(table.shape[1], max_distance, bidirectional)
-        self.bucket_of = torch.tensor(of, dtype=torch.int32).to(dev)
+        self._bucket_of = torch.tensor(of, dtype=torch.int32).to(dev)
+
+    # the kernels read 2 max_distance + 1 places of bucket_of
+    max_distance = property(lambda self: self._max_distance)
+    bidirectional = property(lambda self: self._bidirectional)
+    bucket_of = property(lambda self: self._bucket_of)
 
 
 class Attention(NamedTuple):
@@ -481,13 +489,14 @@ def _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, backward)
                                  _ptr(k_lens), _ptr(q_starts))
     buckets = distance = 0
     if bias is not None:
-        table = bias.table
-        if table.dtype != torch.float32 or table.dim() != 2 or table.shape[0] != H or table.get_device() != at or not table.is_contiguous():
-            raise ValueError(f"the bias must have a contiguous float32 table of {H} heads on {dev}")
-        if bias.bucket_of.get_device() != at:
-            raise ValueError(f"the bias was made on {bias.bucket_of.device}")
-        buckets, distance = table.shape[1], bias.max_distance
-        cfg.bias, cfg.bucket_of, cfg.buckets, cfg.max_distance = table.data_ptr(), bias.bucket_of.data_ptr(), buckets, distance
+        table, of, buckets, distance = bias.table, bias._bucket_of, bias._buckets, bias._max_distance
+        if table.dtype != torch.float32 or table.shape != (H, buckets) or table.get_device() != at or not table.is_contiguous():
+            raise ValueError(f"the bias must have a contiguous float32 table of {H} heads and {buckets} buckets on {dev}")
+        if of.get_device() != at:
+            raise ValueError(f"the bias was made on {of.device}")
+        if of.numel() != 2 * distance + 1 or not of.is_contiguous():
+            raise ValueError("bucket_of has been changed in length")
+        cfg.bias, cfg.bucket_of, cfg.buckets, cfg.max_distance = table.data_ptr(), of.data_ptr(), buckets, distance
     return cfg, rows, _attention_bytes(backward, dt, B, H, K, Sq, Sk, dh, buckets, distance)
 
 

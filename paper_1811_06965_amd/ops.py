@@ -18,6 +18,7 @@ from typing import NamedTuple, Optional, Sequence, Union
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.graph import increment_version
 
 from . import gp
@@ -67,7 +68,11 @@ def _rows(name, t):
 
 
 def _no_graph(*tensors, gradient="token_logprobs_backward"):
-    """The operators build no autograd graph: an input whose gradient would be lost is refused."""
+    """The operators build no autograd graph: an input whose gradient, or whose tangent in forward mode, would be lost is refused."""
+    if forward_ad._current_level >= 0:  # within a dual_level
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("forward-mode differentiation is not supported here: an input has a tangent")
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:

@@ -651,6 +651,7 @@ struct Distances {
     }
     // lo: distance of the block's first key from its last query.  MARKED: a pair of -INFINITY is a masked one
     template <bool MARKED> __device__ __forceinline__ void add(const f32x16& ds, int lo) {
+#pragma clang fp contract(off)
         const auto value = [](float x) { return MARKED && x == -INFINITY ? 0.f : x; };
         if (lo >= D || lo + 62 <= -D) {
             float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -826,6 +827,9 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
                 float sum[2] = {0.f, 0.f};
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
+                    // Sums of dS are of its rounded products in every pass, not fused with them in those that mark nothing: else what a masked
+                    // pair holds, by which the careful pass is taken, would change their last bits.
+#pragma clang fp contract(off)
                     ds[e] = s[e] * (INIT ? dp[e] : dp[e] - delta);
                     if (CAREFUL) ds[e] = s[e] == -INFINITY ? s[e] : ds[e] == -INFINITY ? NAN : ds[e];
                     if (DELTA == REFINED) sum[e & 1] += CAREFUL && s[e] == -INFINITY ? 0.f : ds[e];

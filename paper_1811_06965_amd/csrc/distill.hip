@@ -375,18 +375,31 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const T* z, Logits a,
 // Threads of a workgroup: a wave for short rows, whose reductions wait for nobody; for few or long rows the most loads in
 // flight.  us at 64 / 256 / 1024 threads, bf16 with 32 tokens unless noted: 4096 x 1000 with 8 8.8 / 11.9 / 34.6; 3000 x 4111 14.3 /
 // 17.2 / 42.9; 1024 x 8000 12.0 / 10.1 / 15.3; 512 x 9000 fp32 with 20 12.7 / 8.4 / 8.5; 256 x 14000 13.5 / 8.6 / 8.0; 512 x
-// 27000 21.9 / 12.3 / 11.6; 93 x 50021 fp32 with 100 44.3 / 17.7 / 13.2; 1024 x 32000 26.1 / 19.1 / 23.3.  Rows are split as for log
-// probabilities, whole / split: 1 x 131072 14.6 / 10.7, 32 15.3 / 12.0, 96 15.6 / 14.8, but 64 x 65536 fp32 11.4 / 12.3.
+// 27000 21.9 / 12.3 / 11.6; 93 x 50021 fp32 with 100 44.3 / 17.7 / 13.2; 1024 x 32000 26.1 / 19.1 / 23.3.
 int distill_threads(long rows, int chunks, int splits) {
     if (chunks <= 256 || (chunks <= 700 && rows >= 1024)) return 64;
     if (splits > 1 || chunks <= (rows <= 256 ? 2048 : 3200)) return 256;
     return rows < 768 || chunks > 8192 ? 1024 : 256;
 }
 
+// Rows are split, of those that row_splits would, where that saves more than it costs.  A chunk takes a whole row's workgroup 0.52 ns
+// (bf16) or 0.30 (fp32), a split one's less by 0.002 ns for each row that shares the bandwidth; the join takes 2 us and 7 ns for
+// each token, 40 with a rest and 0.18 for each pair of tokens, whose first places it finds again; and each workgroup reads the tokens
+// anew, 0.2 ns for each of them and row.  us, whole / split, with 32 and 128 tokens and a rest, with 32 and 256 without:
+//   bf16  1 x 131072 14.1 / 10.3, 18.1 / 19.7, 11.6 / 6.7, 12.9 / 9.5;  96 15.0 / 14.2, 18.8 / 25.2, 12.1 / 10.7, 13.5 / 17.8
+//   96 x 262144 25.3 / 19.4, 29.2 / 29.6, 21.7 / 15.8, 23.4 / 22.1;  with 256 and a rest 1 x 262144 32.2 / 39.0, 1 x 524288 49.5 / 40.3
+//   fp32  1 x 65536 10.5 / 10.2, 14.0 / 19.3, 7.9 / 6.5, 9.3 / 9.1;  64 11.0 / 11.8, 14.7 / 21.8, 8.5 / 8.2, 9.8 / 13.3
+//   96 x 131072 18.4 / 18.1, 21.8 / 27.9, 14.6 / 14.2, 16.1 / 20.6;  96 x 262144 30.1 / 25.4, 33.3 / 34.7, 23.9 / 21.8
+int distill_splits(int dtype, long rows, int vocab, int top, bool rest) {
+    const int splits = row_splits(dtype, rows, vocab);
+    const long saved = chunk_count(dtype, vocab) * ((dtype == GP_BF16 ? 520 : 300) - 2 * rows);  // ps
+    return saved > 2000000 + ((rest ? 40000 + 180 * top : 7000) + 200 * rows) * top ? splits : 1;
+}
+
 template <typename T, bool CLIP, bool REST>
 gp_status launch_rows(const T* z, long rows, const Logits& a, const DistillOut& out, void* ws, size_t ws_bytes, hipStream_t st) {
     const int dtype = sizeof(T) == 2 ? GP_BF16 : GP_F32;
-    int splits = row_splits(dtype, rows, a.V);
+    int splits = distill_splits(dtype, rows, a.V, a.top, REST);
     if (splits > 1) {
         const size_t fit = ws ? ws_bytes / (rows * sizeof(Sum)) : 0;
         splits = (int)std::min<size_t>(splits, std::max<size_t>(fit, 1));

@@ -36,3 +36,19 @@ def test_any_scratch(dtype, rest, rows, vocab, top):
         assert written <= (size or 0)
         used[size] = written > 0
     assert used[need] and used[2 * 8 * rows] and not (used[2 * 8 * rows - 1] or used[8 * rows] or used[0] or used[None])
+
+
+@pytest.mark.parametrize("dtype,rows,vocab,top,rest,split", [
+    ("bf16", 1, 131072, 32, True, True), ("bf16", 96, 131072, 32, True, True), ("bf16", 1, 131072, 128, True, False),
+    ("f32", 32, 80000, 32, True, True), ("f32", 64, 65536, 32, True, False), ("f32", 64, 65536, 32, False, True),
+    ("f32", 96, 65536, 32, False, False), ("f32", 1, 262144, 128, True, True), ("f32", 1, 65536, 128, True, False)])
+def test_split_where_that_is_faster(dtype, rows, vocab, top, rest, split):
+    """Rows are split where their chunks cost more than what joining them does: its figures stand beside the rule."""
+    _, z, ids, t = make(rows, vocab, top, dtype, ragged=False)
+    kind = gp.GP_BF16 if dtype == "bf16" else gp.GP_F32
+    need = gp.gp_distill_workspace(kind, rows, vocab)
+    ws = torch.full((need,), 0xa5, dtype=torch.uint8, device="cuda")
+    out = torch.empty(3, rows, device="cuda")
+    gp.gp_distill(kind, z.data_ptr(), rows, vocab, vocab, ids.data_ptr(), t.data_ptr(), top, 1.0, 0.0, rest, out[0].data_ptr(),
+                  out[1].data_ptr(), out[2].data_ptr(), ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+    assert need > 0 and bool((ws != 0xa5).any()) == split

@@ -715,9 +715,8 @@ gp_status gp_attention_workspace(const gp_attention_config* cfg, int backward, s
  *   dbias[h, b] = sum of ds over the pairs of bucket b
  * dk and dv summed over the heads that share them; zero for keys from k_lens[b] on and for queries that see no
  * key or lie at q_lens[b] or beyond.
- *   out    : NULL: delta is formed as sum_j p_ij (dout_i . v_j), without the rounding of out
- *            (slower by two products).  A bf16 call with a bias corrects that rounding in any case, since it is
- *            common to all pairs of a row and adds up in dbias.
+ *   out    : NULL: delta is formed as sum_j p_ij (dout_i . v_j), slower by two products.  From a bf16 out the
+ *            rounding, which is common to all pairs of a row, is corrected by the sum of the row's ds.
  *   dbias  : device fp32 [heads, buckets], overwritten; may be NULL.
  *   ws     : gp_attention_workspace(cfg, 1, &bytes).
  * No atomics: the same call gives the same bits.  The gradients must not overlap each other or any input.

@@ -102,12 +102,13 @@ size_t distance_floats(const AttendArgs& a) {
     const size_t rows = (size_t)distance_rows_of(a);
     return a.bias ? a.H * (rows + (rows + STEP - 1) / STEP) * (2 * (size_t)a.max_distance + 1) : 0;
 }
-// The splits' sums of dQ, dK and dV.
+// The splits' sums of dQ, dK and dV, and in bf16 those that refine dQ and delta.
 size_t part_floats(const AttendArgs& a) {
     const Shape q = dq_shape(a), k = dkv_shape(a);
     const size_t nq = q.splits > 1 ? (size_t)q.splits * a.B * a.H * a.Sq : 0;
     const size_t nk = k.splits > 1 ? (size_t)k.splits * a.B * a.HK * a.Sk * 2 : 0;
-    return (nq + nk) * head_bucket(a.dh);
+    const size_t dh = head_bucket(a.dh);
+    return (a.dtype == GP_BF16 ? refined_floats(nq, dh) : nq * dh) + nk * dh;
 }
 
 } // namespace

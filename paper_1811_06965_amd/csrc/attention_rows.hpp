@@ -38,6 +38,10 @@ struct Shape {
     int blocks = 1;     // of rows
     int splits = 1;     // workgroups of one block
 };
+// The backward's dQ pass corrects delta for the rounding of out (attend_dq).
+template <typename T> constexpr bool refines() { return sizeof(T) == 2; }
+// Floats of the sums that n rows of splits of such a pass leave: dQ', R, two of each row; a multiple of 16 bytes.
+constexpr size_t refined_floats(size_t n, size_t width) { return 2 * n * width + (2 * n + 3) / 4 * 4; }
 constexpr int BW = 4;  // waves of the backward's workgroups
 // Features that a kernel is made for: whole matrix blocks (4 x 2048, 16 heads, bf16 forward: 73 us at 32, 95 at 64, 130 at 96).
 constexpr int head_bucket(int dh) { return (dh + 31) / 32 * 32; }

@@ -688,22 +688,27 @@ struct Distances {
 
 // dQ: a wave owns 32 queries and goes through the keys as the forward does:
 //   P = 2^(S - lse), dP^T = V dO^T, dS = P (dP - delta), dQ^T += K^T dS^T.
-// delta_i = sum_j P_ij dP_ij = dO_i . O_i.  O in bf16 is off by up to 2^-8 of itself, and so would each row's sum of dS be,
-// which all the row's pairs share and the bias's gradient adds up.  So delta is made
-//   FROM_OUT: by the second form (fp32, and calls without a bias);
-//   FROM_WEIGHTS: by the first, in a pass of its own over the keys;
-//   REFINED: by the second, d, and with the sums of dS' = P (dP - d), which are the error e = delta - d (the weights add
+// delta_i = sum_j P_ij dP_ij = dO_i . O_i.  O in bf16 is off by up to 2^-8 of itself, and so would be each row's sum of dS, which all
+// the row's pairs share, dQ multiplies by the row's mean key and the bias's gradient adds up.  So delta is made
+//   FROM_OUT: by the second form (fp32);
+//   FROM_WEIGHTS: by the first, in a pass of its own over the keys (calls without O);
+//   REFINED (bf16): by the second, d, and with the sums of dS' = P (dP - d), which are the error e = delta - d (the weights add
 //   up to 1), and dQ'^T = K^T dS'^T, R^T = K^T P^T, dQ = dQ' - e R: one product for the three, and the
-//   exponential, of a pass of its own.  4 x 2048 queries, 16 heads of 64: 280 us by a pass, 150 refined.  The sum taken
-//   off dQ is that of dS' as it was rounded: the exact dS of a row add up to 0, so what the rounding has in common with the row's
-//   mean key R goes too (dQ's error against 64 bits 0.0023 for 0.0025).
+//   exponential, of a pass of its own.  The sum taken off dQ is that of dS' as it was rounded: the exact dS of a row add up to 0, so what
+//   the rounding has in common with the row's mean key R goes too.  Errors against 64 bits, by O / by the weights / refined, of random
+//   inputs: dQ 0.0028 / 0.0025 / 0.0023, with 7 keys 0.0038 / 0.0025 / 0.0023; where keys and values have means of 3 and 6 times
+//   their spread dQ 0.28 / 0.0056 / 0.0023, dK 0.011 / 0.0023 / 0.0023.  us of a backward, 4 x 2048 queries, 16 heads, by O / by the
+//   weights / refined: 192 / 243 / 208 at width 32, 275 / 340 / 301 at 64, 382 / 470 / 418 at 96, 548 / 664 / 681 at 128; with a bias by the
+//   weights / refined 298 / 260, 392 / 348, 655 / 592, 768 / 800; 64 x 256 queries to 320 keys 152 / 157 / 157 at 64, 352 / 372 / 404 at
+//   128, whose registers leave one wave a SIMD.  Splits of a row's keys leave their sums to attend_refine.
 // Writes (lse, delta) of each row for dK and dV.
 enum Delta { FROM_OUT, FROM_WEIGHTS, REFINED };
 template <typename T, int DH, int KT, int W, bool BIAS, int DELTA>
 __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     typedef Tile<T, DH, KT> Tl;
     constexpr int NK = DH / Elt<T>::E / 2, ND = DH / 32, NB = KT / 32, ST = stages(DH), TB = 2 * Tl::BYTES;
-    constexpr bool INIT = starts_sums<T>() && BIAS;  // without a bias its registers cost the third wave: 63 us for 57
+    // beyond 64 its registers cost the second wave (592 us for 684 at 96 with a bias)
+    constexpr bool INIT = starts_sums<T>() && (BIAS || DELTA == REFINED) && DH <= 64;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     float* const table = reinterpret_cast<float*>(lds + ST * TB);
     const int lane = threadIdx.x & 63, wave = uniform_wave_id(threadIdx.x);
@@ -713,7 +718,6 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
     const bool in = i < a.Sq, live = i < len.q;
     const int pos = i + len.start, pos0 = row0 + len.start;
     const long stat = ((long)wk.b * a.H + wk.h) * 2 * a.stat_rows;
-
 
     typename Elt<T>::frag qf[NK], gf[NK];
     const int ic = min(i, a.Sq - 1);
@@ -849,22 +853,63 @@ __global__ void __launch_bounds__(64 * W) attend_dq(AttendArgs a) {
             pass(std::true_type{});
         }
     }
+    const long n = (long)a.B * a.H * a.Sq, row = ((long)wk.b * a.H + wk.h) * a.Sq + i;  // of the splits' sums
     if constexpr (DELTA == REFINED) {
-        delta += both_sum(error);
+        error = both_sum(error);
         rounded = both_sum(rounded);
+        if (a.splits > 1) {  // attend_refine does the rest
+            if (in) {
+                store_row<float, ND>(reinterpret_cast<char*>(a.part + ((a.splits + wk.split) * n + row) * DH), r, live ? 1.f : 0.f, DH, lane);
+                if (lane < 32) reinterpret_cast<f32x2*>(a.part + 2 * a.splits * n * DH)[wk.split * n + row] = f32x2{live ? error : 0.f, live ? rounded : 0.f};
+            }
+        } else {
+            delta += error;
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) dq[d][e] = __builtin_fmaf(-rounded, r[d][e], dq[d][e]);
+                for (int e = 0; e < 16; ++e) dq[d][e] = __builtin_fmaf(-rounded, r[d][e], dq[d][e]);
+        }
     }
     if (in && a.splits > 1)
-        store_row<float, ND>(reinterpret_cast<char*>(a.part + ((((long)wk.split * a.B + wk.b) * a.H + wk.h) * a.Sq + i) * DH), dq, live ? 1.f : 0.f, DH, lane);
+        store_row<float, ND>(reinterpret_cast<char*>(a.part + (wk.split * n + row) * DH), dq, live ? 1.f : 0.f, DH, lane);
     else if (in)
         store_row<T, ND>(a.dq.at(wk.b, i, wk.h), dq, live ? a.scale : 0.f, a.dh, lane);
     if (wk.split == 0 && lane < 32 && i < a.stat_rows) {
         a.stats[stat + i] = starts_sums<T>() ? -lse2 / c : lse2;
         a.stats[stat + a.stat_rows + i] = starts_sums<T>() ? -delta : delta;
     }
+}
+
+// The rows of dQ, and their deltas, from the splits' sums of a refined pass: dQ', R = sum P k, and (the error of delta, the sum of the
+// rounded dS').  Four features a thread.
+template <typename T, int DH> __global__ void __launch_bounds__(256) attend_refine(AttendArgs a) {
+    const long n = (long)a.B * a.H * a.Sq, x = (long)blockIdx.x * 256 + threadIdx.x, row = x / (DH / 4);
+    const int d = (int)(x % (DH / 4)) * 4;
+    if (row >= n || d >= a.dh) return;
+    const f32x2* sums = reinterpret_cast<const f32x2*>(a.part + 2 * a.splits * n * DH);
+    f32x4 dq = {0.f, 0.f, 0.f, 0.f}, r = {0.f, 0.f, 0.f, 0.f};
+    float error = 0.f, rounded = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < a.splits; ++i) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + (i * n + row) * DH + d);
+        const f32x4 w = *reinterpret_cast<const f32x4*>(a.part + ((a.splits + i) * n + row) * DH + d);
+        const f32x2 y = sums[i * n + row];
+        error += y[0];
+        rounded += y[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            dq[e] += v[e];
+            r[e] += w[e];
+        }
+    }
+    typedef T vec __attribute__((ext_vector_type(4)));
+    vec t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = to_elt<T>(__builtin_fmaf(-rounded, r[e], dq[e]) * a.scale);
+    const long group = row / a.Sq;
+    const int i = (int)(row - group * a.Sq);
+    *reinterpret_cast<vec*>(a.dq.at((int)(group / a.H), i, (int)(group % a.H)) + d * (int)sizeof(T)) = t;
+    if (d == 0) a.stats[group * 2 * a.stat_rows + a.stat_rows + i] -= error;  // -delta
 }
 
 // dK and dV: a wave owns 32 keys and goes through the queries of all the heads that share them, in tiles of QT:
@@ -1101,29 +1146,34 @@ template <typename T, int DH> gp_status backward(const AttendArgs& a, bool exact
     AttendArgs q = a;
     q.blocks = dq.blocks;
     q.splits = dq.splits;
+    constexpr int BY_OUT = refines<T>() ? REFINED : FROM_OUT;
+    const bool refined = refines<T>() && !exact;
     if (q.blocks) {
-        constexpr int BY_BIAS = sizeof(T) == 2 ? REFINED : FROM_OUT;
-        if (a.bias)  // a split of a row's keys has but its share of the error
-            GP_TRY(exact || (BY_BIAS == REFINED && q.splits > 1) ? (launch_dq<T, DH, BW, true, FROM_WEIGHTS>(q, st))
-                                                                : (launch_dq<T, DH, BW, true, BY_BIAS>(q, st)));
+        if (a.bias)
+            GP_TRY(exact ? (launch_dq<T, DH, BW, true, FROM_WEIGHTS>(q, st)) : (launch_dq<T, DH, BW, true, BY_OUT>(q, st)));
         else
-            GP_TRY(exact ? (launch_dq<T, DH, BW, false, FROM_WEIGHTS>(q, st)) : (launch_dq<T, DH, BW, false, FROM_OUT>(q, st)));
+            GP_TRY(exact ? (launch_dq<T, DH, BW, false, FROM_WEIGHTS>(q, st)) : (launch_dq<T, DH, BW, false, BY_OUT>(q, st)));
+        if constexpr (refines<T>())
+            if (refined && q.splits > 1) {
+                klaunch(attend_refine<T, DH>, dim3((unsigned)(((long)a.B * a.H * a.Sq * (DH / 4) + 255) / 256)), dim3(256), 0, st, q);
+                GP_LAUNCH_CHECK();
+            }
     }
     AttendArgs k = a;
     k.blocks = dkv.blocks;
     k.splits = dkv.splits;
     const size_t nq = (size_t)a.B * a.H * a.Sq * DH, nk = (size_t)a.B * a.HK * a.Sk * DH;
-    if (q.splits > 1) k.part += q.splits * nq;
+    if (q.splits > 1) k.part += refined ? refined_floats(nq / DH * q.splits, DH) : q.splits * nq;
     if (k.blocks) GP_TRY(a.bias ? (launch_dkv<T, DH, BW, true>(k, st)) : (launch_dkv<T, DH, BW, false>(k, st)));
     Sums sums;
     int n = 0;
-    if (q.blocks && q.splits > 1) sums.of[n++] = {q.part, a.dq, a.H, a.Sq, q.splits, a.scale};
+    if (q.blocks && q.splits > 1 && !refined) sums.of[n++] = {q.part, a.dq, a.H, a.Sq, q.splits, a.scale};
     if (k.blocks && k.splits > 1) {
         sums.of[n++] = {k.part, a.dk, a.HK, a.Sk, k.splits, a.scale};
         sums.of[n++] = {k.part + k.splits * nk, a.dv, a.HK, a.Sk, k.splits, 1.f};
     }
     if (n) {
-        const size_t most = std::max(q.splits > 1 ? nq : 0, k.splits > 1 ? nk : 0) / 4;
+        const size_t most = std::max(q.splits > 1 && !refined ? nq : 0, k.splits > 1 ? nk : 0) / 4;
         klaunch(attend_sum<T, DH>, dim3((unsigned)((most + 255) / 256), n), dim3(256), 0, st, sums, a.B, a.dh);
         GP_LAUNCH_CHECK();
     }

@@ -528,7 +528,7 @@ def attention_backward(q, k, v, out, lse, dout, q_lens=None, k_lens=None, q_star
                        bias: Optional[RelativeBias] = None, grads=None) -> AttentionGrads:
     """gp_attention_backward: the gradients of sum dout out with respect to q, k,
     v and the bias's table, from the out and lse that ``attention`` gave for the same
-    arguments.  out=None: without the rounding of out, slower.  grads: (dq, dk, dv), tensors of
+    arguments.  out=None: where it was not kept; slower.  grads: (dq, dk, dv), tensors of
     the shapes of q, k and v that receive them; allocated otherwise."""
     _no_graph(q, k, v, out, lse, dout, None if bias is None else bias.table, *(grads or ()), gradient="this call's results")
     cfg, rows, need = _attention(q, k, v, q_lens, k_lens, q_starts, causal, scale, bias, 1)

@@ -1,6 +1,6 @@
 """Gradients in bf16 whose delta is rid of the rounding of out, by the norms of their errors (attention_delta.py has the bounds, and
-test_attention_delta.py what exceeds them): with a bias, where the sums of dS correct it in one pass (no workgroup's keys are
-split), or it is summed from the weights (split keys, and calls without out); without a bias and without out."""
+test_attention_delta.py what exceeds them): with out, where the sums of dS correct it in one pass, with a bias and without, with keys that
+are split over workgroups and not; without out, where it is summed from the weights."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +48,51 @@ def test_from_the_weights(ops, dh, causal, size, with_out, buckets):
     r = ad.ratios(got, *ad.bounds(e, refined=False))
     assert set(r) == ({"dq", "dk", "dbias"} if buckets else {"dq", "dk"})
     assert all(x <= 1.0 for x in r.values()), r
+
+
+@pytest.mark.parametrize("dh", [32, 64, 72, 96, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("size,buckets", [(WHOLE, 0), (SPLIT, 0), (SPLIT, 32), (dict(B=3, H=2, K=1, Sq=70, Sk=600), 0)])
+def test_corrected_without_a_bias_and_over_splits(ops, dh, causal, size, buckets):
+    e, got = gradients(ops, dict(size, dh=dh), causal, buckets)
+    r = ad.ratios(got, *ad.bounds(e, refined=True))
+    assert set(r) == ({"dq", "dk", "dbias"} if buckets else {"dq", "dk"})
+    assert all(x <= 1.0 for x in r.values()), r
+
+
+@pytest.mark.parametrize("Sk", [2, 7, 12])
+@pytest.mark.parametrize("size", [dict(B=31, H=2, K=2, Sq=12), dict(B=16, H=16, K=16, Sq=150)])
+def test_few_keys(ops, size, Sk):
+    """Weights that are large, so that all that delta is off by reaches dK too."""
+    e, got = gradients(ops, dict(size, Sk=Sk, dh=64), False, 0)
+    r = ad.ratios(got, *ad.bounds(e, refined=True))
+    assert all(x <= 1.0 for x in r.values()), r
+
+
+def test_split_rows_captured_and_ragged(ops):
+    """The launch that joins the splits, in a graph, with sequences that end early or hold nothing; replayed with other inputs."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    B, H, K, Sq, Sk, dh = 3, 4, 2, 150, 700, 64
+    q, dout = (torch.randn(B, Sq, H, dh, generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(B, Sk, K, dh, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q_lens = torch.tensor([150, 33, 100], dtype=torch.int32, device="cuda")
+    k_lens = torch.tensor([700, 650, 0], dtype=torch.int32, device="cuda")
+
+    def step():
+        r = ops.attention(q, k, v, q_lens=q_lens, k_lens=k_lens)
+        return [*r, *ops.attention_backward(q, k, v, r.out, r.lse, dout, q_lens=q_lens, k_lens=k_lens)[:3]]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for _ in range(3):
+        for t in (q, k, v, dout):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(step(), outs))
+        dq, dk, dv = outs[2:]
+        assert (dq[1, 33:] == 0).all() and (dq[2] == 0).all() and (dk[1, 650:] == 0).all() and (dk[2] == 0).all() and (dv[2] == 0).all()
+        assert dq[:2].isfinite().all() and (dq[0] != 0).any()

@@ -720,6 +720,8 @@ gp_status gp_attention_workspace(const gp_attention_config* cfg, int backward, s
  *   dbias  : device fp32 [heads, buckets], overwritten; may be NULL.
  *   ws     : gp_attention_workspace(cfg, 1, &bytes).
  * No atomics: the same call gives the same bits.  The gradients must not overlap each other or any input.
+ * The weights come back from lse, which fp32 rounds by 2^-24 of itself, and are off by that: what is to mask is -1e30 or less,
+ * not a moderate bias (-1e9) that all of a row's keys may have.
  * GP_ERR_INVALID_ARG, GP_ERR_UNSUPPORTED: as gp_attention; lse NULL; dbias without a bias.
  */
 gp_status gp_attention_backward(const gp_attention_config* cfg, const gp_head_rows* q, const gp_head_rows* k,

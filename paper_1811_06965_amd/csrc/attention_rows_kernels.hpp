@@ -404,8 +404,9 @@ struct Work {
 // the next tile on its way while this one is used.  S^T = K Q^T puts a query's scores into one lane and its neighbour
 // half a wave on, so that the softmax needs one exchange per tile; P^T is then already the operand of O^T += V^T P^T.
 // Each row keeps its sums around a reference score, which follows the largest one only where that is 2^8 ahead: most
-// tiles rescale nothing.  Bound by vector instructions and products: 4 x 2048 queries and keys, 16 heads of 64, bf16, 95 us (723
-// TFLOP/s); 1000 queries to 50000 keys, width 128, 426 us (960); short loops by what surrounds them, 64 x 256 to up to 320 keys 43 us.
+// tiles rescale nothing.  Bound by vector instructions and products: 4 x 2048 queries and keys, 16 heads of 64, bf16, 93 to 96 us (723
+// TFLOP/s); 1000 queries to 50000 keys, width 128, 420 to 475 us from card to card (865 to 975); short loops by what surrounds them, 64 x 256
+// to up to 320 keys 42 to 50 us.
 // Few rows (KEYS): the W waves own the same 32 rows and every W-th tile each, without barriers, and join their sums in LDS: one
 // token of 4 sequences of up to 200 keys 7.2 us (8.4 by one wave), of 16 of up to 32768 266 us (5.3 TB/s; 276).
 template <typename T, int DH, int KT, int W, bool BIAS, bool KEYS>
@@ -915,7 +916,9 @@ template <typename T, int DH> __global__ void __launch_bounds__(256) attend_refi
 // dK and dV: a wave owns 32 keys and goes through the queries of all the heads that share them, in tiles of QT:
 //   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS,
 // and dS by distance for the bias's gradient.  Bound by vector instructions and products, at two waves a SIMD: 4 x 2048, 16 heads of 64,
-// bf16, 193 us with a bias, 45 of them for the distances; 64 x 256 queries to up to 320 keys 82 us.
+// bf16, 194 us with a bias, 45 of them for the distances; 64 x 256 queries to up to 320 keys 81 us.  In fp32 at 36 to 64 wide two waves
+// keep 5 registers in memory (33 with a bias) that one would not, yet take less: backward of 8 x 512, 16 heads of 64, 249 us for 266, with a bias
+// 285 for 304, 2 x 2048 896 for 961; of 2 x 2048 causal ones, whose workgroups are fewer, 695 for 616.
 template <typename T, int DH, int QT, int W, bool BIAS>
 __global__ void __launch_bounds__(64 * W, DH <= 64 ? 2 : 1) attend_dkv(AttendArgs a) {
     typedef Tile<T, DH, QT> Tl;

@@ -150,7 +150,7 @@ __device__ __forceinline__ void finish_row(const DistillOut& o, long row, Sum aw
 // with a running reference, four loads ahead of their use.  REST: the named tokens are left out of the sum, which
 // alone keeps the rest's share exact where the student gives it little (the difference of the sums would not): a byte
 // in LDS marks them in each chunk, WINDOW chunks at a time.  Bound by HBM where rows are many: 4096 of 128000 bf16 with 64 tokens
-// 183 us (5.7 TB/s), else by a row's chain of tokens, marks, loads and reductions: 93 rows of 50021 fp32 with 100 tokens 13.
+// 180 to 192 us (5.5 to 5.8 TB/s), else by a row's chain of tokens, marks, loads and reductions: 93 rows of 50021 fp32 with 100 tokens 13.
 // The next loads before these sums, in more registers, made the long rows 7% slower.
 constexpr int WINDOW = 16384;
 template <typename T, bool CLIP, bool REST, int NT>
